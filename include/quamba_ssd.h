@@ -39,7 +39,8 @@ typedef enum quamba_status {
     QUAMBA_OK = 0,
     QUAMBA_ENULL = -1,      /* a required pointer is NULL                                   */
     QUAMBA_ESHAPE = -2,     /* a dimension is non-positive, inconsistent or unsupported      */
-    QUAMBA_EWORKSPACE = -3, /* a shape needs more scratch memory than an entry point with a fixed scratch area has */
+    QUAMBA_EWORKSPACE = -3, /* a shape needs more scratch memory than an entry point with a fixed scratch area has,
+                               or a workspace that is required is missing, too small or not aligned */
     QUAMBA_EHIP = -4,       /* the HIP runtime refused the launch (no device, bad stream ...) */
     QUAMBA_EINVAL = -5      /* an argument value is invalid (unknown flag, bad permutation ...) */
 } quamba_status;
@@ -399,6 +400,95 @@ int quamba_quantize_x(const quamba_ssd_shape_t *shape, const quamba_ssd_scales_t
                       const float *x, int8_t *xq);
 int quamba_quantize_groups(int64_t tokens, int32_t ngroups, int32_t d_state, const float *group_scales,
                            const float *v, int8_t *vq);
+
+/* ---- the operators around a generated token: projections in 8-bit floating point, beams, their caches ---- */
+
+/* Element types of the tensors below that come in several. */
+typedef enum quamba_dtype { QUAMBA_F32 = 0, QUAMBA_F16 = 1, QUAMBA_BF16 = 2 } quamba_dtype;
+
+/*
+ * Quantizes a matrix to 8-bit floating point with one scale for each block of block_rows x 128 values: the operands of
+ * quamba_fp8_matmul.
+ *   x      device, x_type (quamba_dtype) [rows, cols], rows x_stride >= cols values apart
+ *   q      device e4m3 codes [rows, cols] (4 exponent bits, bias 7, 3 mantissa bits, largest 448, no infinities, 0x7f a NaN), rows
+ *          q_stride >= cols bytes apart; must not overlap x
+ *   scales device fp32 [ceil(rows / block_rows), ceil(cols / 128)], dense
+ *   block_rows  1 (activations: one scale for 128 values of a token) or 128 (weights)
+ * With top = max |x| of a block: scale = top / 448, and code = the e4m3 value nearest to x * (1 / scale), ties to even; the
+ * division, the reciprocal and the product are each rounded to fp32.  Where top / 448 is below 2^-126 (an all-zero
+ * block among them) the scale is 1.  A NaN or an infinity makes its whole block NaN: the scale and every code.  Blocks
+ * at the right and lower edge hold what there is.
+ * No rows or no columns: nothing is launched.  Any alignment and any stride are taken.
+ * Errors: ENULL, ESHAPE (negative sizes, strides below cols, more than 2^31 - 1 rows or 2^30
+ * columns), EINVAL (x_type,
+ * block_rows), EHIP.
+ */
+int quamba_fp8_quantize(int64_t rows, int64_t cols, int32_t block_rows, const void *x, int32_t x_type, int64_t x_stride,
+                        uint8_t *q, int64_t q_stride, float *scales, void *hip_stream);
+
+/*
+ * Matrix product of such operands, a projection's y = x w^T:
+ *   y[i, j] = sum over blocks b of 128 of  x_scales[i, b] * w_scales[j / 128, b] * sum over k in b of x[i, k] * w[j, k]
+ *   x device e4m3 [m, k], rows x_stride >= k bytes apart;  x_scales device fp32 [m, ceil(k / 128)]
+ *   w device e4m3 [n, k], rows w_stride >= k bytes apart;  w_scales device fp32 [ceil(n / 128), ceil(k / 128)]
+ *   y device y_type (quamba_dtype) [m, n], rows y_stride >= n values apart; must not overlap the operands
+ *   workspace  device scratch of workspace_bytes, 16-byte aligned
+ * Products and sums are fp32, rounded once to y_type; the sum over the blocks is made in parts where few outputs would
+ * leave the device idle, always in the same order.  A NaN code or a non-finite scale reaches the outputs that it belongs to
+ * and no others.  m = 0: nothing is launched.  Any alignment and any stride are taken; rows that start at multiples of 16
+ * bytes are read fastest.
+ * quamba_fp8_matmul_workspace_size is the scratch memory with which a product of this size takes its fastest launch on
+ * the current device (may be 0; 0 for invalid sizes).  With a workspace that is NULL, smaller or not aligned the sum is not split: same
+ * result to rounding.  Calls that share a workspace must not overlap.
+ * Errors: ENULL, ESHAPE (n or k not positive, m negative, strides, m or n above 2^31 - 1, k above 2^30), EINVAL (y_type), EHIP.
+ */
+size_t quamba_fp8_matmul_workspace_size(int64_t m, int64_t n, int64_t k);
+int quamba_fp8_matmul(int64_t m, int64_t n, int64_t k, const uint8_t *x, int64_t x_stride, const float *x_scales,
+                      const uint8_t *w, int64_t w_stride, const float *w_scales, void *y, int32_t y_type,
+                      int64_t y_stride, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * One step of a beam search: the best `count` continuations of every sequence over its beams and the vocabulary.
+ *   logits device, type (quamba_dtype) [batch, beams, vocab], rows of vocab values logits_stride >= vocab values apart
+ *   scores device fp32 [batch, beams]  log probability of each beam so far
+ *   finished device bytes [batch, beams] or NULL (none): not 0 for a beam that has ended
+ * Candidate (k, v) of a sequence is worth
+ *   scores[k] + ((logits[k, v] - max_k) - log sum over u of exp(logits[k, u] - max_k))
+ * in fp32, max_k the largest logit of the beam; a finished beam has one candidate, (k, pad_token), worth scores[k].  A logit of
+ * -infinity forbids its token.  A beam offers nothing whose score is not finite (a place that is still empty), which has a
+ * logit of NaN or +infinity, or none above -infinity.
+ *   out_scores  device fp32  [batch, count]  the values of the best candidates, best first; equal ones by rising beam, then token
+ *   out_parents device int32 [batch, count]  their beams            out_tokens device int32 [batch, count]  their tokens
+ * Where fewer candidates than `count` are left, the places behind them get the value -infinity, the beam (place mod beams) and
+ * pad_token.  Candidates of one beam are told apart by their logits.
+ *   workspace   device scratch of at least quamba_beam_select_workspace_size bytes, 16-byte aligned.  Calls that share it
+ *               must not overlap.
+ * batch = 0: nothing is launched.
+ * Errors: ENULL, ESHAPE (sizes not positive, beams > 64, count > 128, vocab > 2^30, beams * vocab > 2^32 - 1, 2^24 or more
+ * pieces of 16384 logits in all, stride), EINVAL (type, pad_token out of the vocabulary), EWORKSPACE (missing, too small or not aligned), EHIP.
+ */
+size_t quamba_beam_select_workspace_size(int32_t batch, int32_t beams, int32_t vocab, int32_t count);
+int quamba_beam_select(int32_t batch, int32_t beams, int32_t vocab, int32_t count, const void *logits, int32_t type,
+                       int64_t logits_stride, const float *scores, const uint8_t *finished, int32_t pad_token,
+                       float *out_scores, int32_t *out_parents, int32_t *out_tokens, void *workspace,
+                       size_t workspace_bytes, void *hip_stream);
+
+/* One cache of a beam search: the data of every beam of every sequence, device memory [batch, beams, bytes], dense. */
+typedef struct quamba_beam_cache_t {
+    void *data;
+    int64_t bytes; /* of one beam */
+} quamba_beam_cache_t;
+
+/*
+ * Moves the cached states behind a selection, in place: beam k of every sequence gets what beam parents[k] of that sequence held,
+ * in every one of n_caches caches (the scan's state in fp32 or 8 bits, the convolution's window, of every layer).
+ *   parents device int32 [batch, beams];  caches HOST array of n_caches structs, read before the call returns
+ * A beam that stays where it is is neither read (but by others) nor written.  An index outside 0 .. beams - 1 leaves its
+ * beam as it is.  Caches must not overlap.  batch = 0, no caches, or caches of 0 bytes: nothing is done for them.
+ * Errors: ENULL, ESHAPE (negative sizes, no beams, beams > 64, more than 2^34 bytes of a beam), EHIP.
+ */
+int quamba_beam_reorder(int32_t batch, int32_t beams, const int32_t *parents, int32_t n_caches,
+                        const quamba_beam_cache_t *caches, void *hip_stream);
 
 /* Static description of a quamba_status value. */
 const char *quamba_strerror(int status);

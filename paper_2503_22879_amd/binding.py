@@ -29,6 +29,8 @@ EXPORTED_SYMBOLS = ("quamba_ssd_prefill_workspace_size", "quamba_ssd_prefill", "
                     "quamba_ssd_prefill_gated", "quamba_ssd_decode_step_gated", "quamba_ssd_decode_step_q8_gated",
                     "quamba_reorder_params", "quamba_gather_rows", "quamba_quantize_x",
                     "quamba_quantize_groups", "quamba_strerror",
+                    "quamba_fp8_quantize", "quamba_fp8_matmul_workspace_size", "quamba_fp8_matmul",
+                    "quamba_beam_select_workspace_size", "quamba_beam_select", "quamba_beam_reorder",
                     # measurement helpers of the benchmark harness (include/quamba_probe.h)
                     "quamba_probe_mfma", "quamba_probe_stream_rmw", "quamba_probe_stream_read", "quamba_probe_clock",
                     "quamba_probe_clock_xcd")
@@ -51,6 +53,11 @@ class _ScalesStruct(C.Structure):
     """quamba_ssd_scales_t"""
     _fields_ = [("x_scales", C.c_void_p), ("head_cluster_end", C.c_void_p), ("chan_cluster_end", C.c_void_p),
                 ("B_scales", C.c_void_p), ("C_scales", C.c_void_p)]
+
+
+class _BeamCacheStruct(C.Structure):
+    """quamba_beam_cache_t"""
+    _fields_ = [("data", C.c_void_p), ("bytes", C.c_int64)]
 
 
 class _GateStruct(C.Structure):
@@ -146,6 +153,21 @@ def load_library():
                                           C.c_void_p]
         lib.quamba_quantize_groups.restype = C.c_int
         lib.quamba_quantize_groups.argtypes = [C.c_int64, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p]
+        lib.quamba_fp8_quantize.restype = C.c_int
+        lib.quamba_fp8_quantize.argtypes = [C.c_int64, C.c_int64, C.c_int32, C.c_void_p, C.c_int32, C.c_int64, C.c_void_p, C.c_int64,
+                                            C.c_void_p, C.c_void_p]
+        lib.quamba_fp8_matmul_workspace_size.restype = C.c_size_t
+        lib.quamba_fp8_matmul_workspace_size.argtypes = [C.c_int64] * 3
+        lib.quamba_fp8_matmul.restype = C.c_int
+        lib.quamba_fp8_matmul.argtypes = [C.c_int64] * 3 + [C.c_void_p, C.c_int64, C.c_void_p] * 2 + \
+            [C.c_void_p, C.c_int32, C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p]
+        lib.quamba_beam_select_workspace_size.restype = C.c_size_t
+        lib.quamba_beam_select_workspace_size.argtypes = [C.c_int32] * 4
+        lib.quamba_beam_select.restype = C.c_int
+        lib.quamba_beam_select.argtypes = [C.c_int32] * 4 + [C.c_void_p, C.c_int32, C.c_int64, C.c_void_p, C.c_void_p, C.c_int32] + \
+            [C.c_void_p] * 4 + [C.c_size_t, C.c_void_p]
+        lib.quamba_beam_reorder.restype = C.c_int
+        lib.quamba_beam_reorder.argtypes = [C.c_int32, C.c_int32, C.c_void_p, C.c_int32, C.POINTER(_BeamCacheStruct), C.c_void_p]
         lib.quamba_strerror.restype = C.c_char_p
         lib.quamba_strerror.argtypes = [C.c_int]
         _lib = lib
@@ -165,7 +187,8 @@ def _load_bind():
     mod.bind(*(C.cast(f, C.c_void_p).value for f in (
         lib.quamba_ssd_prefill_gated, lib.quamba_ssd_prefill_noalloc, lib.quamba_ssd_decode_step_gated,
         lib.quamba_ssd_decode_step_q8_gated, lib.quamba_ssd_quantize_state, lib.quamba_hadamard_quantize,
-        lib.quamba_mamba1_scan_gated, lib.quamba_mamba1_decode_step_gated, lib.quamba_conv1d_q8)), Shape, _ScalesStruct, _GateStruct,
+        lib.quamba_mamba1_scan_gated, lib.quamba_mamba1_decode_step_gated, lib.quamba_conv1d_q8, lib.quamba_fp8_quantize,
+        lib.quamba_fp8_matmul, lib.quamba_beam_select, lib.quamba_beam_reorder)), Shape, _ScalesStruct, _GateStruct,
         DeviceScales, Gate, lambda p: C.cast(p, C.c_void_p).value)
     _bind = mod
     return mod
@@ -317,6 +340,49 @@ def quamba_hadamard_quantize(y, s_y: float, out, stream=None) -> None:
     rc = (_bind or _load_bind()).hadamard(y, s_y, out, stream)
     if rc != 0:
         raise QuambaError(rc, "quamba_hadamard_quantize")
+
+
+def quamba_fp8_quantize(x, q, scales, block_rows: int = 1, stream=None) -> None:
+    """Enqueue q, scales = e4m3 codes of x [rows, cols] (fp32, fp16 or bf16; rows any distance apart) and one fp32 scale for each
+    block of block_rows (1: activations, 128: weights) x 128 values.  q: float8_e4m3fn or uint8, like x; scales:
+    [ceil(rows / block_rows), ceil(cols / 128)]."""
+    rc = (_bind or _load_bind()).fp8_quantize(x, q, scales, block_rows, stream)
+    if rc != 0:
+        raise QuambaError(rc, "quamba_fp8_quantize")
+
+
+def quamba_fp8_matmul_workspace_size(m: int, n: int, k: int) -> int:
+    return int(load_library().quamba_fp8_matmul_workspace_size(m, n, k))
+
+
+def quamba_fp8_matmul(x, x_scales, w, w_scales, y, workspace=None, stream=None) -> None:
+    """Enqueue y = x w^T of e4m3 codes x [m, k] with a scale for 1 x 128 values and w [n, k] with one for 128 x 128; y [m, n] in
+    fp32, fp16 or bf16.  The rows of x, w and y may lie any distance apart."""
+    rc = (_bind or _load_bind()).fp8_matmul(x, x_scales, w, w_scales, y, workspace, stream)
+    if rc != 0:
+        raise QuambaError(rc, "quamba_fp8_matmul")
+
+
+def quamba_beam_select_workspace_size(batch: int, beams: int, vocab: int, count: int) -> int:
+    return int(load_library().quamba_beam_select_workspace_size(batch, beams, vocab, count))
+
+
+def quamba_beam_select(logits, scores, out_scores, out_parents, out_tokens, workspace, finished=None, pad_token: int = 0,
+                       stream=None) -> None:
+    """Enqueue one step of a beam search: the out_scores.shape[1] best continuations of every sequence over its beams and the
+    vocabulary, best first.  logits [batch, beams, vocab] in fp32, fp16 or bf16 (rows one distance apart), scores [batch, beams]
+    fp32, finished [batch, beams] uint8 or bool; the outputs [batch, count] fp32, int32 and int32."""
+    rc = (_bind or _load_bind()).beam_select(logits, scores, out_scores, out_parents, out_tokens, workspace, finished, pad_token, stream)
+    if rc != 0:
+        raise QuambaError(rc, "quamba_beam_select")
+
+
+def quamba_beam_reorder(parents, caches, stream=None) -> None:
+    """Enqueue the move of cached states behind a selection, in place: caches is a sequence of contiguous tensors
+    [batch, beams, ...] of any type, parents int32 [batch, beams]."""
+    rc = (_bind or _load_bind()).beam_reorder(parents, caches, stream)
+    if rc != 0:
+        raise QuambaError(rc, "quamba_beam_reorder")
 
 
 def quamba_reorder_params(nheads, headdim, ngroups, m, n, d_state, x_calib_absmax, B_calib_absmax,

@@ -347,6 +347,107 @@ extern "C" int quamba_hadamard_quantize(const uint16_t *y, int64_t rows, int32_t
     return e == hipSuccess ? QUAMBA_OK : QUAMBA_EHIP;
 }
 
+namespace {
+
+bool known_type(int32_t t) { return t == QUAMBA_F32 || t == QUAMBA_F16 || t == QUAMBA_BF16; }
+
+}  // namespace
+
+extern "C" int quamba_fp8_quantize(int64_t rows, int64_t cols, int32_t block_rows, const void *x, int32_t x_type,
+                                   int64_t x_stride, uint8_t *q, int64_t q_stride, float *scales, void *hip_stream)
+{
+    if (rows < 0 || cols < 0 || rows > 0x7fffffffLL || cols > quamba::kFp8MaxDepth || x_stride < cols || q_stride < cols)
+        return QUAMBA_ESHAPE;
+    if (!known_type(x_type) || (block_rows != 1 && block_rows != 128)) return QUAMBA_EINVAL;
+    if (rows == 0 || cols == 0) return QUAMBA_OK;
+    if (!x || !q || !scales) return QUAMBA_ENULL;
+    quamba::QuantizeArgs a;
+    a.x = x; a.rows = rows; a.cols = cols; a.x_stride = x_stride;
+    a.q = q; a.q_stride = q_stride; a.scales = scales;
+    const hipError_t e = quamba::launch_fp8_quantize(a, block_rows, x_type, static_cast<hipStream_t>(hip_stream));
+    return e == hipSuccess ? QUAMBA_OK : QUAMBA_EHIP;
+}
+
+namespace {
+bool matmul_size(int64_t m, int64_t n, int64_t k)
+{
+    return m >= 0 && m <= 0x7fffffffLL && n > 0 && n <= 0x7fffffffLL && k > 0 && k <= quamba::kFp8MaxDepth;
+}
+}  // namespace
+
+extern "C" size_t quamba_fp8_matmul_workspace_size(int64_t m, int64_t n, int64_t k)
+{
+    return matmul_size(m, n, k) && m ? quamba::fp8_matmul_workspace_bytes((int32_t)m, (int32_t)n, (int32_t)k) : 0;
+}
+
+extern "C" int quamba_fp8_matmul(int64_t m, int64_t n, int64_t k, const uint8_t *x, int64_t x_stride,
+                                 const float *x_scales, const uint8_t *w, int64_t w_stride, const float *w_scales,
+                                 void *y, int32_t y_type, int64_t y_stride, void *workspace, size_t workspace_bytes,
+                                 void *hip_stream)
+{
+    if (!matmul_size(m, n, k) || x_stride < k || w_stride < k || y_stride < n) return QUAMBA_ESHAPE;
+    if (!known_type(y_type)) return QUAMBA_EINVAL;
+    if (m == 0) return QUAMBA_OK;
+    if (!x || !x_scales || !w || !w_scales || !y) return QUAMBA_ENULL;
+    quamba::MatmulArgs a;
+    a.x = x; a.x_stride = x_stride; a.x_scales = x_scales;
+    a.w = w; a.w_stride = w_stride; a.w_scales = w_scales;
+    a.y = y; a.y_type = y_type; a.y_stride = y_stride;
+    a.m = (int32_t)m; a.n = (int32_t)n; a.k = (int32_t)k; a.blocks = (int32_t)((k + 127) / 128);
+    // a workspace that is missing, too small or not aligned selects the launch that needs none
+    if (!workspace || !aligned16(workspace) || workspace_bytes < quamba_fp8_matmul_workspace_size(m, n, k)) workspace = nullptr;
+    const hipError_t e = quamba::launch_fp8_matmul(a, workspace, static_cast<hipStream_t>(hip_stream));
+    return e == hipSuccess ? QUAMBA_OK : QUAMBA_EHIP;
+}
+
+namespace {
+bool select_size(int32_t batch, int32_t beams, int32_t vocab, int32_t count)
+{
+    return batch >= 0 && beams > 0 && beams <= quamba::kMaxBeams && vocab > 0 && count > 0 && count <= quamba::kMaxChoices &&
+           quamba::beam_select_supports(batch, beams, vocab);
+}
+}  // namespace
+
+extern "C" size_t quamba_beam_select_workspace_size(int32_t batch, int32_t beams, int32_t vocab, int32_t count)
+{
+    return select_size(batch, beams, vocab, count) ? quamba::beam_select_workspace_bytes(batch, beams, vocab, count) : 0;
+}
+
+extern "C" int quamba_beam_select(int32_t batch, int32_t beams, int32_t vocab, int32_t count, const void *logits,
+                                  int32_t type, int64_t logits_stride, const float *scores, const uint8_t *finished,
+                                  int32_t pad_token, float *out_scores, int32_t *out_parents, int32_t *out_tokens,
+                                  void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    if (!select_size(batch, beams, vocab, count) || logits_stride < vocab) return QUAMBA_ESHAPE;
+    if (!known_type(type) || pad_token < 0 || pad_token >= vocab) return QUAMBA_EINVAL;
+    if (batch == 0) return QUAMBA_OK;
+    if (!logits || !scores || !out_scores || !out_parents || !out_tokens) return QUAMBA_ENULL;
+    if (!workspace || !aligned16(workspace) ||
+        workspace_bytes < quamba::beam_select_workspace_bytes(batch, beams, vocab, count))
+        return QUAMBA_EWORKSPACE;
+    quamba::SelectArgs a;
+    a.logits = logits; a.type = type; a.stride = logits_stride; a.scores = scores; a.finished = finished;
+    a.out_scores = out_scores; a.out_parents = out_parents; a.out_tokens = out_tokens;
+    a.batch = batch; a.beams = beams; a.vocab = vocab; a.count = count; a.pad = pad_token;
+    const hipError_t e = quamba::launch_beam_select(a, workspace, static_cast<hipStream_t>(hip_stream));
+    return e == hipSuccess ? QUAMBA_OK : QUAMBA_EHIP;
+}
+
+extern "C" int quamba_beam_reorder(int32_t batch, int32_t beams, const int32_t *parents, int32_t n_caches,
+                                   const quamba_beam_cache_t *caches, void *hip_stream)
+{
+    if (batch < 0 || beams <= 0 || beams > quamba::kMaxBeams || n_caches < 0) return QUAMBA_ESHAPE;
+    if (batch == 0 || n_caches == 0) return QUAMBA_OK;
+    if (!parents || !caches) return QUAMBA_ENULL;
+    for (int32_t i = 0; i < n_caches; ++i) {
+        if (caches[i].bytes < 0 || caches[i].bytes > quamba::kMaxCacheBytes) return QUAMBA_ESHAPE;
+        if (caches[i].bytes > 0 && !caches[i].data) return QUAMBA_ENULL;
+    }
+    const hipError_t e = quamba::launch_beam_reorder(batch, beams, parents, n_caches, caches,
+                                                     static_cast<hipStream_t>(hip_stream));
+    return e == hipSuccess ? QUAMBA_OK : QUAMBA_EHIP;
+}
+
 extern "C" const char *quamba_strerror(int status)
 {
     switch (status) {

@@ -13,6 +13,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <initializer_list>
+#include <vector>
 
 #include "quamba_ssd.h"
 
@@ -29,6 +30,10 @@ struct Entry {
     decltype(&quamba_mamba1_scan_gated) mamba1_scan;
     decltype(&quamba_mamba1_decode_step_gated) mamba1_decode;
     decltype(&quamba_conv1d_q8) conv1d;
+    decltype(&quamba_fp8_quantize) fp8_quantize;
+    decltype(&quamba_fp8_matmul) fp8_matmul;
+    decltype(&quamba_beam_select) beam_select;
+    decltype(&quamba_beam_reorder) beam_reorder;
 } entry;
 
 // The ctypes structures that carry the shape, the scale tables and the side inputs, and the classes that are read directly:
@@ -410,6 +415,151 @@ PyObject *conv1d(PyObject *const *a)
     return call([&] { return entry.conv1d(&s, &sc, in, weight, bias, scale, st_in, x, B, C, st_out, stream); });
 }
 
+// A device matrix whose rows lie any distance apart; values of a row lie side by side.
+struct Matrix {
+    void *p;
+    int64_t rows, cols, stride;
+    at::ScalarType type;
+    Matrix(PyObject *o, const char *name)
+    {
+        const at::Tensor *t = tensor_or_null(o, name);
+        if (!t || t->dim() != 2) fail(PyExc_ValueError, "%s must be a tensor of rows and columns", name);
+        rows = t->size(0);
+        cols = t->size(1);
+        if (!t->is_cuda() || (cols > 1 && t->stride(1) != 1) || (rows > 1 && t->stride(0) < cols))
+            fail(PyExc_ValueError, "%s must be a device tensor with rows of adjacent values that do not overlap", name);
+        stride = rows > 1 ? t->stride(0) : cols;
+        type = t->scalar_type();
+        p = t->data_ptr();
+    }
+    // e4m3 codes, as such or as plain bytes
+    uint8_t *codes(const char *name) const
+    {
+        if (type != at::kFloat8_e4m3fn && type != at::kByte)
+            fail(PyExc_ValueError, "%s must have dtype torch.float8_e4m3fn or torch.uint8", name);
+        return static_cast<uint8_t *>(p);
+    }
+    void expect(int64_t r, int64_t c, const char *name) const
+    {
+        if (rows != r || cols != c) {
+            PyErr_Format(PyExc_ValueError, "%s must have shape (%lld, %lld), got (%lld, %lld)", name, (long long)r, (long long)c,
+                         (long long)rows, (long long)cols);
+            throw Fail();
+        }
+    }
+};
+
+int32_t dtype_of(at::ScalarType type, const char *name)
+{
+    switch (type) {
+        case at::kFloat: return QUAMBA_F32;
+        case at::kHalf: return QUAMBA_F16;
+        case at::kBFloat16: return QUAMBA_BF16;
+        default: fail(PyExc_ValueError, "%s must have dtype torch.float32, torch.float16 or torch.bfloat16", name);
+    }
+}
+
+int64_t blocks(int64_t n, int64_t of) { return (n + of - 1) / of; }
+
+int64_t integer(PyObject *o)
+{
+    const long long v = PyLong_AsLongLong(o);
+    if (v == -1 && PyErr_Occurred()) throw Fail();
+    return v;
+}
+
+int32_t small_integer(PyObject *o, const char *name)
+{
+    const int64_t v = integer(o);
+    if (v < INT32_MIN || v > INT32_MAX) fail(PyExc_ValueError, "%s does not fit 32 bits", name);
+    return (int32_t)v;
+}
+
+// x, q, scales, block_rows, stream
+PyObject *fp8_quantize(PyObject *const *a)
+{
+    const Matrix x(a[0], "x"), q(a[1], "q");
+    const int32_t block_rows = small_integer(a[3], "block_rows"), type = dtype_of(x.type, "x");
+    uint8_t *codes = q.codes("q");
+    q.expect(x.rows, x.cols, "q");
+    float *scales = pointer<float>(a[2], at::kFloat, {blocks(x.rows, block_rows > 0 ? block_rows : 1), blocks(x.cols, 128)}, "scales");
+    void *stream = stream_of(a[4]);
+    return call([&] { return entry.fp8_quantize(x.rows, x.cols, block_rows, x.p, type, x.stride, codes, q.stride, scales, stream); });
+}
+
+// x, x_scales, w, w_scales, y, workspace, stream
+PyObject *fp8_matmul(PyObject *const *a)
+{
+    const Matrix x(a[0], "x"), w(a[2], "w"), y(a[4], "y");
+    const uint8_t *xc = x.codes("x"), *wc = w.codes("w");
+    w.expect(w.rows, x.cols, "w");
+    y.expect(x.rows, w.rows, "y");
+    const int32_t type = dtype_of(y.type, "y");
+    const float *xs = pointer<float>(a[1], at::kFloat, {x.rows, blocks(x.cols, 128)}, "x_scales");
+    const float *ws = pointer<float>(a[3], at::kFloat, {blocks(w.rows, 128), blocks(x.cols, 128)}, "w_scales");
+    const at::Tensor *space = tensor_or_null(a[5], "workspace");
+    void *sp = device_pointer(space, "workspace");
+    const size_t bytes = space ? (size_t)space->numel() * space->element_size() : 0;
+    void *stream = stream_of(a[6]);
+    return call([&] {
+        return entry.fp8_matmul(x.rows, w.rows, x.cols, xc, x.stride, xs, wc, w.stride, ws, y.p, type, y.stride, sp, bytes, stream);
+    });
+}
+
+// logits, scores, out_scores, out_parents, out_tokens, workspace, finished, pad_token, stream
+PyObject *beam_select(PyObject *const *a)
+{
+    const at::Tensor *logits = tensor_or_null(a[0], "logits"), *best = tensor_or_null(a[2], "out_scores");
+    if (!logits || logits->dim() != 3) fail(PyExc_ValueError, "%s must be a tensor [batch, beams, vocab]", "logits");
+    if (!best || best->dim() != 2) fail(PyExc_ValueError, "%s must be a tensor [batch, count]", "out_scores");
+    const int64_t b = logits->size(0), K = logits->size(1), V = logits->size(2), count = best->size(1);
+    if (b > INT32_MAX || K > INT32_MAX || V > INT32_MAX || count > INT32_MAX) return PyLong_FromLong(QUAMBA_ESHAPE);
+    const int64_t stride = K > 1 ? logits->stride(1) : b > 1 ? logits->stride(0) : V;
+    if (!logits->is_cuda() || (V > 1 && logits->stride(2) != 1) || (K > 1 && b > 1 && logits->stride(0) != K * stride))
+        fail(PyExc_ValueError, "%s must be a device tensor with rows of adjacent values, one distance apart", "logits");
+    const int32_t type = dtype_of(logits->scalar_type(), "logits");
+    const float *scores = pointer<float>(a[1], at::kFloat, {b, K}, "scores");
+    float *out = pointer<float>(a[2], at::kFloat, {b, count}, "out_scores");
+    int32_t *parents = pointer<int32_t>(a[3], at::kInt, {b, count}, "out_parents");
+    int32_t *tokens = pointer<int32_t>(a[4], at::kInt, {b, count}, "out_tokens");
+    const at::Tensor *space = tensor_or_null(a[5], "workspace");
+    void *sp = device_pointer(space, "workspace");
+    const size_t bytes = space ? (size_t)space->numel() * space->element_size() : 0;
+    const at::Tensor *finished = tensor_or_null(a[6], "finished");
+    const bool flags = finished && finished->scalar_type() == at::kBool;
+    const uint8_t *done = pointer<uint8_t>(a[6], flags ? at::kBool : at::kByte, {b, K}, "finished");
+    const int32_t pad = small_integer(a[7], "pad_token");
+    void *stream = stream_of(a[8]);
+    void *lp = logits->data_ptr();
+    return call([&] {
+        return entry.beam_select((int32_t)b, (int32_t)K, (int32_t)V, (int32_t)count, lp, type, stride, scores, done, pad, out, parents,
+                                 tokens, sp, bytes, stream);
+    });
+}
+
+// parents, caches (a sequence of tensors [batch, beams, ...]), stream
+PyObject *beam_reorder(PyObject *const *a)
+{
+    const at::Tensor *t = tensor_or_null(a[0], "parents");
+    if (!t || t->dim() != 2) fail(PyExc_ValueError, "%s must be a tensor [batch, beams]", "parents");
+    const int64_t b = t->size(0), K = t->size(1);
+    if (b > INT32_MAX || K > INT32_MAX) return PyLong_FromLong(QUAMBA_ESHAPE);
+    const int32_t *parents = pointer<int32_t>(a[0], at::kInt, {b, K}, "parents");
+    Ref list(PySequence_Fast(a[1], "caches must be a sequence of tensors"));
+    const Py_ssize_t n = PySequence_Fast_GET_SIZE(list.o);
+    if (n > INT32_MAX) return PyLong_FromLong(QUAMBA_ESHAPE);
+    std::vector<quamba_beam_cache_t> caches((size_t)n);
+    for (Py_ssize_t i = 0; i < n; ++i) {
+        const at::Tensor *c = tensor_or_null(PySequence_Fast_GET_ITEM(list.o, i), "every cache");
+        if (!c || c->dim() < 2 || c->size(0) != b || c->size(1) != K)
+            fail(PyExc_ValueError, "%s must be a tensor [batch, beams, ...]", "every cache");
+        caches[i].data = device_pointer(c, "every cache");
+        caches[i].bytes = b && K ? (int64_t)(c->numel() / (b * K) * c->element_size()) : 0;
+    }
+    void *stream = stream_of(a[2]);
+    return call([&] { return entry.beam_reorder((int32_t)b, (int32_t)K, parents, (int32_t)n, caches.data(), stream); });
+}
+
 template <PyObject *(*F)(PyObject *const *), int N>
 PyObject *method(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
@@ -427,7 +577,7 @@ PyObject *method(PyObject *, PyObject *const *a, Py_ssize_t n)
 // The addresses of the library's functions, in the order of Entry, and what binding.py has for the objects above.
 PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
-    constexpr int kEntries = 9;
+    constexpr int kEntries = 13;
     PyObject **const objects[] = {&shape_type, &scales_type, &gate_struct_type, &device_scales_type, &gate_type, &address_of};
     constexpr int kObjects = sizeof(objects) / sizeof(objects[0]);
     void *p[kEntries];
@@ -467,6 +617,10 @@ PyMethodDef methods[] = {
     QUAMBA_METHOD(mamba1_scan, 13),
     QUAMBA_METHOD(mamba1_decode, 12),
     QUAMBA_METHOD(conv1d, 12),
+    QUAMBA_METHOD(fp8_quantize, 5),
+    QUAMBA_METHOD(fp8_matmul, 7),
+    QUAMBA_METHOD(beam_select, 9),
+    QUAMBA_METHOD(beam_reorder, 3),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_bind", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -385,4 +385,48 @@ hipError_t launch_prefill_shared(const SsdArgs &a, void *workspace, bool precise
 hipError_t launch_prefill_wide(const SsdArgs &a, bool halves, bool precise, hipStream_t stream);
 bool prefill_generic_supports(const quamba_ssd_shape_t &s);
 
+// ---- 8-bit floating point (e4m3 with a scale for each block of 128) ----
+constexpr int64_t kFp8MaxDepth = (int64_t)1 << 30;  // columns of a matrix
+struct QuantizeArgs {
+    const void *x;
+    int64_t rows, cols, x_stride, q_stride;  // strides in values
+    uint8_t *q;
+    float *scales;
+    // set by the launcher
+    Divisor by_row_blocks;
+    int32_t row_blocks;  // blocks along a row
+    int32_t blocks;      // of the launch
+};
+hipError_t launch_fp8_quantize(QuantizeArgs a, int32_t block_rows, int32_t x_type, hipStream_t stream);
+struct MatmulArgs {
+    const uint8_t *x, *w;
+    const float *x_scales, *w_scales;
+    void *y;
+    int64_t x_stride, w_stride, y_stride;
+    int32_t m, n, k;
+    int32_t blocks;      // of the depth
+    int32_t y_type;
+};
+size_t fp8_matmul_workspace_bytes(int32_t m, int32_t n, int32_t k);
+hipError_t launch_fp8_matmul(const MatmulArgs &a, void *workspace, hipStream_t stream);
+
+// ---- beams ----
+constexpr int kMaxBeams = 64;
+constexpr int kMaxChoices = 128;
+constexpr int64_t kMaxCacheBytes = (int64_t)1 << 34;  // of a beam
+struct SelectArgs {
+    const void *logits;
+    int64_t stride;      // values from row to row
+    const float *scores;
+    const uint8_t *finished;  // or null
+    float *out_scores;
+    int32_t *out_parents, *out_tokens;
+    int32_t batch, beams, vocab, count, pad, type;
+};
+bool beam_select_supports(int32_t batch, int32_t beams, int32_t vocab);
+size_t beam_select_workspace_bytes(int32_t batch, int32_t beams, int32_t vocab, int32_t count);
+hipError_t launch_beam_select(const SelectArgs &a, void *workspace, hipStream_t stream);
+hipError_t launch_beam_reorder(int32_t batch, int32_t beams, const int32_t *parents, int32_t n, const quamba_beam_cache_t *caches,
+                               hipStream_t stream);
+
 }  // namespace quamba
