@@ -440,7 +440,8 @@ int quamba_fp8_quantize(int64_t rows, int64_t cols, int32_t block_rows, const vo
  * quamba_fp8_matmul_workspace_size is the scratch memory with which a product of this size takes its fastest launch on
  * the current device (may be 0; 0 for invalid sizes).  With a workspace that is NULL, smaller or not aligned the sum is not split: same
  * result to rounding.  Calls that share a workspace must not overlap.
- * Errors: ENULL, ESHAPE (n or k not positive, m negative, strides, m or n above 2^31 - 1, k above 2^30), EINVAL (y_type), EHIP.
+ * Errors: ENULL, ESHAPE (n or k not positive, m negative, strides, m above 2^31 - 1, n above 2^26, k above
+ * 2^30), EINVAL (y_type), EHIP.
  */
 size_t quamba_fp8_matmul_workspace_size(int64_t m, int64_t n, int64_t k);
 int quamba_fp8_matmul(int64_t m, int64_t n, int64_t k, const uint8_t *x, int64_t x_stride, const float *x_scales,

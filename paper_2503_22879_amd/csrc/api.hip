@@ -371,7 +371,7 @@ extern "C" int quamba_fp8_quantize(int64_t rows, int64_t cols, int32_t block_row
 namespace {
 bool matmul_size(int64_t m, int64_t n, int64_t k)
 {
-    return m >= 0 && m <= 0x7fffffffLL && n > 0 && n <= 0x7fffffffLL && k > 0 && k <= quamba::kFp8MaxDepth;
+    return m >= 0 && m <= 0x7fffffffLL && n > 0 && n <= quamba::kFp8MaxColumns && k > 0 && k <= quamba::kFp8MaxDepth;
 }
 }  // namespace
 

@@ -78,29 +78,273 @@ __device__ __forceinline__ void store(void *y, int type, int64_t at, float v)
         static_cast<__bf16 *>(y)[at] = (__bf16)v;
 }
 
-// A wave for 16 x 16 outputs, operands from memory to registers.
-__global__ __launch_bounds__(64) void fp8_matmul_any_kernel(MatmulArgs a)
+// ---- up to 64 rows of x: the weight streams past ----
+
+// A workgroup takes 16 columns of y (rows of w) over the whole depth, every wave one block in 8; codes go from memory to registers.
+template <int MF>  // 16-row parts of x
+__global__ __launch_bounds__(512) void fp8_matmul_rows_kernel(MatmulArgs a)
 {
-    const int lane = threadIdx.x, r = lane & 15, part = lane >> 4;
-    const int64_t i = (int64_t)blockIdx.y * 16 + r, j = (int64_t)blockIdx.x * 16 + r;  // this lane's rows of x and of w
-    const uint8_t *xp = a.x + min(i, (int64_t)a.m - 1) * a.x_stride, *wp = a.w + min(j, (int64_t)a.n - 1) * a.w_stride;
-    const float *xs = a.x_scales + min(i, (int64_t)a.m - 1) * a.blocks;
-    const float *ws = a.w_scales + (int64_t)(blockIdx.x * 16 / kBlock) * a.blocks;
-    float4v sum{0, 0, 0, 0};
-    for (int b = 0; b < a.blocks; ++b) {
-        const int k = b * kBlock + part * 32;
-        const Part x(load16(xp + k, a.k - k), load16(xp + k + 16, a.k - k - 16));
-        const Part w(load16(wp + k, a.k - k), load16(wp + k + 16, a.k - k - 16));
-        const float4v p = multiply(w, x);
-        const float s = xs[b] * ws[b];
+    constexpr int kWaves = 8, kAhead = MF == 1 ? 4 : 2;
+    __shared__ float red[kWaves][MF * 4][64];
+    const int lane = threadIdx.x & 63, r = lane & 15, part = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n0 = blockIdx.x * 16;
+    const uint8_t *wp = a.w + (int64_t)min(n0 + r, a.n - 1) * a.w_stride + part * 32;
+    const uint8_t *xp[MF];
+    const float *xs[MF];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sum[e] = fmaf(p[e], s, sum[e]);
+    for (int f = 0; f < MF; ++f) {
+        const int64_t row = min(f * 16 + r, a.m - 1);
+        xp[f] = a.x + row * a.x_stride + part * 32;
+        xs[f] = a.x_scales + row * a.blocks;
     }
-    const int64_t jo = (int64_t)blockIdx.x * 16 + part * 4;
-    if (i < a.m)
+    const float *ws = a.w_scales + (int64_t)(n0 / kBlock) * a.blocks;
+    float4v sum[MF];
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (jo + e < a.n) store(a.y, a.y_type, i * a.y_stride + jo + e, sum[e]);
+    for (int f = 0; f < MF; ++f) sum[f] = float4v{0, 0, 0, 0};
+    auto step = [&](int b, const int4v &w0, const int4v &w1, const int4v *x, const float *s) {
+        const Part w(w0, w1);
+#pragma unroll
+        for (int f = 0; f < MF; ++f) {
+            const float4v p = multiply(w, Part(x[2 * f], x[2 * f + 1]));
+            const float scale = s[f] * ws[b];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[f][e] = fmaf(p[e], scale, sum[f][e]);
+        }
+    };
+    const int whole = a.k / kBlock;
+    int b = wave;
+    for (; b + (kAhead - 1) * kWaves < whole; b += kAhead * kWaves) {
+        int4v w[kAhead][2], x[kAhead][2 * MF];
+        float s[kAhead][MF];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int64_t k = (int64_t)(b + u * kWaves) * kBlock;
+            __builtin_memcpy(&w[u][0], wp + k, 16);
+            __builtin_memcpy(&w[u][1], wp + k + 16, 16);
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+            for (int f = 0; f < MF; ++f) {
+                const int64_t k = (int64_t)(b + u * kWaves) * kBlock;
+                __builtin_memcpy(&x[u][2 * f], xp[f] + k, 16);
+                __builtin_memcpy(&x[u][2 * f + 1], xp[f] + k + 16, 16);
+                s[u][f] = xs[f][b + u * kWaves];
+            }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) step(b + u * kWaves, w[u][0], w[u][1], x[u], s[u]);
+    }
+    for (; b < a.blocks; b += kWaves) {
+        const int64_t k = (int64_t)b * kBlock;
+        const int left = a.k - b * kBlock - part * 32;
+        int4v x[2 * MF];
+        float s[MF];
+#pragma unroll
+        for (int f = 0; f < MF; ++f) {
+            x[2 * f] = load16(xp[f] + k, left);
+            x[2 * f + 1] = load16(xp[f] + k + 16, left - 16);
+            s[f] = xs[f][b];
+        }
+        step(b, load16(wp + k, left), load16(wp + k + 16, left - 16), x, s);
+    }
+#pragma unroll
+    for (int f = 0; f < MF; ++f)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) red[wave][4 * f + e][lane] = sum[f][e];
+    __syncthreads();
+    for (int t = threadIdx.x; t < MF * 256; t += 512) {
+        const int i = t >> 4, j = t & 15;
+        const int at = 4 * (i >> 4) + (j & 3), from = (j >> 2) * 16 + (i & 15);
+        float v = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) v += red[w][at][from];
+        if (i < a.m && n0 + j < a.n) store(a.y, a.y_type, i * a.y_stride + n0 + j, v);
+    }
+}
+
+// ---- more rows: tiles of x and w in LDS ----
+
+// 16 (or 4) bytes for each lane from `base` + its offset into LDS at `to` + 16 (4) times the lane, without a register between.  Their
+// arrival counts as a vector load's: wait_for_tiles() waits for it.
+__device__ __forceinline__ void load_to_lds16(const void *base, uint32_t offset, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory", "m0");
+}
+__device__ __forceinline__ void load_to_lds4(const void *base, uint32_t offset, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory", "m0");
+}
+__device__ __forceinline__ void wait_for_tiles() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+__device__ __forceinline__ uint32_t lds_address(const void *p)
+{
+    return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char *)p;
+}
+
+// The order of the tiles: the device hands workgroups to its 8 dies in turn, so every eighth one belongs to a die; each die gets
+// consecutive tiles, and these go up and down bands of 8 tiles along m, so that the die's cache holds what they share.
+__device__ __forceinline__ void tile_of(int id, int tiles_m, int tiles_n, int &tm, int &tn)
+{
+    constexpr int kDies = 8, kBand = 8;
+    const int all = tiles_m * tiles_n, each = all / kDies, more = all % kDies, die = id % kDies;
+    id = die * each + min(die, more) + id / kDies;
+    const int band = id / (kBand * tiles_n), first = band * kBand, rows = min(kBand, tiles_m - first);
+    const int in_band = id - first * tiles_n;
+    tn = in_band / rows;
+    tm = first + in_band - tn * rows;
+}
+
+// BM x BN outputs to a workgroup of WM x WN waves.  LDS holds two blocks (128 codes deep) of BM + BN rows and the scales of x's rows; the next
+// block arrives while one is multiplied.  The 16-byte pieces of a row are stored in an order that depends on the row (piece c
+// of row r at c ^ (r % 8)), so that the 8 lanes that read together hit different banks.  DIRECT: rows at multiples of 16
+// bytes less than 2^24 bytes apart go from memory to LDS by themselves; else through registers.
+template <int BM, int BN, int WM, int WN, bool DIRECT>
+__global__ __launch_bounds__(64 * WM * WN, 2) void fp8_matmul_tile_kernel(MatmulArgs a, int tiles_m, int tiles_n)
+{
+    constexpr int kWaves = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
+    constexpr int kRows = BM + BN, kScales = kRows * kBlock, kStage = kScales + BM * 4;
+    static_assert(kRows / 8 % kWaves == 0 && BM % 64 == 0 && BM / 64 <= kWaves && BN % 128 == 0 && (BN / WN) <= 128, "");
+    extern __shared__ char lds[];
+    const int lane = threadIdx.x & 63, r = lane & 15, part = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave % WM, wn = wave / WM;
+    int tm, tn;
+    tile_of(blockIdx.x, tiles_m, tiles_n, tm, tn);
+    const int m0 = tm * BM, n0 = tn * BN;
+    const uint8_t *xb = a.x + (int64_t)m0 * a.x_stride, *wb = a.w + (int64_t)n0 * a.w_stride;
+    const float *xsb = a.x_scales + (int64_t)m0 * a.blocks;
+    const auto *ws = (const __attribute__((address_space(4))) float *)(a.w_scales + (int64_t)((n0 + wn * (BN / WN)) / kBlock) * a.blocks);
+    const int last_x = a.m - 1 - m0, last_w = a.n - 1 - n0;
+
+    // 8 rows of a tile in turn: this lane's piece of them
+    constexpr int kTurns = kRows / 8 / kWaves;
+    const int piece = (lane & 7) ^ (lane >> 3);
+    auto row_of = [&](int turn) { return (turn * kWaves + wave) * 8 + (lane >> 3); };
+    auto is_x = [&](int turn) { return (turn * kWaves + wave) * 8 < BM; };
+    uint32_t offset[DIRECT ? kTurns : 1], scale_offset = 0;
+    if (DIRECT) {
+#pragma unroll
+        for (int t = 0; t < kTurns; ++t)
+            offset[t] = is_x(t) ? (uint32_t)min(row_of(t), last_x) * (uint32_t)a.x_stride + piece * 16
+                                : (uint32_t)min(row_of(t) - BM, last_w) * (uint32_t)a.w_stride + piece * 16;
+        scale_offset = (uint32_t)min(wave * 64 + lane, last_x) * (uint32_t)a.blocks * 4;
+    }
+    const uint32_t base = lds_address(lds);
+    auto start = [&](int b) {  // DIRECT: a whole block on its way
+        const uint32_t to = base + (b & 1) * kStage;
+        const uint8_t *x = xb + (int64_t)b * kBlock, *w = wb + (int64_t)b * kBlock;
+#pragma unroll
+        for (int t = 0; t < kTurns; ++t) load_to_lds16(is_x(t) ? x : w, offset[t], to + (t * kWaves + wave) * 1024);
+        if (wave < BM / 64) load_to_lds4(xsb + b, scale_offset, to + kScales + wave * 256);
+    };
+    int4v held[kTurns];
+    float held_scale = 0.0f;
+    auto fetch = [&](int b) {  // any block, to registers
+        const int left = a.k - b * kBlock - piece * 16;
+#pragma unroll
+        for (int t = 0; t < kTurns; ++t) {
+            const uint8_t *p = is_x(t) ? xb + (int64_t)min(row_of(t), last_x) * a.x_stride : wb + (int64_t)min(row_of(t) - BM, last_w) * a.w_stride;
+            held[t] = load16(p + (int64_t)b * kBlock + piece * 16, left);
+        }
+        if ((int)threadIdx.x < BM) held_scale = xsb[(int64_t)min((int)threadIdx.x, last_x) * a.blocks + b];
+    };
+    auto put = [&](int b) {
+        char *to = lds + (b & 1) * kStage;
+#pragma unroll
+        for (int t = 0; t < kTurns; ++t) *reinterpret_cast<int4v *>(to + (t * kWaves + wave) * 1024 + lane * 16) = held[t];
+        if ((int)threadIdx.x < BM) reinterpret_cast<float *>(to + kScales)[threadIdx.x] = held_scale;
+    };
+
+    float4v sum[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) sum[i][j] = float4v{0, 0, 0, 0};
+    const int at = r * kBlock + ((2 * part) ^ (r & 7)) * 16;
+    auto compute = [&](int b) {
+        const char *x = lds + (b & 1) * kStage + wm * (BM / WM) * kBlock, *w = lds + (b & 1) * kStage + (BM + wn * (BN / WN)) * kBlock;
+        const float *xs = reinterpret_cast<const float *>(lds + (b & 1) * kStage + kScales) + wm * (BM / WM) + r;
+        const float wsc = ws[b];
+        Part wf[TN];
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+            wf[j] = Part(*reinterpret_cast<const int4v *>(w + j * 16 * kBlock + at), *reinterpret_cast<const int4v *>(w + j * 16 * kBlock + (at ^ 16)));
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            const Part xf(*reinterpret_cast<const int4v *>(x + i * 16 * kBlock + at), *reinterpret_cast<const int4v *>(x + i * 16 * kBlock + (at ^ 16)));
+            const float s = xs[i * 16] * wsc;
+            float4v p[TN];
+#pragma unroll
+            for (int j = 0; j < TN; ++j) p[j] = multiply(wf[j], xf);
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum[i][j][e] = fmaf(p[j][e], s, sum[i][j][e]);
+        }
+    };
+
+    if (DIRECT) {
+        const int whole = a.k / kBlock;
+        if (whole) start(0);
+        for (int b = 0; b < whole; ++b) {
+            wait_for_tiles();  // block b is there for all waves, and block b - 1 has been read by all
+            if (b + 1 < whole) start(b + 1);
+            compute(b);
+        }
+        if (whole < a.blocks) {
+            fetch(whole);
+            put(whole);  // where block whole - 2 was, which all waves have left behind
+            __syncthreads();
+            compute(whole);
+        }
+    } else {
+        fetch(0);
+        for (int b = 0; b < a.blocks; ++b) {
+            put(b);
+            __syncthreads();
+            if (b + 1 < a.blocks) fetch(b + 1);
+            compute(b);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+        const int row = m0 + wm * (BM / WM) + i * 16 + r;
+        if (row < a.m)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) {
+                const int col = n0 + wn * (BN / WN) + j * 16 + part * 4;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (col + e < a.n) store(a.y, a.y_type, row * a.y_stride + col + e, sum[i][j][e]);
+            }
+    }
+}
+
+template <int BM, int BN, int WM, int WN, bool DIRECT>
+hipError_t launch_tiles(const MatmulArgs &a, hipStream_t stream)
+{
+    constexpr auto kernel = &fp8_matmul_tile_kernel<BM, BN, WM, WN, DIRECT>;
+    const hipError_t e = allow_full_lds<kernel>();
+    if (e != hipSuccess) return e;
+    const int tiles_m = (a.m + BM - 1) / BM, tiles_n = (a.n + BN - 1) / BN;
+    kernel<<<tiles_m * tiles_n, 64 * WM * WN, 2 * ((BM + BN) * kBlock + BM * 4), stream>>>(a, tiles_m, tiles_n);
+    return hipGetLastError();
+}
+
+hipError_t launch_part(const MatmulArgs &a, hipStream_t stream)
+{
+    if (a.m <= 64) {
+        const int grid = (a.n + 15) / 16;
+        if (a.m <= 16)
+            fp8_matmul_rows_kernel<1><<<grid, 512, 0, stream>>>(a);
+        else if (a.m <= 32)
+            fp8_matmul_rows_kernel<2><<<grid, 512, 0, stream>>>(a);
+        else
+            fp8_matmul_rows_kernel<4><<<grid, 512, 0, stream>>>(a);
+        return hipGetLastError();
+    }
+    auto direct = [](const uint8_t *p, int64_t stride) { return (reinterpret_cast<uintptr_t>(p) | (uint64_t)stride) % 16 == 0 && stride < 1 << 24; };
+    return direct(a.x, a.x_stride) && direct(a.w, a.w_stride) ? launch_tiles<128, 128, 2, 2, true>(a, stream)
+                                                              : launch_tiles<128, 128, 2, 2, false>(a, stream);
 }
 
 }  // namespace
@@ -109,15 +353,16 @@ size_t fp8_matmul_workspace_bytes(int32_t, int32_t, int32_t) { return 0; }
 
 hipError_t launch_fp8_matmul(const MatmulArgs &a, void *, hipStream_t stream)
 {
-    constexpr int kRows = kMaxGridY * 16;  // of a launch
-    for (int64_t first = 0; first < a.m; first += kRows) {
+    // launches of fewer than 2^22 tiles of 128 x 128 (n has at most 2^19, m any number): threads and tiles fit 32 bits
+    const int64_t tiles_n = ((int64_t)a.n + 127) / 128;
+    const int64_t rows = std::max<int64_t>(1, ((int64_t)1 << 22) / tiles_n) * 128;
+    for (int64_t first = 0; first < a.m; first += rows) {
         MatmulArgs p = a;
-        p.m = (int32_t)std::min<int64_t>(kRows, a.m - first);
+        p.m = (int32_t)std::min<int64_t>(rows, a.m - first);
         p.x = a.x + first * a.x_stride;
         p.x_scales = a.x_scales + first * a.blocks;
         p.y = static_cast<char *>(a.y) + first * a.y_stride * (a.y_type == QUAMBA_F32 ? 4 : 2);
-        fp8_matmul_any_kernel<<<dim3((a.n + 15) / 16, (p.m + 15) / 16), 64, 0, stream>>>(p);
-        const hipError_t e = hipGetLastError();
+        const hipError_t e = launch_part(p, stream);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;

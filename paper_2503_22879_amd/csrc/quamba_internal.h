@@ -386,7 +386,8 @@ hipError_t launch_prefill_wide(const SsdArgs &a, bool halves, bool precise, hipS
 bool prefill_generic_supports(const quamba_ssd_shape_t &s);
 
 // ---- 8-bit floating point (e4m3 with a scale for each block of 128) ----
-constexpr int64_t kFp8MaxDepth = (int64_t)1 << 30;  // columns of a matrix
+constexpr int64_t kFp8MaxDepth = (int64_t)1 << 30;    // columns of an operand
+constexpr int64_t kFp8MaxColumns = (int64_t)1 << 26;  // of a product
 struct QuantizeArgs {
     const void *x;
     int64_t rows, cols, x_stride, q_stride;  // strides in values
