@@ -43,43 +43,42 @@ struct Chooser {
 };
 
 // The `count` largest of the workgroup's keys, key(e) for e < E in every thread, 0 for none and otherwise all different: out[0 ..
-// count - 1], largest first, 0 where there are no more.  `out` is written by some threads; the caller waits before it is read
-// elsewhere.
+// count - 1], largest first, 0 where there are no more.  `top` is the upper half of the thread's largest key, and from(bound) gives
+// the test, for e, whether key(e)'s upper half is at least `bound`.  `out` is written by some threads; the caller waits before
+// it is read elsewhere.
 //
 // `count` threads have a key at least as large as the count-th largest of the threads' own largest ones, so nothing below that
-// is among the best: what is left is mostly little more than `count` keys, which are ranked by counting.  The bound is
-// sought bit by bit in the upper half of the keys, by every wave for itself.
-template <int E, int BITS, typename Key, typename Out>
-__device__ __forceinline__ void choose(Chooser &c, int count, const Key &key, const Out &out)
+// is among the best: what is left is mostly little more than `count` keys, which are ranked by counting.  The bound is sought bit
+// by bit, by every wave for itself, in the upper 16 of a key's bits (for floats the sign, the exponent and 7 bits more: the
+// last bits would spare few keys).
+template <int E, typename From, typename Key, typename Out>
+__device__ __forceinline__ void choose(Chooser &c, int count, uint32_t top, const From &from, const Key &key, const Out &out)
 {
     const int t = threadIdx.x, lane = t & 63;
-    uint64_t top = 0;
-#pragma unroll
-    for (int e = 0; e < E; ++e) top = max(top, key(e));
-    const uint32_t top_hi = (uint32_t)(top >> 32);
-    c.tops[t] = top_hi;
+    c.tops[t] = top;
     if (t == 0) c.n = 0;
     __syncthreads();
     uint32_t mine[kWaves], bound = 0;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) mine[w] = c.tops[w * 64 + lane];
-    for (int bit = 31; bit >= 32 - BITS; --bit) {
+#pragma unroll
+    for (int bit = 31; bit >= 16; --bit) {
         const uint32_t higher = bound | 1u << bit;
         int n = 0;
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) n += __builtin_popcountll(__builtin_amdgcn_ballot_w64(mine[w] >= higher));
-        if (n >= count) bound = higher;
+        bound = n >= count ? higher : bound;
     }
     bound = max(bound, 1u);
-    if (top_hi >= bound)
+    if (top >= bound) {
+        const auto candidate = from(bound);
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const uint64_t k = key(e);
-            if ((uint32_t)(k >> 32) >= bound) {
+        for (int e = 0; e < E; ++e)
+            if (candidate(e)) {
                 const int at = atomicAdd(&c.n, 1);
-                if (at < kGathered) c.gathered[at] = k;
+                if (at < kGathered) c.gathered[at] = key(e);
             }
-        }
+    }
     __syncthreads();
     const int n = c.n;
     if (n <= kGathered) {
@@ -153,46 +152,49 @@ __global__ __launch_bounds__(kThreads) void beam_pieces_kernel(SelectArgs a, int
     float x[E];
     const int first = part * (kThreads * E);
     auto token = [&](int e) { return first + (e / kVec * kThreads + t) * kVec + e % kVec; };
+    if (first + kThreads * E <= a.vocab) {
+        char raw[E / kVec][16];
 #pragma unroll
-    for (int v = 0; v < E / kVec; ++v) {
-        const int at = token(v * kVec);
-        if (at + kVec <= a.vocab) {
-            char raw[16];
-            __builtin_memcpy(raw, p + (int64_t)at * kBytes, 16);
+        for (int v = 0; v < E / kVec; ++v) __builtin_memcpy(raw[v], p + (int64_t)token(v * kVec) * kBytes, 16);
 #pragma unroll
-            for (int i = 0; i < kVec; ++i) x[v * kVec + i] = logit_of<TYPE>(raw + i * kBytes);
-        } else {
+        for (int e = 0; e < E; ++e) x[e] = logit_of<TYPE>(raw[e / kVec] + e % kVec * kBytes);
+    } else {
 #pragma unroll
-            for (int i = 0; i < kVec; ++i)
-                x[v * kVec + i] = at + i < a.vocab ? logit_of<TYPE>(p + (int64_t)(at + i) * kBytes) : -__builtin_inff();
+        for (int v = 0; v < E / kVec; ++v) {
+            const int at = token(v * kVec);
+            if (at + kVec <= a.vocab) {
+                char raw[16];
+                __builtin_memcpy(raw, p + (int64_t)at * kBytes, 16);
+#pragma unroll
+                for (int i = 0; i < kVec; ++i) x[v * kVec + i] = logit_of<TYPE>(raw + i * kBytes);
+            } else {
+#pragma unroll
+                for (int i = 0; i < kVec; ++i)
+                    x[v * kVec + i] = at + i < a.vocab ? logit_of<TYPE>(p + (int64_t)(at + i) * kBytes) : -__builtin_inff();
+            }
         }
     }
-    float top = -__builtin_inff();
-    bool bad = false;
+    float mine = -__builtin_inff();  // past a NaN, which the sum shows
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-        top = fmaxf(top, x[e]);
-        bad |= !(x[e] < __builtin_inff());
-    }
-    top = bad ? __builtin_inff() : top;
-    top = wave_max(top);
+    for (int e = 0; e < E; ++e) mine = fmaxf(mine, x[e]);
+    float top = wave_max(mine);
     if (t % 64 == 0) wave_f[0][t / 64] = top;
     __syncthreads();
     top = fmaxf(fmaxf(wave_f[0][0], wave_f[0][1]), fmaxf(wave_f[0][2], wave_f[0][3]));
+    const float against = top > -__builtin_inff() ? top : 0.0f;
     float sum = 0.0f;
-    if (top > -__builtin_inff()) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) sum += __expf(x[e] - top);
-    }
+    for (int e = 0; e < E; ++e) sum += __expf(x[e] - against);
     sum = group_sum<64>(sum);
     if (t % 64 == 0) wave_f[1][t / 64] = sum;
     uint64_t *to = best + (int64_t)blockIdx.x * a.count;
-    choose<E, TYPE == QUAMBA_F32 ? 32 : 20>(
-        chooser, a.count,
-        [&](int e) {
-            const uint32_t o = x[e] > -__builtin_inff() ? ordered(x[e] + 0.0f) : 0u;  // -0 is 0
-            return o ? (uint64_t)o << 32 | (uint32_t)~token(e) : (uint64_t)0;
+    choose<E>(
+        chooser, a.count, mine > -__builtin_inff() ? ordered(mine + 0.0f) : 0u,  // -0 is 0
+        [&](uint32_t bound) {
+            const float least = max(of_ordered(bound), -__FLT_MAX__);
+            return [&x, least](int e) { return x[e] >= least; };
         },
+        [&](int e) { return x[e] > -__builtin_inff() ? (uint64_t)ordered(x[e] + 0.0f) << 32 | (uint32_t)~token(e) : (uint64_t)0; },
         [&](int i, uint64_t k) { to[i] = k; });
     if (t == 0) {
         const float all = (wave_f[1][0] + wave_f[1][1]) + (wave_f[1][2] + wave_f[1][3]);
@@ -200,73 +202,87 @@ __global__ __launch_bounds__(kThreads) void beam_pieces_kernel(SelectArgs a, int
     }
 }
 
-// A workgroup to a sequence.
-__global__ __launch_bounds__(kThreads) void beam_join_kernel(SelectArgs a, int pieces, const uint64_t *best, const Piece *piece)
+template <int CTRL>
+__device__ __forceinline__ float row_step_max(float v) { return fmaxf(v, dpp_move<CTRL>(v)); }
+__device__ __forceinline__ float row_max(float v)  // of 16 lanes
+{
+    return row_step_max<0x140>(row_step_max<0x141>(row_step_max<0x4E>(row_step_max<0xB1>(v))));
+}
+
+// A workgroup to a sequence: 16 lanes join a beam's pieces, then all take the best of the pieces' best.
+__global__ __launch_bounds__(kThreads) void beam_join_kernel(SelectArgs a, int pieces, Divisor by_beam, const uint64_t *best,
+                                                             const Piece *piece)
 {
     constexpr int E = 8;
     __shared__ Chooser chooser;
-    __shared__ float score[kMaxBeams], row_max[kMaxBeams], row_log[kMaxBeams];
+    __shared__ float score[kMaxBeams], row_top[kMaxBeams], row_log[kMaxBeams];
     __shared__ uint8_t kind[kMaxBeams];  // 0: offers nothing, 1: its pieces' tokens, 2: finished
     __shared__ uint64_t list[kMaxChoices];
-    const int t = threadIdx.x, lane = t & 63, b = blockIdx.x;
-    for (int k = t / 64; k < a.beams; k += kWaves) {
+    const int t = threadIdx.x, b = blockIdx.x;
+    const int per_beam = pieces * a.count, all = a.beams * per_beam;
+    const uint64_t *candidates = best + (int64_t)b * all;
+    uint64_t c[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) c[e] = candidates[min(e * kThreads + t, all - 1)];
+    for (int k = t / 16; k < a.beams; k += kThreads / 16) {
         const int row = b * a.beams + k;
+        const Piece *p = piece + (int64_t)row * pieces;
         const bool valid = offers(a, row), done = a.finished && a.finished[row];
         float m = -__builtin_inff(), s = 0.0f;
-        if (valid && !done) {
-            const Piece *p = piece + (int64_t)row * pieces;
-            for (int i = lane; i < pieces; i += 64) m = fmaxf(m, p[i].max);
-            m = wave_max(m);
-            if (m > -__builtin_inff())
-                for (int i = lane; i < pieces; i += 64) s += p[i].sum * __expf(p[i].max - m);
-            s = group_sum<64>(s);
-        }
-        if (lane == 0) {
+        for (int i = t % 16; i < pieces; i += 16) m = fmaxf(m, p[i].max);
+        m = row_max(m);
+        const float against = m > -__builtin_inff() ? m : 0.0f;
+        for (int i = t % 16; i < pieces; i += 16) s += p[i].sum * __expf(p[i].max - against);
+        s = group_sum<16>(s);
+        if (t % 16 == 0) {
             score[k] = a.scores[row];
-            row_max[k] = m;
+            row_top[k] = m;
             row_log[k] = logf(s);
             kind[k] = !valid ? 0 : done ? 2 : s > 0.0f && m < __builtin_inff() ? 1 : 0;
         }
     }
     for (int i = t; i < kMaxChoices; i += kThreads) list[i] = 0;
     __syncthreads();
-    const int per_beam = pieces * a.count;
-    const int64_t all = (int64_t)a.beams * per_beam;
-    for (int64_t first = 0; first < all; first += kThreads * E) {
+    for (int first = 0; first < all; first += kThreads * E) {
         uint64_t key[E + 1];
+        uint32_t top = 0;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             key[e] = 0;
-            const int64_t i = first + e * kThreads + t;
+            const int i = first + e * kThreads + t;
             if (i < all) {
-                const int k = (int)(i / per_beam), j = (int)(i - (int64_t)k * per_beam);
-                uint32_t token = 0;
+                const int k = quotient(i, by_beam);
+                uint32_t token = ~(uint32_t)c[e];
                 float v = -__builtin_inff();
                 if (kind[k] == 1) {
-                    const uint64_t c = best[(int64_t)(b * a.beams + k) * per_beam + j];
-                    token = ~(uint32_t)c;
-                    if (c) v = score[k] + ((of_ordered((uint32_t)(c >> 32)) - row_max[k]) - row_log[k]);
-                } else if (kind[k] == 2 && j == 0) {
+                    if (c[e]) v = score[k] + ((of_ordered((uint32_t)(c[e] >> 32)) - row_top[k]) - row_log[k]);
+                } else if (kind[k] == 2 && i == k * per_beam) {
                     token = (uint32_t)a.pad;
                     v = score[k];
                 }
                 if (v > -__builtin_inff())
                     key[e] = (uint64_t)ordered(v + 0.0f) << 32 | ~((uint32_t)k * (uint32_t)a.vocab + token);
+                const int64_t next = (int64_t)i + kThreads * E;
+                if (next < all) c[e] = candidates[next];
             }
+            top = max(top, (uint32_t)(key[e] >> 32));
         }
         key[E] = t < kMaxChoices ? list[t] : 0;
+        top = max(top, (uint32_t)(key[E] >> 32));
         __syncthreads();
-        choose<E + 1, 32>(chooser, a.count, [&](int e) { return key[e]; }, [&](int i, uint64_t k) { list[i] = k; });
+        choose<E + 1>(
+            chooser, a.count, top, [&](uint32_t bound) { return [&key, bound](int e) { return (uint32_t)(key[e] >> 32) >= bound; }; },
+            [&](int e) { return key[e]; }, [&](int i, uint64_t k) { list[i] = k; });
         __syncthreads();
     }
     for (int i = t; i < a.count; i += kThreads) {
-        const uint64_t c = list[i];
-        const uint32_t at = ~(uint32_t)c;
+        const uint64_t chosen = list[i];
+        const uint32_t at = ~(uint32_t)chosen;
         const uint32_t k = at / (uint32_t)a.vocab;
         const int64_t o = (int64_t)b * a.count + i;
-        a.out_scores[o] = c ? of_ordered((uint32_t)(c >> 32)) : -__builtin_inff();
-        a.out_parents[o] = c ? (int32_t)k : i % a.beams;
-        a.out_tokens[o] = c ? (int32_t)(at - k * (uint32_t)a.vocab) : a.pad;
+        a.out_scores[o] = chosen ? of_ordered((uint32_t)(chosen >> 32)) : -__builtin_inff();
+        a.out_parents[o] = chosen ? (int32_t)k : i % a.beams;
+        a.out_tokens[o] = chosen ? (int32_t)(at - k * (uint32_t)a.vocab) : a.pad;
     }
 }
 
@@ -295,7 +311,7 @@ void launch_pieces(const SelectArgs &a, int e, int pieces, uint64_t *best, Piece
 
 // ---- the caches ----
 
-constexpr int kCaches = 32;  // of a launch
+constexpr int kCaches = 64;  // of a launch, a lane's each
 struct ReorderArgs {
     const int32_t *parents;
     int32_t batch, beams, n;
@@ -303,62 +319,67 @@ struct ReorderArgs {
     quamba_beam_cache_t cache[kCaches];
 };
 
-// A workgroup moves one slice of 4 KiB of every beam of a sequence: all loads stand before the stores, and no other thread
-// touches the bytes, so the move is in place whatever the order of the beams.
+// Bytes that a thread moves of every beam: 16, fewer for many beams, so that they fit 64 registers.
+constexpr int move_bytes(int beams) { return beams <= 16 ? 16 : 256 / beams; }
+
+// The parents of a sequence's beams, a byte each in scalar registers.
+template <int BEAMS>
+struct Parents {
+    uint32_t four[(BEAMS + 3) / 4];
+    __device__ __forceinline__ int operator[](int k) const { return (int)(four[k / 4] >> k % 4 * 8 & 0xffu); }
+};
+
+// Beams K and above: every load stands before every store.
+template <int K, int BEAMS, typename Vec>
+__device__ __forceinline__ void move_beams(char *base, int64_t bytes, const Parents<BEAMS> &parents, uint64_t &moved)
+{
+    Vec v;
+    if (moved >> K & 1) v = *reinterpret_cast<const Vec *>(base + parents[K] * bytes);
+    if constexpr (K + 1 < BEAMS)
+        move_beams<K + 1, BEAMS, Vec>(base, bytes, parents, moved);
+    else  // the same conditions again, but not to the compiler, which would make a path of its own for each set of beams
+        asm volatile("" : "+s"(moved));
+    if (moved >> K & 1) *reinterpret_cast<Vec *>(base + K * bytes) = v;
+}
+
+// A workgroup moves one slice of every beam of a sequence: all loads stand before the stores, and no other thread touches the
+// bytes, so the move is in place whatever the order of the beams.  BEAMS: at least as many as there are.
 template <int BEAMS>
 __global__ __launch_bounds__(kThreads) void beam_reorder_kernel(ReorderArgs a)
 {
-    typedef uint32_t Vec __attribute__((ext_vector_type(4), aligned(1)));  // caches may lie at any address
+    constexpr int kBytes = move_bytes(BEAMS);
+    typedef uint32_t Vec __attribute__((ext_vector_type(kBytes / 4), aligned(1)));  // caches may lie at any address
     const int b = blockIdx.y;
-    int c = 0;
-    for (int i = 1; i < a.n; ++i) c += (int)blockIdx.x >= a.first[i];
-    const int64_t bytes = a.cache[c].bytes, at = ((int64_t)((int)blockIdx.x - a.first[c]) * kThreads + threadIdx.x) * 16;
-    if (at >= bytes) return;
-    char *base = static_cast<char *>(a.cache[c].data) + (int64_t)b * a.beams * bytes + at;
-    const int32_t *parents = a.parents + (int64_t)b * a.beams;
-    int from[BEAMS];
+    // lane k knows beam k's parent
+    const int lane = threadIdx.x & 63, parent = a.parents[(int64_t)b * a.beams + min(lane, a.beams - 1)];
+    const bool moves = lane < a.beams && (uint32_t)parent < (uint32_t)a.beams && parent != lane;
+    uint64_t moved = __builtin_amdgcn_ballot_w64(moves);
+    // read here, where every lane is active: a lane's registers are not its own any more behind a branch that it does not take
+    Parents<BEAMS> parents;
 #pragma unroll
     for (int k = 0; k < BEAMS; ++k) {
-        const int p = k < a.beams ? parents[k] : k;
-        from[k] = (uint32_t)p < (uint32_t)a.beams ? p : k;
+        const uint32_t p = (uint32_t)__builtin_amdgcn_readlane(parent, k) & 0xffu;
+        parents.four[k / 4] = k % 4 ? parents.four[k / 4] | p << k % 4 * 8 : p;
     }
-    if (at + 16 <= bytes) {
-        Vec v[BEAMS];
-#pragma unroll
-        for (int k = 0; k < BEAMS; ++k)
-            if (from[k] != k) v[k] = *reinterpret_cast<const Vec *>(base + from[k] * bytes);
-#pragma unroll
-        for (int k = 0; k < BEAMS; ++k)
-            if (from[k] != k) *reinterpret_cast<Vec *>(base + k * bytes) = v[k];
-    } else {  // the last bytes one by one, of all beams alike
+    const int c = __builtin_popcountll(__builtin_amdgcn_ballot_w64(lane < a.n && (int)blockIdx.x >= a.first[lane])) - 1;
+    const int64_t bytes = a.cache[c].bytes, at = ((int64_t)((int)blockIdx.x - a.first[c]) * kThreads + threadIdx.x) * kBytes;
+    if (at >= bytes) return;
+    char *base = static_cast<char *>(a.cache[c].data) + (int64_t)b * a.beams * bytes + at;
+    if (at + kBytes <= bytes) {
+        move_beams<0, BEAMS, Vec>(base, bytes, parents, moved);
+    } else {
 #pragma unroll 1
-        for (int i = 0; at + i < bytes; ++i) {
-            char v[BEAMS];
-#pragma unroll
-            for (int k = 0; k < BEAMS; ++k)
-                if (k < a.beams) v[k] = base[from[k] * bytes + i];
-#pragma unroll
-            for (int k = 0; k < BEAMS; ++k)
-                if (k < a.beams) base[k * bytes + i] = v[k];
+        for (int i = 0; at + i < bytes; ++i) {  // the last bytes one by one
+            uint64_t m = moved;
+            move_beams<0, BEAMS, uint8_t>(base + i, bytes, parents, m);
         }
     }
 }
 
-void launch_slices(const ReorderArgs &a, int slices, int sequences, hipStream_t stream)
+template <int BEAMS>
+void launch_slices(const ReorderArgs &a, int slices, hipStream_t stream)
 {
-    const dim3 grid(slices, sequences);
-    if (a.beams <= 2)
-        beam_reorder_kernel<2><<<grid, kThreads, 0, stream>>>(a);
-    else if (a.beams <= 4)
-        beam_reorder_kernel<4><<<grid, kThreads, 0, stream>>>(a);
-    else if (a.beams <= 8)
-        beam_reorder_kernel<8><<<grid, kThreads, 0, stream>>>(a);
-    else if (a.beams <= 16)
-        beam_reorder_kernel<16><<<grid, kThreads, 0, stream>>>(a);
-    else if (a.beams <= 32)
-        beam_reorder_kernel<32><<<grid, kThreads, 0, stream>>>(a);
-    else
-        beam_reorder_kernel<64><<<grid, kThreads, 0, stream>>>(a);
+    beam_reorder_kernel<BEAMS><<<dim3(slices, a.batch), kThreads, 0, stream>>>(a);
 }
 
 }  // namespace
@@ -388,16 +409,19 @@ hipError_t launch_beam_select(const SelectArgs &a, void *workspace, hipStream_t 
     }
     hipError_t err = hipGetLastError();
     if (err != hipSuccess) return err;
-    beam_join_kernel<<<a.batch, kThreads, 0, stream>>>(a, pieces, best, piece);
+    beam_join_kernel<<<a.batch, kThreads, 0, stream>>>(a, pieces, divisor((uint32_t)(pieces * a.count)), best, piece);
     return hipGetLastError();
 }
 
 hipError_t launch_beam_reorder(int32_t batch, int32_t beams, const int32_t *parents, int32_t n, const quamba_beam_cache_t *caches,
                                hipStream_t stream)
 {
-    // launches of up to kCaches caches, 2^22 slices (16 GiB of a beam, the longest cache) and 65535 sequences
-    constexpr int64_t kSlice = kThreads * 16, kSlices = kMaxCacheBytes / kSlice;
+    // launches of up to kCaches caches, as many slices as the longest cache has (2^24 at most), and 65535 sequences
     if (beams == 1) return hipSuccess;
+    const auto launch = beams <= 2 ? launch_slices<2> : beams <= 4 ? launch_slices<4> : beams <= 8 ? launch_slices<8>
+                      : beams <= 16 ? launch_slices<16> : beams <= 32 ? launch_slices<32> : launch_slices<64>;
+    const int64_t slice = kThreads * (beams <= 16 ? move_bytes(16) : beams <= 32 ? move_bytes(32) : move_bytes(64));
+    const int64_t most = kMaxCacheBytes / slice;
     for (int32_t s0 = 0; s0 < batch; s0 += kMaxGridY) {
         const int sequences = std::min(batch - s0, kMaxGridY);
         ReorderArgs a;
@@ -407,15 +431,15 @@ hipError_t launch_beam_reorder(int32_t batch, int32_t beams, const int32_t *pare
         a.n = 0;
         int64_t slices = 0;
         auto flush = [&] {
-            if (a.n) launch_slices(a, (int)slices, sequences, stream);
+            if (a.n) launch(a, (int)slices, stream);
             a.n = 0;
             slices = 0;
             return hipGetLastError();
         };
         for (int32_t i = 0; i < n; ++i) {
-            const int64_t need = (caches[i].bytes + kSlice - 1) / kSlice;
+            const int64_t need = (caches[i].bytes + slice - 1) / slice;
             if (!need) continue;
-            if (a.n == kCaches || slices + need > kSlices) {
+            if (a.n == kCaches || slices + need > most) {
                 const hipError_t e = flush();
                 if (e != hipSuccess) return e;
             }
