@@ -7,6 +7,7 @@
 // depth 13 bits below the largest of them: sums of 128 normal values are off by 1.6e-5 of themselves, and by 5e-5 where the
 // values' sizes spread, against 1e-8 here.
 #include <algorithm>
+#include <type_traits>
 
 #include "quamba_internal.h"
 
@@ -76,6 +77,36 @@ __device__ __forceinline__ void store(void *y, int type, int64_t at, float v)
         static_cast<uint16_t *>(y)[at] = f32_to_f16_bits(v);
     else
         static_cast<__bf16 *>(y)[at] = (__bf16)v;
+}
+
+// N adjacent values of a row at `at`, of which the first `left` belong to it.
+template <int TYPE, int N>
+__device__ __forceinline__ void store_row(void *y, int64_t at, const float (&v)[N], int left)
+{
+    if (TYPE == QUAMBA_F32) {
+        float *p = static_cast<float *>(y) + at;
+        if (left >= N) {
+#pragma unroll
+            for (int i = 0; i < N; i += 4) __builtin_memcpy(p + i, &v[i], 16);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (i < left) p[i] = v[i];
+        }
+    } else {
+        uint16_t *p = static_cast<uint16_t *>(y) + at;
+        uint16_t h[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) h[i] = TYPE == QUAMBA_F16 ? f32_to_f16_bits(v[i]) : __builtin_bit_cast(uint16_t, (__bf16)v[i]);
+        if (left >= N) {
+#pragma unroll
+            for (int i = 0; i < N; i += 8) __builtin_memcpy(p + i, &h[i], N < 8 ? 2 * N : 16);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (i < left) p[i] = h[i];
+        }
+    }
 }
 
 // ---- up to 64 rows of x: the weight streams past ----
@@ -195,8 +226,10 @@ __device__ __forceinline__ void tile_of(int id, int tiles_m, int tiles_n, int &t
 }
 
 // BM x BN outputs to a workgroup of WM x WN waves.  LDS holds two blocks (128 codes deep) of BM + BN rows and the scales of x's rows; the next
-// block arrives while one is multiplied.  The 16-byte pieces of a row are stored in an order that depends on the row (piece c
-// of row r at c ^ (r % 8)), so that the 8 lanes that read together hit different banks.  DIRECT: rows at multiples of 16
+// block arrives while one is multiplied.  A lane takes pieces l / 16 and l / 16 + 4 of the 8 of 16 bytes that a row has (any order along the
+// depth will do that is the same for x and w), and piece c of row r lies at c ^ (r / 2 % 8), so that the lanes that read together
+// hit different banks.  Which row of w stands where in a 16-row part is free as well: row 4 p + e of part j is the wave's row
+// 4 TN p + 4 j + e, so that a lane ends up with 4 TN adjacent columns of y.  DIRECT: rows at multiples of 16
 // bytes less than 2^24 bytes apart go from memory to LDS by themselves; else through registers.
 template <int BM, int BN, int WM, int WN, bool DIRECT>
 __global__ __launch_bounds__(64 * WM * WN, 2) void fp8_matmul_tile_kernel(MatmulArgs a, int tiles_m, int tiles_n)
@@ -217,33 +250,37 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void fp8_matmul_tile_kernel(Matmul
 
     // 8 rows of a tile in turn: this lane's piece of them
     constexpr int kTurns = kRows / 8 / kWaves;
-    const int piece = (lane & 7) ^ (lane >> 3);
     auto row_of = [&](int turn) { return (turn * kWaves + wave) * 8 + (lane >> 3); };
     auto is_x = [&](int turn) { return (turn * kWaves + wave) * 8 < BM; };
+    auto order = [&](int turn) {  // among the 16 rows that are read together
+        const int row = row_of(turn);
+        return is_x(turn) ? row >> 1 & 7 : (row >> 1 & 1) | (row / (4 * TN) & 3) << 1;
+    };
+    auto piece_of = [&](int turn) { return (lane & 7) ^ order(turn); };
     uint32_t offset[DIRECT ? kTurns : 1], scale_offset = 0;
     if (DIRECT) {
 #pragma unroll
         for (int t = 0; t < kTurns; ++t)
-            offset[t] = is_x(t) ? (uint32_t)min(row_of(t), last_x) * (uint32_t)a.x_stride + piece * 16
-                                : (uint32_t)min(row_of(t) - BM, last_w) * (uint32_t)a.w_stride + piece * 16;
+            offset[t] = is_x(t) ? (uint32_t)min(row_of(t), last_x) * (uint32_t)a.x_stride + piece_of(t) * 16
+                                : (uint32_t)min(row_of(t) - BM, last_w) * (uint32_t)a.w_stride + piece_of(t) * 16;
         scale_offset = (uint32_t)min(wave * 64 + lane, last_x) * (uint32_t)a.blocks * 4;
     }
     const uint32_t base = lds_address(lds);
-    auto start = [&](int b) {  // DIRECT: a whole block on its way
+    auto start = [&](int b, int half) {  // DIRECT: a half of a whole block (2: all of it) on its way
         const uint32_t to = base + (b & 1) * kStage;
         const uint8_t *x = xb + (int64_t)b * kBlock, *w = wb + (int64_t)b * kBlock;
 #pragma unroll
-        for (int t = 0; t < kTurns; ++t) load_to_lds16(is_x(t) ? x : w, offset[t], to + (t * kWaves + wave) * 1024);
-        if (wave < BM / 64) load_to_lds4(xsb + b, scale_offset, to + kScales + wave * 256);
+        for (int t = 0; t < kTurns; ++t)
+            if (half == 2 || half == t / (kTurns / 2)) load_to_lds16(is_x(t) ? x : w, offset[t], to + (t * kWaves + wave) * 1024);
+        if (half != 1 && wave < BM / 64) load_to_lds4(xsb + b, scale_offset, to + kScales + wave * 256);
     };
     int4v held[kTurns];
     float held_scale = 0.0f;
     auto fetch = [&](int b) {  // any block, to registers
-        const int left = a.k - b * kBlock - piece * 16;
 #pragma unroll
         for (int t = 0; t < kTurns; ++t) {
             const uint8_t *p = is_x(t) ? xb + (int64_t)min(row_of(t), last_x) * a.x_stride : wb + (int64_t)min(row_of(t) - BM, last_w) * a.w_stride;
-            held[t] = load16(p + (int64_t)b * kBlock + piece * 16, left);
+            held[t] = load16(p + (int64_t)b * kBlock + piece_of(t) * 16, a.k - b * kBlock - piece_of(t) * 16);
         }
         if ((int)threadIdx.x < BM) held_scale = xsb[(int64_t)min((int)threadIdx.x, last_x) * a.blocks + b];
     };
@@ -259,18 +296,21 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void fp8_matmul_tile_kernel(Matmul
     for (int i = 0; i < TM; ++i)
 #pragma unroll
         for (int j = 0; j < TN; ++j) sum[i][j] = float4v{0, 0, 0, 0};
-    const int at = r * kBlock + ((2 * part) ^ (r & 7)) * 16;
-    auto compute = [&](int b) {
+    const int at = r * kBlock + (part ^ r >> 1) * 16, at_w = ((r >> 2) * 4 * TN + (r & 3)) * kBlock + (part ^ r >> 1) * 16;
+    // Multiplies block b; between its first parts block `next` (below 0: none) is started, in two halves: a wave waits where it
+    // issues more loads than fit a queue, and after the first part's reads it has products to make meanwhile (16384 x 18560 x 4096: 2.15 -> 2.11 ms).
+    auto compute = [&](int b, int next) {
         const char *x = lds + (b & 1) * kStage + wm * (BM / WM) * kBlock, *w = lds + (b & 1) * kStage + (BM + wn * (BN / WN)) * kBlock;
         const float *xs = reinterpret_cast<const float *>(lds + (b & 1) * kStage + kScales) + wm * (BM / WM) + r;
         const float wsc = ws[b];
         Part wf[TN];
 #pragma unroll
         for (int j = 0; j < TN; ++j)
-            wf[j] = Part(*reinterpret_cast<const int4v *>(w + j * 16 * kBlock + at), *reinterpret_cast<const int4v *>(w + j * 16 * kBlock + (at ^ 16)));
+            wf[j] = Part(*reinterpret_cast<const int4v *>(w + j * 4 * kBlock + at_w), *reinterpret_cast<const int4v *>(w + j * 4 * kBlock + (at_w ^ 64)));
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
-            const Part xf(*reinterpret_cast<const int4v *>(x + i * 16 * kBlock + at), *reinterpret_cast<const int4v *>(x + i * 16 * kBlock + (at ^ 16)));
+            const Part xf(*reinterpret_cast<const int4v *>(x + i * 16 * kBlock + at), *reinterpret_cast<const int4v *>(x + i * 16 * kBlock + (at ^ 64)));
+            if (DIRECT && i < 2 && next >= 0) start(next, i);
             const float s = xs[i * 16] * wsc;
             float4v p[TN];
 #pragma unroll
@@ -284,17 +324,16 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void fp8_matmul_tile_kernel(Matmul
 
     if (DIRECT) {
         const int whole = a.k / kBlock;
-        if (whole) start(0);
+        if (whole) start(0, 2);
         for (int b = 0; b < whole; ++b) {
             wait_for_tiles();  // block b is there for all waves, and block b - 1 has been read by all
-            if (b + 1 < whole) start(b + 1);
-            compute(b);
+            compute(b, b + 1 < whole ? b + 1 : -1);
         }
         if (whole < a.blocks) {
             fetch(whole);
             put(whole);  // where block whole - 2 was, which all waves have left behind
             __syncthreads();
-            compute(whole);
+            compute(whole, -1);
         }
     } else {
         fetch(0);
@@ -302,21 +341,26 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void fp8_matmul_tile_kernel(Matmul
             put(b);
             __syncthreads();
             if (b + 1 < a.blocks) fetch(b + 1);
-            compute(b);
+            compute(b, -1);
         }
     }
+    auto write = [&](auto type) {
+        const int col = n0 + wn * (BN / WN) + part * 4 * TN;
 #pragma unroll
-    for (int i = 0; i < TM; ++i) {
-        const int row = m0 + wm * (BM / WM) + i * 16 + r;
-        if (row < a.m)
+        for (int i = 0; i < TM; ++i) {
+            const int row = m0 + wm * (BM / WM) + i * 16 + r;
+            float v[4 * TN];
 #pragma unroll
-            for (int j = 0; j < TN; ++j) {
-                const int col = n0 + wn * (BN / WN) + j * 16 + part * 4;
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (col + e < a.n) store(a.y, a.y_type, row * a.y_stride + col + e, sum[i][j][e]);
-            }
-    }
+            for (int j = 0; j < 4 * TN; ++j) v[j] = sum[i][j / 4][j % 4];
+            if (row < a.m) store_row<decltype(type)::value>(a.y, row * a.y_stride + col, v, a.n - col);
+        }
+    };
+    if (a.y_type == QUAMBA_F32)
+        write(std::integral_constant<int, QUAMBA_F32>());
+    else if (a.y_type == QUAMBA_F16)
+        write(std::integral_constant<int, QUAMBA_F16>());
+    else
+        write(std::integral_constant<int, QUAMBA_BF16>());
 }
 
 template <int BM, int BN, int WM, int WN, bool DIRECT>
@@ -343,8 +387,10 @@ hipError_t launch_part(const MatmulArgs &a, hipStream_t stream)
         return hipGetLastError();
     }
     auto direct = [](const uint8_t *p, int64_t stride) { return (reinterpret_cast<uintptr_t>(p) | (uint64_t)stride) % 16 == 0 && stride < 1 << 24; };
-    return direct(a.x, a.x_stride) && direct(a.w, a.w_stride) ? launch_tiles<128, 128, 2, 2, true>(a, stream)
-                                                              : launch_tiles<128, 128, 2, 2, false>(a, stream);
+    if (!direct(a.x, a.x_stride) || !direct(a.w, a.w_stride)) return launch_tiles<128, 128, 2, 2, false>(a, stream);
+    if (a.m > 128 && (int64_t)((a.m + 255) / 256) * ((a.n + 255) / 256) >= compute_units() * 3 / 4)
+        return launch_tiles<256, 256, 2, 4, true>(a, stream);
+    return launch_tiles<128, 128, 2, 2, true>(a, stream);
 }
 
 }  // namespace
