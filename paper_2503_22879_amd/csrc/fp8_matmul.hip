@@ -109,92 +109,6 @@ __device__ __forceinline__ void store_row(void *y, int64_t at, const float (&v)[
     }
 }
 
-// ---- up to 64 rows of x: the weight streams past ----
-
-// A workgroup takes 16 columns of y (rows of w) over the whole depth, every wave one block in 8; codes go from memory to registers.
-template <int MF>  // 16-row parts of x
-__global__ __launch_bounds__(512) void fp8_matmul_rows_kernel(MatmulArgs a)
-{
-    constexpr int kWaves = 8, kAhead = MF == 1 ? 4 : 2;
-    __shared__ float red[kWaves][MF * 4][64];
-    const int lane = threadIdx.x & 63, r = lane & 15, part = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int n0 = blockIdx.x * 16;
-    const uint8_t *wp = a.w + (int64_t)min(n0 + r, a.n - 1) * a.w_stride + part * 32;
-    const uint8_t *xp[MF];
-    const float *xs[MF];
-#pragma unroll
-    for (int f = 0; f < MF; ++f) {
-        const int64_t row = min(f * 16 + r, a.m - 1);
-        xp[f] = a.x + row * a.x_stride + part * 32;
-        xs[f] = a.x_scales + row * a.blocks;
-    }
-    const float *ws = a.w_scales + (int64_t)(n0 / kBlock) * a.blocks;
-    float4v sum[MF];
-#pragma unroll
-    for (int f = 0; f < MF; ++f) sum[f] = float4v{0, 0, 0, 0};
-    auto step = [&](int b, const int4v &w0, const int4v &w1, const int4v *x, const float *s) {
-        const Part w(w0, w1);
-#pragma unroll
-        for (int f = 0; f < MF; ++f) {
-            const float4v p = multiply(w, Part(x[2 * f], x[2 * f + 1]));
-            const float scale = s[f] * ws[b];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) sum[f][e] = fmaf(p[e], scale, sum[f][e]);
-        }
-    };
-    const int whole = a.k / kBlock;
-    int b = wave;
-    for (; b + (kAhead - 1) * kWaves < whole; b += kAhead * kWaves) {
-        int4v w[kAhead][2], x[kAhead][2 * MF];
-        float s[kAhead][MF];
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            const int64_t k = (int64_t)(b + u * kWaves) * kBlock;
-            __builtin_memcpy(&w[u][0], wp + k, 16);
-            __builtin_memcpy(&w[u][1], wp + k + 16, 16);
-        }
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u)
-#pragma unroll
-            for (int f = 0; f < MF; ++f) {
-                const int64_t k = (int64_t)(b + u * kWaves) * kBlock;
-                __builtin_memcpy(&x[u][2 * f], xp[f] + k, 16);
-                __builtin_memcpy(&x[u][2 * f + 1], xp[f] + k + 16, 16);
-                s[u][f] = xs[f][b + u * kWaves];
-            }
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) step(b + u * kWaves, w[u][0], w[u][1], x[u], s[u]);
-    }
-    for (; b < a.blocks; b += kWaves) {
-        const int64_t k = (int64_t)b * kBlock;
-        const int left = a.k - b * kBlock - part * 32;
-        int4v x[2 * MF];
-        float s[MF];
-#pragma unroll
-        for (int f = 0; f < MF; ++f) {
-            x[2 * f] = load16(xp[f] + k, left);
-            x[2 * f + 1] = load16(xp[f] + k + 16, left - 16);
-            s[f] = xs[f][b];
-        }
-        step(b, load16(wp + k, left), load16(wp + k + 16, left - 16), x, s);
-    }
-#pragma unroll
-    for (int f = 0; f < MF; ++f)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) red[wave][4 * f + e][lane] = sum[f][e];
-    __syncthreads();
-    for (int t = threadIdx.x; t < MF * 256; t += 512) {
-        const int i = t >> 4, j = t & 15;
-        const int at = 4 * (i >> 4) + (j & 3), from = (j >> 2) * 16 + (i & 15);
-        float v = 0.0f;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) v += red[w][at][from];
-        if (i < a.m && n0 + j < a.n) store(a.y, a.y_type, i * a.y_stride + n0 + j, v);
-    }
-}
-
-// ---- more rows: tiles of x and w in LDS ----
-
 // 16 (or 4) bytes for each lane from `base` + its offset into LDS at `to` + 16 (4) times the lane, without a register between.  Their
 // arrival counts as a vector load's: wait_for_tiles() waits for it.
 __device__ __forceinline__ void load_to_lds16(const void *base, uint32_t offset, uint32_t to)
@@ -211,6 +125,155 @@ __device__ __forceinline__ uint32_t lds_address(const void *p)
 {
     return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char *)p;
 }
+
+// ---- up to 64 rows of x: the weight streams past ----
+
+template <int N>
+__device__ __forceinline__ void wait_for_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+
+constexpr int rows_ahead(int mf, int waves) { return mf * waves > 8 && waves > 4 ? 2 : 3; }  // blocks of a ring
+constexpr int rows_stage(int mf) { return (2 + 2 * mf) * 1024 + 256; }                      // bytes of one
+
+// 16 columns of y (rows of w) at a time to a workgroup, over the whole depth, every wave one block in kWaves.  A wave has its own ring of
+// kAhead blocks in LDS, of 16 rows of w and 16 MF of x and the scales of x's rows, and waits for nobody until the waves' sums
+// meet at the end of a column part; the loads go on into the next part meanwhile.  Rows pass through LDS because 8 lanes that
+// take a row's 128 codes together are one access to a cache, and 16 lanes on 16 rows, as the products want them, are 16 (one row of x,
+// 18560 x 4096: 15.0 us, 16 rows 24.6 us, straight to registers).  The order of a row's pieces in LDS is the tiles'
+// below.  The first block depends on the workgroup: rows 4096 bytes apart lie in one channel of the memory, and
+// workgroups that go through the depth together would all be at that one.
+template <int MF, int kWaves, bool DIRECT>
+__global__ __launch_bounds__(64 * kWaves) void fp8_matmul_rows_kernel(MatmulArgs a, int parts)
+{
+    constexpr int kAhead = rows_ahead(MF, kWaves), kTurns = 2 + 2 * MF, kStage = rows_stage(MF), kLoads = kTurns + 1;
+    extern __shared__ __align__(16) char lds[];
+    const int lane = threadIdx.x & 63, r = lane & 15, part = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    char *ring = lds + wave * kAhead * kStage;
+    auto red = reinterpret_cast<float(*)[kWaves][MF * 4][64]>(lds + kWaves * kAhead * kStage);
+    const uint32_t ring_at = lds_address(ring);
+    const int whole = a.k / kBlock, each = (a.blocks - wave + kWaves - 1) / kWaves;  // blocks of this wave in a part
+    const int mine = (parts - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x;  // parts of this workgroup
+    auto columns = [&](int q) { return ((int)blockIdx.x + q * (int)gridDim.x) * 16; };
+    const int turned = (int)(blockIdx.x >> 3) % a.blocks;
+    auto block = [&](int i) {
+        const int b = wave + i * kWaves + turned;
+        return b >= a.blocks ? b - a.blocks : b;
+    };
+    // 8 rows in turn, 8 lanes to a row: w's 16, then x's
+    auto piece_of = [&](int turn) { return (lane & 7) ^ ((turn & 1) << 2 | lane >> 4); };
+    const int last_piece = (a.k - whole * kBlock) / 16 - 1;  // of a last block in part
+    uint32_t x_offset[DIRECT ? 2 * MF : 1], scale_offset = 0;
+    if (DIRECT) {
+#pragma unroll
+        for (int t = 0; t < 2 * MF; ++t) x_offset[t] = (uint32_t)min(t * 8 + (lane >> 3), a.m - 1) * (uint32_t)a.x_stride;
+        scale_offset = (uint32_t)min(lane, a.m - 1) * (uint32_t)a.blocks * 4;
+    }
+    auto start = [&](int slot, int n0, int b) {  // DIRECT: any block; the pieces behind the depth repeat the last one
+        const int most = b < whole ? 7 : last_piece;
+        const uint32_t to = ring_at + slot * kStage;
+        const uint8_t *x = a.x + (int64_t)b * kBlock, *w = a.w + (int64_t)n0 * a.w_stride + (int64_t)b * kBlock;
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // what was read from the slot has arrived
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+            load_to_lds16(w, (uint32_t)min(t * 8 + (lane >> 3), a.n - 1 - n0) * (uint32_t)a.w_stride + min(piece_of(t), most) * 16, to + t * 1024);
+#pragma unroll
+        for (int t = 0; t < 2 * MF; ++t) load_to_lds16(x, x_offset[t] + min(piece_of(t), most) * 16, to + 2048 + t * 1024);
+        load_to_lds4(a.x_scales + b, scale_offset, to + kTurns * 1024);
+    };
+    int4v held[kTurns];
+    float held_scale;
+    auto fetch = [&](int n0, int b) {  // any block, to registers
+#pragma unroll
+        for (int t = 0; t < kTurns; ++t) {
+            const uint8_t *p = t < 2 ? a.w + (int64_t)min(n0 + t * 8 + (lane >> 3), a.n - 1) * a.w_stride
+                                     : a.x + (int64_t)min((t - 2) * 8 + (lane >> 3), a.m - 1) * a.x_stride;
+            held[t] = load16(p + (int64_t)b * kBlock + piece_of(t) * 16, a.k - b * kBlock - piece_of(t) * 16);
+        }
+        held_scale = a.x_scales[(int64_t)min(lane, a.m - 1) * a.blocks + b];
+    };
+    auto put = [&](int slot) {
+        char *to = ring + slot * kStage;
+#pragma unroll
+        for (int t = 0; t < kTurns; ++t) *reinterpret_cast<int4v *>(to + t * 1024 + lane * 16) = held[t];
+        reinterpret_cast<float *>(to + kTurns * 1024)[lane] = held_scale;
+    };
+    float4v sum[MF];
+    const int at = r * kBlock + (part ^ r >> 1) * 16;
+    auto step = [&](int slot, int n0, int b) {
+        const char *from = ring + slot * kStage;
+        const float *xs = reinterpret_cast<const float *>(from + kTurns * 1024);
+        const float wsc = ((const __attribute__((address_space(4))) float *)a.w_scales)[(int64_t)(n0 / kBlock) * a.blocks + b];
+        // what stands behind the depth counts as zeros
+        const bool lo = !DIRECT || b < whole || part <= last_piece, hi = !DIRECT || b < whole || part + 4 <= last_piece;
+        auto codes = [&](const char *p) {
+            int4v c0 = *reinterpret_cast<const int4v *>(p + at), c1 = *reinterpret_cast<const int4v *>(p + (at ^ 64));
+            if (DIRECT && b >= whole) {
+                c0 = lo ? c0 : int4v{0, 0, 0, 0};
+                c1 = hi ? c1 : int4v{0, 0, 0, 0};
+            }
+            return Part(c0, c1);
+        };
+        const Part wf = codes(from);
+#pragma unroll
+        for (int f = 0; f < MF; ++f) {
+            const float4v p = multiply(wf, codes(from + 2048 + f * 2048));
+            const float scale = xs[f * 16 + r] * wsc;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[f][e] = fmaf(p[e], scale, sum[f][e]);
+        }
+    };
+
+    // the loads run ahead of the products, through the blocks of this workgroup's parts
+    int next_q = 0, next_i = 0, slot = 0;
+    auto ahead = [&](int to) {
+        if (next_q < mine) {
+            start(to, columns(next_q), block(next_i));
+            if (++next_i == each) {
+                next_i = 0;
+                ++next_q;
+            }
+        }
+    };
+    if (DIRECT && each)
+        for (int u = 0; u < kAhead; ++u) ahead(u);
+    for (int q = 0; q < mine; ++q) {
+        const int n0 = columns(q);
+#pragma unroll
+        for (int f = 0; f < MF; ++f) sum[f] = float4v{0, 0, 0, 0};
+        if (!DIRECT && each) fetch(n0, block(0));
+        for (int i = 0; i < each; ++i) {
+            const int b = block(i);
+            if (!DIRECT) {
+                put(0);
+                if (i + 1 < each) fetch(n0, block(i + 1));
+                step(0, n0, b);
+            } else {
+                if (next_q < mine)  // kAhead - 1 blocks behind this one are on their way
+                    wait_for_loads<kLoads *(kAhead - 1)>();
+                else
+                    wait_for_loads<0>();
+                step(slot, n0, b);
+                ahead(slot);
+                slot = slot + 1 == kAhead ? 0 : slot + 1;
+            }
+        }
+        auto &sums = red[q & 1];
+#pragma unroll
+        for (int f = 0; f < MF; ++f)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sums[wave][4 * f + e][lane] = sum[f][e];
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");  // not for the loads
+        for (int t = threadIdx.x; t < MF * 256; t += 64 * kWaves) {
+            const int i = t >> 4, j = t & 15;
+            const int e = 4 * (i >> 4) + (j & 3), from = (j >> 2) * 16 + (i & 15);
+            float v = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) v += sums[w][e][from];
+            if (i < a.m && n0 + j < a.n) store(a.y, a.y_type, i * a.y_stride + n0 + j, v);
+        }
+    }
+}
+
+// ---- more rows: tiles of x and w in LDS ----
 
 // The order of the tiles: the device hands workgroups to its 8 dies in turn, so every eighth one belongs to a die; each die gets
 // consecutive tiles, and these go up and down bands of 8 tiles along m, so that the die's cache holds what they share.
@@ -237,7 +300,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void fp8_matmul_tile_kernel(Matmul
     constexpr int kWaves = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
     constexpr int kRows = BM + BN, kScales = kRows * kBlock, kStage = kScales + BM * 4;
     static_assert(kRows / 8 % kWaves == 0 && BM % 64 == 0 && BM / 64 <= kWaves && BN % 128 == 0 && (BN / WN) <= 128, "");
-    extern __shared__ char lds[];
+    extern __shared__ __align__(16) char lds[];
     const int lane = threadIdx.x & 63, r = lane & 15, part = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave % WM, wn = wave / WM;
     int tm, tn;
@@ -374,20 +437,34 @@ hipError_t launch_tiles(const MatmulArgs &a, hipStream_t stream)
     return hipGetLastError();
 }
 
+template <int MF, int kWaves, bool DIRECT>
+hipError_t launch_rows_as(const MatmulArgs &a, hipStream_t stream)
+{
+    constexpr auto kernel = &fp8_matmul_rows_kernel<MF, kWaves, DIRECT>;
+    constexpr size_t kRing = (size_t)rows_ahead(MF, kWaves) * rows_stage(MF) * kWaves, kSums = 2 * kWaves * MF * 1024;
+    static_assert(kRing + kSums <= kLdsPerCu, "");
+    const hipError_t e = allow_full_lds<kernel>();
+    if (e != hipSuccess) return e;
+    const int parts = (a.n + 15) / 16, resident = (int)(kLdsPerCu / (kRing + kSums)) * compute_units();
+    kernel<<<std::min(parts, resident), 64 * kWaves, kRing + kSums, stream>>>(a, parts);
+    return hipGetLastError();
+}
+
+template <int MF>
+hipError_t launch_rows(const MatmulArgs &a, bool direct, hipStream_t stream)
+{
+    if (MF < 4 && (a.n + 15) / 16 <= compute_units() && a.blocks >= 16)  // the depth in more parts where a unit has no more than one workgroup
+        return direct ? launch_rows_as<MF, MF < 4 ? 8 : 4, true>(a, stream) : launch_rows_as<MF, MF < 4 ? 8 : 4, false>(a, stream);
+    return direct ? launch_rows_as<MF, 4, true>(a, stream) : launch_rows_as<MF, 4, false>(a, stream);
+}
+
 hipError_t launch_part(const MatmulArgs &a, hipStream_t stream)
 {
-    if (a.m <= 64) {
-        const int grid = (a.n + 15) / 16;
-        if (a.m <= 16)
-            fp8_matmul_rows_kernel<1><<<grid, 512, 0, stream>>>(a);
-        else if (a.m <= 32)
-            fp8_matmul_rows_kernel<2><<<grid, 512, 0, stream>>>(a);
-        else
-            fp8_matmul_rows_kernel<4><<<grid, 512, 0, stream>>>(a);
-        return hipGetLastError();
-    }
-    auto direct = [](const uint8_t *p, int64_t stride) { return (reinterpret_cast<uintptr_t>(p) | (uint64_t)stride) % 16 == 0 && stride < 1 << 24; };
-    if (!direct(a.x, a.x_stride) || !direct(a.w, a.w_stride)) return launch_tiles<128, 128, 2, 2, false>(a, stream);
+    auto aligned = [](const uint8_t *p, int64_t stride) { return (reinterpret_cast<uintptr_t>(p) | (uint64_t)stride) % 16 == 0 && stride < 1 << 24; };
+    const bool direct = aligned(a.x, a.x_stride) && aligned(a.w, a.w_stride) && a.k % 16 == 0;
+    if (a.m <= 64)
+        return a.m <= 16 ? launch_rows<1>(a, direct, stream) : a.m <= 32 ? launch_rows<2>(a, direct, stream) : launch_rows<4>(a, direct, stream);
+    if (!direct) return launch_tiles<128, 128, 2, 2, false>(a, stream);
     if (a.m > 128 && (int64_t)((a.m + 255) / 256) * ((a.n + 255) / 256) >= compute_units() * 3 / 4)
         return launch_tiles<256, 256, 2, 4, true>(a, stream);
     return launch_tiles<128, 128, 2, 2, true>(a, stream);
