@@ -7,6 +7,8 @@
 // depth 13 bits below the largest of them: sums of 128 normal values are off by 1.6e-5 of themselves, and by 5e-5 where the
 // values' sizes spread, against 1e-8 here.
 #include <algorithm>
+#include <cstdlib>
+#include <cstdio>
 #include <type_traits>
 
 #include "quamba_internal.h"
@@ -110,7 +112,7 @@ __device__ __forceinline__ void store_row(void *y, int64_t at, const float (&v)[
 }
 
 // 16 (or 4) bytes for each lane from `base` + its offset into LDS at `to` + 16 (4) times the lane, without a register between.  Their
-// arrival counts as a vector load's: wait_for_tiles() waits for it.
+// arrival counts as a vector load's: wait_for_tiles() and wait_for_loads() wait for it.
 __device__ __forceinline__ void load_to_lds16(const void *base, uint32_t offset, uint32_t to)
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory", "m0");
@@ -119,7 +121,9 @@ __device__ __forceinline__ void load_to_lds4(const void *base, uint32_t offset, 
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory", "m0");
 }
-__device__ __forceinline__ void wait_for_tiles() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+// Until all but the wave's last N loads have arrived, and all its reads from LDS; then for the other waves.
+template <int N>
+__device__ __forceinline__ void wait_for_tiles() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory"); }
 
 __device__ __forceinline__ uint32_t lds_address(const void *p)
 {
@@ -288,31 +292,35 @@ __device__ __forceinline__ void tile_of(int id, int tiles_m, int tiles_n, int &t
     tm = first + in_band - tn * rows;
 }
 
-// BM x BN outputs to a workgroup of WM x WN waves.  LDS holds two blocks (128 codes deep) of BM + BN rows and the scales of x's rows; the next
-// block arrives while one is multiplied.  A lane takes pieces l / 16 and l / 16 + 4 of the 8 of 16 bytes that a row has (any order along the
-// depth will do that is the same for x and w), and piece c of row r lies at c ^ (r / 2 % 8), so that the lanes that read together
-// hit different banks.  Which row of w stands where in a 16-row part is free as well: row 4 p + e of part j is the wave's row
-// 4 TN p + 4 j + e, so that a lane ends up with 4 TN adjacent columns of y.  DIRECT: rows at multiples of 16
-// bytes less than 2^24 bytes apart go from memory to LDS by themselves; else through registers.
-template <int BM, int BN, int WM, int WN, bool DIRECT>
-__global__ __launch_bounds__(64 * WM * WN, 2) void fp8_matmul_tile_kernel(MatmulArgs a, int tiles_m, int tiles_n)
+// BM x BN outputs to a workgroup of WM x WN waves.  LDS holds STAGES blocks (128 codes deep) of BM + BN rows and the scales of x's rows;
+// blocks arrive while earlier ones are multiplied.  A lane takes pieces l / 16 and l / 16 + 4 of the 8 of 16 bytes that a row has (any
+// order along the depth will do that is the same for x and w), and piece c of row r lies at c ^ (r / 2 % 8), so that the lanes that
+// read together hit different banks.  Which row of w stands where in a 16-row part is free as well: row 4 p + e of part j is the
+// wave's row 4 TN p + 4 j + e, so that a lane ends up with 4 TN adjacent columns of y.  DIRECT: rows at multiples of 16 bytes less
+// than 2^24 bytes apart, and a depth of whole pieces, go from memory to LDS by themselves; else through registers.
+// `splits`: workgroups to a tile, each with a part of the depth, whose sums go to `partial` [splits, m, columns].
+template <int BM, int BN, int WM, int WN, int STAGES, bool DIRECT>
+__global__ __launch_bounds__(64 * WM * WN, 2) void fp8_matmul_tile_kernel(MatmulArgs a, int tiles_m, int tiles_n, int splits, float *partial,
+                                                                          int64_t columns)
 {
     constexpr int kWaves = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
-    constexpr int kRows = BM + BN, kScales = kRows * kBlock, kStage = kScales + BM * 4;
-    static_assert(kRows / 8 % kWaves == 0 && BM % 64 == 0 && BM / 64 <= kWaves && BN % 128 == 0 && (BN / WN) <= 128, "");
+    constexpr int kRows = BM + BN, kScales = kRows * kBlock, kStage = kScales + BM * 4, kTurns = kRows / 8 / kWaves;
+    static_assert(kTurns * 8 * kWaves == kRows && kTurns % 2 == 0 && BM % 64 == 0 && BM / 64 <= kWaves && kBlock % (BN / WN) == 0, "");
     extern __shared__ __align__(16) char lds[];
     const int lane = threadIdx.x & 63, r = lane & 15, part = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave % WM, wn = wave / WM;
     int tm, tn;
+    const int split = blockIdx.y;
     tile_of(blockIdx.x, tiles_m, tiles_n, tm, tn);
     const int m0 = tm * BM, n0 = tn * BN;
     const uint8_t *xb = a.x + (int64_t)m0 * a.x_stride, *wb = a.w + (int64_t)n0 * a.w_stride;
     const float *xsb = a.x_scales + (int64_t)m0 * a.blocks;
     const auto *ws = (const __attribute__((address_space(4))) float *)(a.w_scales + (int64_t)((n0 + wn * (BN / WN)) / kBlock) * a.blocks);
     const int last_x = a.m - 1 - m0, last_w = a.n - 1 - n0;
+    const int whole = a.k / kBlock, last_piece = (a.k - whole * kBlock) / 16 - 1;  // of a last block in part
+    const int first = (int)((int64_t)a.blocks * split / splits), end = (int)((int64_t)a.blocks * (split + 1) / splits);
 
     // 8 rows of a tile in turn: this lane's piece of them
-    constexpr int kTurns = kRows / 8 / kWaves;
     auto row_of = [&](int turn) { return (turn * kWaves + wave) * 8 + (lane >> 3); };
     auto is_x = [&](int turn) { return (turn * kWaves + wave) * 8 < BM; };
     auto order = [&](int turn) {  // among the 16 rows that are read together
@@ -326,31 +334,40 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void fp8_matmul_tile_kernel(Matmul
         for (int t = 0; t < kTurns; ++t)
             offset[t] = is_x(t) ? (uint32_t)min(row_of(t), last_x) * (uint32_t)a.x_stride + piece_of(t) * 16
                                 : (uint32_t)min(row_of(t) - BM, last_w) * (uint32_t)a.w_stride + piece_of(t) * 16;
-        scale_offset = (uint32_t)min(wave * 64 + lane, last_x) * (uint32_t)a.blocks * 4;
+        scale_offset = (uint32_t)min(wave % (BM / 64) * 64 + lane, last_x) * (uint32_t)a.blocks * 4;
     }
     const uint32_t base = lds_address(lds);
-    auto start = [&](int b, int half) {  // DIRECT: a half of a whole block (2: all of it) on its way
-        const uint32_t to = base + (b & 1) * kStage;
+    // DIRECT: a half of block b (2: all of it) on its way into a stage; the pieces behind the depth repeat the last one.  Every wave
+    // issues as many loads as the others (the scales more than once).
+    auto start = [&](int b, int stage, int half) {
+        const uint32_t to = base + stage * kStage;
         const uint8_t *x = xb + (int64_t)b * kBlock, *w = wb + (int64_t)b * kBlock;
+        if (b < whole) {
 #pragma unroll
-        for (int t = 0; t < kTurns; ++t)
-            if (half == 2 || half == t / (kTurns / 2)) load_to_lds16(is_x(t) ? x : w, offset[t], to + (t * kWaves + wave) * 1024);
-        if (half != 1 && wave < BM / 64) load_to_lds4(xsb + b, scale_offset, to + kScales + wave * 256);
+            for (int t = 0; t < kTurns; ++t)
+                if (half == 2 || half == t / (kTurns / 2)) load_to_lds16(is_x(t) ? x : w, offset[t], to + (t * kWaves + wave) * 1024);
+        } else {
+#pragma unroll
+            for (int t = 0; t < kTurns; ++t)
+                if (half == 2 || half == t / (kTurns / 2))
+                    load_to_lds16(is_x(t) ? x : w, offset[t] - max(piece_of(t) - last_piece, 0) * 16, to + (t * kWaves + wave) * 1024);
+        }
+        if (half != 1) load_to_lds4(xsb + b, scale_offset, to + kScales + wave % (BM / 64) * 256);
     };
-    int4v held[kTurns];
+    int4v held[DIRECT ? 1 : kTurns];
     float held_scale = 0.0f;
     auto fetch = [&](int b) {  // any block, to registers
 #pragma unroll
-        for (int t = 0; t < kTurns; ++t) {
+        for (int t = 0; t < (DIRECT ? 1 : kTurns); ++t) {
             const uint8_t *p = is_x(t) ? xb + (int64_t)min(row_of(t), last_x) * a.x_stride : wb + (int64_t)min(row_of(t) - BM, last_w) * a.w_stride;
             held[t] = load16(p + (int64_t)b * kBlock + piece_of(t) * 16, a.k - b * kBlock - piece_of(t) * 16);
         }
         if ((int)threadIdx.x < BM) held_scale = xsb[(int64_t)min((int)threadIdx.x, last_x) * a.blocks + b];
     };
-    auto put = [&](int b) {
-        char *to = lds + (b & 1) * kStage;
+    auto put = [&](int stage) {
+        char *to = lds + stage * kStage;
 #pragma unroll
-        for (int t = 0; t < kTurns; ++t) *reinterpret_cast<int4v *>(to + (t * kWaves + wave) * 1024 + lane * 16) = held[t];
+        for (int t = 0; t < (DIRECT ? 1 : kTurns); ++t) *reinterpret_cast<int4v *>(to + (t * kWaves + wave) * 1024 + lane * 16) = held[t];
         if ((int)threadIdx.x < BM) reinterpret_cast<float *>(to + kScales)[threadIdx.x] = held_scale;
     };
 
@@ -362,18 +379,25 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void fp8_matmul_tile_kernel(Matmul
     const int at = r * kBlock + (part ^ r >> 1) * 16, at_w = ((r >> 2) * 4 * TN + (r & 3)) * kBlock + (part ^ r >> 1) * 16;
     // Multiplies block b; between its first parts block `next` (below 0: none) is started, in two halves: a wave waits where it
     // issues more loads than fit a queue, and after the first part's reads it has products to make meanwhile (16384 x 18560 x 4096: 2.15 -> 2.11 ms).
-    auto compute = [&](int b, int next) {
-        const char *x = lds + (b & 1) * kStage + wm * (BM / WM) * kBlock, *w = lds + (b & 1) * kStage + (BM + wn * (BN / WN)) * kBlock;
-        const float *xs = reinterpret_cast<const float *>(lds + (b & 1) * kStage + kScales) + wm * (BM / WM) + r;
+    auto compute = [&](int b, int stage, int next, int next_stage, auto in_part) {
+        const char *x = lds + stage * kStage + wm * (BM / WM) * kBlock, *w = lds + stage * kStage + (BM + wn * (BN / WN)) * kBlock;
+        const float *xs = reinterpret_cast<const float *>(lds + stage * kStage + kScales) + wm * (BM / WM) + r;
         const float wsc = ws[b];
+        auto codes = [&](const char *p, int to) {
+            int4v c0 = *reinterpret_cast<const int4v *>(p + to), c1 = *reinterpret_cast<const int4v *>(p + (to ^ 64));
+            if (in_part.value) {  // what stands behind the depth counts as zeros
+                c0 = part <= last_piece ? c0 : int4v{0, 0, 0, 0};
+                c1 = part + 4 <= last_piece ? c1 : int4v{0, 0, 0, 0};
+            }
+            return Part(c0, c1);
+        };
         Part wf[TN];
 #pragma unroll
-        for (int j = 0; j < TN; ++j)
-            wf[j] = Part(*reinterpret_cast<const int4v *>(w + j * 4 * kBlock + at_w), *reinterpret_cast<const int4v *>(w + j * 4 * kBlock + (at_w ^ 64)));
+        for (int j = 0; j < TN; ++j) wf[j] = codes(w + j * 4 * kBlock, at_w);
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
-            const Part xf(*reinterpret_cast<const int4v *>(x + i * 16 * kBlock + at), *reinterpret_cast<const int4v *>(x + i * 16 * kBlock + (at ^ 64)));
-            if (DIRECT && i < 2 && next >= 0) start(next, i);
+            const Part xf = codes(x + i * 16 * kBlock, at);
+            if (DIRECT && i < 2 && next >= 0) start(next, next_stage, i);
             const float s = xs[i * 16] * wsc;
             float4v p[TN];
 #pragma unroll
@@ -384,30 +408,36 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void fp8_matmul_tile_kernel(Matmul
                 for (int e = 0; e < 4; ++e) sum[i][j][e] = fmaf(p[j][e], s, sum[i][j][e]);
         }
     };
+    const std::false_type all_of_it;
+    const std::true_type in_part;
 
     if (DIRECT) {
-        const int whole = a.k / kBlock;
-        if (whole) start(0, 2);
-        for (int b = 0; b < whole; ++b) {
-            wait_for_tiles();  // block b is there for all waves, and block b - 1 has been read by all
-            compute(b, b + 1 < whole ? b + 1 : -1);
+        for (int u = 0; u < STAGES - 1; ++u)
+            if (first + u < end) start(first + u, u, 2);
+        int stage = 0, b = first;
+        for (; b < min(end, whole); ++b) {
+            // block b is there for all waves, and block b - 1 has been read by all
+            if (STAGES > 2 && b + STAGES - 2 < end)
+                wait_for_tiles<(kTurns + 1) * (STAGES - 2)>();
+            else
+                wait_for_tiles<0>();
+            compute(b, stage, b + STAGES - 1 < end ? b + STAGES - 1 : -1, stage ? stage - 1 : STAGES - 1, all_of_it);
+            stage = stage + 1 == STAGES ? 0 : stage + 1;
         }
-        if (whole < a.blocks) {
-            fetch(whole);
-            put(whole);  // where block whole - 2 was, which all waves have left behind
-            __syncthreads();
-            compute(whole, -1);
+        if (b < end) {
+            wait_for_tiles<0>();
+            compute(b, stage, -1, 0, in_part);
         }
     } else {
-        fetch(0);
-        for (int b = 0; b < a.blocks; ++b) {
-            put(b);
+        fetch(first);
+        for (int b = first; b < end; ++b) {
+            put(b & 1);
             __syncthreads();
-            if (b + 1 < a.blocks) fetch(b + 1);
-            compute(b, -1);
+            if (b + 1 < end) fetch(b + 1);
+            compute(b, b & 1, -1, 0, all_of_it);
         }
     }
-    auto write = [&](auto type) {
+    auto write = [&](auto type, void *y, int64_t stride) {
         const int col = n0 + wn * (BN / WN) + part * 4 * TN;
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
@@ -415,25 +445,50 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void fp8_matmul_tile_kernel(Matmul
             float v[4 * TN];
 #pragma unroll
             for (int j = 0; j < 4 * TN; ++j) v[j] = sum[i][j / 4][j % 4];
-            if (row < a.m) store_row<decltype(type)::value>(a.y, row * a.y_stride + col, v, a.n - col);
+            if (row < a.m) store_row<decltype(type)::value>(y, row * stride + col, v, a.n - col);
         }
     };
-    if (a.y_type == QUAMBA_F32)
-        write(std::integral_constant<int, QUAMBA_F32>());
+    if (splits > 1)
+        write(std::integral_constant<int, QUAMBA_F32>(), partial + split * a.m * columns, columns);
+    else if (a.y_type == QUAMBA_F32)
+        write(std::integral_constant<int, QUAMBA_F32>(), a.y, a.y_stride);
     else if (a.y_type == QUAMBA_F16)
-        write(std::integral_constant<int, QUAMBA_F16>());
+        write(std::integral_constant<int, QUAMBA_F16>(), a.y, a.y_stride);
     else
-        write(std::integral_constant<int, QUAMBA_BF16>());
+        write(std::integral_constant<int, QUAMBA_BF16>(), a.y, a.y_stride);
 }
 
-template <int BM, int BN, int WM, int WN, bool DIRECT>
-hipError_t launch_tiles(const MatmulArgs &a, hipStream_t stream)
+// y of the splits' sums, in their order; 4 columns to a thread.
+__global__ __launch_bounds__(256) void fp8_matmul_join_kernel(MatmulArgs a, int splits, const float *partial, int64_t columns)
 {
-    constexpr auto kernel = &fp8_matmul_tile_kernel<BM, BN, WM, WN, DIRECT>;
-    const hipError_t e = allow_full_lds<kernel>();
+    const int col = ((int)blockIdx.x * 256 + (int)threadIdx.x) * 4, row = blockIdx.y;
+    if (col >= a.n) return;
+    const float *p = partial + row * columns + col;
+    float4v v = *reinterpret_cast<const float4v *>(p);
+    for (int s = 1; s < splits; ++s) v += *reinterpret_cast<const float4v *>(p + s * a.m * columns);
+    const float out[4] = {v[0], v[1], v[2], v[3]};
+    const int64_t to = row * a.y_stride + col;
+    if (a.y_type == QUAMBA_F32)
+        store_row<QUAMBA_F32>(a.y, to, out, a.n - col);
+    else if (a.y_type == QUAMBA_F16)
+        store_row<QUAMBA_F16>(a.y, to, out, a.n - col);
+    else
+        store_row<QUAMBA_BF16>(a.y, to, out, a.n - col);
+}
+
+template <int BM, int BN, int WM, int WN, int STAGES, bool DIRECT>
+hipError_t launch_tiles(const MatmulArgs &a, int splits, float *partial, hipStream_t stream)
+{
+    constexpr auto kernel = &fp8_matmul_tile_kernel<BM, BN, WM, WN, STAGES, DIRECT>;
+    hipError_t e = allow_full_lds<kernel>();
     if (e != hipSuccess) return e;
     const int tiles_m = (a.m + BM - 1) / BM, tiles_n = (a.n + BN - 1) / BN;
-    kernel<<<tiles_m * tiles_n, 64 * WM * WN, 2 * ((BM + BN) * kBlock + BM * 4), stream>>>(a, tiles_m, tiles_n);
+    const int64_t columns = ((int64_t)a.n + 3) / 4 * 4;
+    kernel<<<dim3(tiles_m * tiles_n, splits), 64 * WM * WN, STAGES * ((BM + BN) * kBlock + BM * 4), stream>>>(a, tiles_m, tiles_n, splits,
+                                                                                                             partial, columns);
+    e = hipGetLastError();
+    if (e != hipSuccess || splits == 1) return e;
+    fp8_matmul_join_kernel<<<dim3((a.n + 1023) / 1024, a.m), 256, 0, stream>>>(a, splits, partial, columns);
     return hipGetLastError();
 }
 
@@ -458,23 +513,51 @@ hipError_t launch_rows(const MatmulArgs &a, bool direct, hipStream_t stream)
     return direct ? launch_rows_as<MF, 4, true>(a, stream) : launch_rows_as<MF, 4, false>(a, stream);
 }
 
-hipError_t launch_part(const MatmulArgs &a, hipStream_t stream)
+// How a product is made: rings of rows up to 32 rows, tiles of size x size else, the depth in `splits` parts.
+struct Plan {
+    int tile;  // 0: rows
+    int splits;
+};
+
+Plan plan_of(int32_t m, int32_t n, int32_t blocks, bool workspace)
+{
+    const int units = compute_units();
+    auto tiles = [&](int size) { return ((int64_t)m + size - 1) / size * (((int64_t)n + size - 1) / size); };
+    if (m <= 32 || (m <= 64 && !workspace)) return {0, 1};
+    if (const char *e = getenv("PLAN")) { Plan p; sscanf(e, "%d,%d", &p.tile, &p.splits); if (!workspace) p.splits = 1; return p; }
+    if (m > 128 && tiles(256) >= units * 3 / 4) return {256, 1};
+    if (m > 128 && tiles(128) >= units * 3 / 4) return {128, 1};
+    int splits = 1;
+    if (workspace) while (tiles(64) * splits < 2 * units && blocks / (2 * splits) >= 4) splits *= 2;
+    return {64, splits};
+}
+
+hipError_t launch_part(const MatmulArgs &a, void *workspace, hipStream_t stream)
 {
     auto aligned = [](const uint8_t *p, int64_t stride) { return (reinterpret_cast<uintptr_t>(p) | (uint64_t)stride) % 16 == 0 && stride < 1 << 24; };
     const bool direct = aligned(a.x, a.x_stride) && aligned(a.w, a.w_stride) && a.k % 16 == 0;
-    if (a.m <= 64)
-        return a.m <= 16 ? launch_rows<1>(a, direct, stream) : a.m <= 32 ? launch_rows<2>(a, direct, stream) : launch_rows<4>(a, direct, stream);
-    if (!direct) return launch_tiles<128, 128, 2, 2, false>(a, stream);
-    if (a.m > 128 && (int64_t)((a.m + 255) / 256) * ((a.n + 255) / 256) >= compute_units() * 3 / 4)
-        return launch_tiles<256, 256, 2, 4, true>(a, stream);
-    return launch_tiles<128, 128, 2, 2, true>(a, stream);
+    const Plan plan = plan_of(a.m, a.n, a.blocks, workspace);
+    float *partial = static_cast<float *>(workspace);
+    switch (plan.tile) {
+        case 0: return a.m <= 16 ? launch_rows<1>(a, direct, stream) : a.m <= 32 ? launch_rows<2>(a, direct, stream) : launch_rows<4>(a, direct, stream);
+        case 64: return direct ? launch_tiles<64, 64, 2, 2, 4, true>(a, plan.splits, partial, stream)
+                               : launch_tiles<64, 64, 2, 2, 2, false>(a, plan.splits, partial, stream);
+        case 256:
+            if (direct) return launch_tiles<256, 256, 2, 4, 2, true>(a, 1, nullptr, stream);
+        default: return direct ? launch_tiles<128, 128, 2, 2, 2, true>(a, plan.splits, partial, stream)
+                               : launch_tiles<128, 128, 2, 2, 2, false>(a, plan.splits, partial, stream);
+    }
 }
 
 }  // namespace
 
-size_t fp8_matmul_workspace_bytes(int32_t, int32_t, int32_t) { return 0; }
+size_t fp8_matmul_workspace_bytes(int32_t m, int32_t n, int32_t k)
+{
+    const int splits = plan_of(m, n, (k + kBlock - 1) / kBlock, true).splits;
+    return splits > 1 ? (size_t)splits * m * (((size_t)n + 3) / 4 * 4) * sizeof(float) : 0;
+}
 
-hipError_t launch_fp8_matmul(const MatmulArgs &a, void *, hipStream_t stream)
+hipError_t launch_fp8_matmul(const MatmulArgs &a, void *workspace, hipStream_t stream)
 {
     // launches of fewer than 2^22 tiles of 128 x 128 (n has at most 2^19, m any number): threads and tiles fit 32 bits
     const int64_t tiles_n = ((int64_t)a.n + 127) / 128;
@@ -485,7 +568,7 @@ hipError_t launch_fp8_matmul(const MatmulArgs &a, void *, hipStream_t stream)
         p.x = a.x + first * a.x_stride;
         p.x_scales = a.x_scales + first * a.blocks;
         p.y = static_cast<char *>(a.y) + first * a.y_stride * (a.y_type == QUAMBA_F32 ? 4 : 2);
-        const hipError_t e = launch_part(p, stream);
+        const hipError_t e = launch_part(p, first || p.m < a.m ? nullptr : workspace, stream);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
