@@ -7,8 +7,6 @@
 // depth 13 bits below the largest of them: sums of 128 normal values are off by 1.6e-5 of themselves, and by 5e-5 where the
 // values' sizes spread, against 1e-8 here.
 #include <algorithm>
-#include <cstdlib>
-#include <cstdio>
 #include <type_traits>
 
 #include "quamba_internal.h"
@@ -202,64 +200,48 @@ __global__ __launch_bounds__(64 * kWaves) void fp8_matmul_rows_kernel(MatmulArgs
     };
     float4v sum[MF];
     const int at = r * kBlock + (part ^ r >> 1) * 16;
-    auto step = [&](int slot, int n0, int b) {
+    struct Raw {  // a block of the ring in registers
+        int4v w[2], x[MF][2];
+        float xs[MF], ws;
+    };
+    auto read = [&](Raw &v, int slot, int n0, int b) {
         const char *from = ring + slot * kStage;
-        const float *xs = reinterpret_cast<const float *>(from + kTurns * 1024);
-        const float wsc = ((const __attribute__((address_space(4))) float *)a.w_scales)[(int64_t)(n0 / kBlock) * a.blocks + b];
-        // what stands behind the depth counts as zeros
-        const bool lo = !DIRECT || b < whole || part <= last_piece, hi = !DIRECT || b < whole || part + 4 <= last_piece;
-        auto codes = [&](const char *p) {
-            int4v c0 = *reinterpret_cast<const int4v *>(p + at), c1 = *reinterpret_cast<const int4v *>(p + (at ^ 64));
-            if (DIRECT && b >= whole) {
-                c0 = lo ? c0 : int4v{0, 0, 0, 0};
-                c1 = hi ? c1 : int4v{0, 0, 0, 0};
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            v.w[h] = *reinterpret_cast<const int4v *>(from + (at ^ 64 * h));
+#pragma unroll
+            for (int f = 0; f < MF; ++f) v.x[f][h] = *reinterpret_cast<const int4v *>(from + 2048 * (1 + f) + (at ^ 64 * h));
+        }
+#pragma unroll
+        for (int f = 0; f < MF; ++f) v.xs[f] = reinterpret_cast<const float *>(from + kTurns * 1024)[f * 16 + r];
+        v.ws = ((const __attribute__((address_space(4))) float *)a.w_scales)[(int64_t)(n0 / kBlock) * a.blocks + b];
+    };
+    auto step = [&](Raw &v, int b) {
+        if (DIRECT && b >= whole) {  // what stands behind the depth counts as zeros
+            const int4v none{0, 0, 0, 0};
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const bool in = part + 4 * h <= last_piece;
+                v.w[h] = in ? v.w[h] : none;
+#pragma unroll
+                for (int f = 0; f < MF; ++f) v.x[f][h] = in ? v.x[f][h] : none;
             }
-            return Part(c0, c1);
-        };
-        const Part wf = codes(from);
+        }
+        const Part wf(v.w[0], v.w[1]);
 #pragma unroll
         for (int f = 0; f < MF; ++f) {
-            const float4v p = multiply(wf, codes(from + 2048 + f * 2048));
-            const float scale = xs[f * 16 + r] * wsc;
+            const float4v p = multiply(wf, Part(v.x[f][0], v.x[f][1]));
+            const float scale = v.xs[f] * v.ws;
 #pragma unroll
             for (int e = 0; e < 4; ++e) sum[f][e] = fmaf(p[e], scale, sum[f][e]);
         }
     };
-
-    // the loads run ahead of the products, through the blocks of this workgroup's parts
-    int next_q = 0, next_i = 0, slot = 0;
-    auto ahead = [&](int to) {
-        if (next_q < mine) {
-            start(to, columns(next_q), block(next_i));
-            if (++next_i == each) {
-                next_i = 0;
-                ++next_q;
-            }
-        }
-    };
-    if (DIRECT && each)
-        for (int u = 0; u < kAhead; ++u) ahead(u);
-    for (int q = 0; q < mine; ++q) {
-        const int n0 = columns(q);
+    auto clear = [&] {
 #pragma unroll
         for (int f = 0; f < MF; ++f) sum[f] = float4v{0, 0, 0, 0};
-        if (!DIRECT && each) fetch(n0, block(0));
-        for (int i = 0; i < each; ++i) {
-            const int b = block(i);
-            if (!DIRECT) {
-                put(0);
-                if (i + 1 < each) fetch(n0, block(i + 1));
-                step(0, n0, b);
-            } else {
-                if (next_q < mine)  // kAhead - 1 blocks behind this one are on their way
-                    wait_for_loads<kLoads *(kAhead - 1)>();
-                else
-                    wait_for_loads<0>();
-                step(slot, n0, b);
-                ahead(slot);
-                slot = slot + 1 == kAhead ? 0 : slot + 1;
-            }
-        }
+    };
+    auto finish = [&](int q) {  // the waves' sums of a part meet
+        const int n0 = columns(q);
         auto &sums = red[q & 1];
 #pragma unroll
         for (int f = 0; f < MF; ++f)
@@ -274,6 +256,67 @@ __global__ __launch_bounds__(64 * kWaves) void fp8_matmul_rows_kernel(MatmulArgs
             for (int w = 0; w < kWaves; ++w) v += sums[w][e][from];
             if (i < a.m && n0 + j < a.n) store(a.y, a.y_type, i * a.y_stride + n0 + j, v);
         }
+        clear();
+    };
+    clear();
+    if (each == 0) {  // fewer blocks than waves
+        for (int q = 0; q < mine; ++q) finish(q);
+        return;
+    }
+    if (!DIRECT) {
+        Raw v;
+        for (int q = 0; q < mine; ++q) {
+            fetch(columns(q), block(0));
+            for (int i = 0; i < each; ++i) {
+                put(0);
+                if (i + 1 < each) fetch(columns(q), block(i + 1));
+                read(v, 0, columns(q), block(i));
+                step(v, block(i));
+            }
+            finish(q);
+        }
+        return;
+    }
+    // The loads run kAhead blocks ahead of the products, through the blocks of this workgroup's parts, and the reads from LDS one
+    // block: a wave has its SIMD for itself or nearly so, and would wait for each of them.
+    int next_q = 0, next_i = 0, slot = 0, q = 0, i = 0;
+    auto ahead = [&](int to) {
+        if (next_q < mine) {
+            start(to, columns(next_q), block(next_i));
+            if (++next_i == each) {
+                next_i = 0;
+                ++next_q;
+            }
+        }
+    };
+    for (int u = 0; u < kAhead; ++u) ahead(u);
+    Raw even, odd;
+    auto wait = [&] {  // for the block behind the kAhead - 1 last ones
+        if (next_q < mine)
+            wait_for_loads<kLoads *(kAhead - 1)>();
+        else
+            wait_for_loads<0>();
+    };
+    wait();
+    read(even, 0, columns(0), block(0));
+    auto turn = [&](Raw &now, Raw &then) {  // false behind the last block
+        const int b = block(i), this_q = q;
+        const bool ends = ++i == each;
+        if (ends) {
+            i = 0;
+            ++q;
+        }
+        ahead(slot);  // `now` has left it
+        slot = slot + 1 == kAhead ? 0 : slot + 1;
+        if (q < mine) {
+            wait();
+            read(then, slot, columns(q), block(i));
+        }
+        step(now, b);
+        if (ends) finish(this_q);
+        return q < mine;
+    };
+    while (turn(even, odd) && turn(odd, even)) {
     }
 }
 
@@ -298,17 +341,22 @@ __device__ __forceinline__ void tile_of(int id, int tiles_m, int tiles_n, int &t
 // read together hit different banks.  Which row of w stands where in a 16-row part is free as well: row 4 p + e of part j is the
 // wave's row 4 TN p + 4 j + e, so that a lane ends up with 4 TN adjacent columns of y.  DIRECT: rows at multiples of 16 bytes less
 // than 2^24 bytes apart, and a depth of whole pieces, go from memory to LDS by themselves; else through registers.
-// `splits`: workgroups to a tile, each with a part of the depth, whose sums go to `partial` [splits, m, columns].
-template <int BM, int BN, int WM, int WN, int STAGES, bool DIRECT>
-__global__ __launch_bounds__(64 * WM * WN, 2) void fp8_matmul_tile_kernel(MatmulArgs a, int tiles_m, int tiles_n, int splits, float *partial,
+// GROUPS of WM x WN waves take the blocks in turn, each from stages of its own, and their sums meet in LDS at the end: more waves to
+// wait for memory and LDS where tiles are small.  `splits`: workgroups to a tile, each with a part of the depth, whose sums go to
+// `partial` [splits, m, columns].
+template <int BM, int BN, int WM, int WN, int GROUPS, int STAGES, bool DIRECT>
+__global__ __launch_bounds__(64 * WM * WN * GROUPS, GROUPS > 2 ? 4 : 2) void fp8_matmul_tile_kernel(MatmulArgs a, int tiles_m, int tiles_n, int splits, float *partial,
                                                                           int64_t columns)
 {
     constexpr int kWaves = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
     constexpr int kRows = BM + BN, kScales = kRows * kBlock, kStage = kScales + BM * 4, kTurns = kRows / 8 / kWaves;
     static_assert(kTurns * 8 * kWaves == kRows && kTurns % 2 == 0 && BM % 64 == 0 && BM / 64 <= kWaves && kBlock % (BN / WN) == 0, "");
-    extern __shared__ __align__(16) char lds[];
-    const int lane = threadIdx.x & 63, r = lane & 15, part = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    static_assert((GROUPS - 1) * BM * BN * 4 <= GROUPS * STAGES * kStage, "");
+    extern __shared__ __align__(16) char all_lds[];
+    const int lane = threadIdx.x & 63, r = lane & 15, part = lane >> 4, any_wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int group = any_wave / kWaves, wave = any_wave % kWaves, thread = wave * 64 + lane;
     const int wm = wave % WM, wn = wave / WM;
+    char *lds = all_lds + group * STAGES * kStage;
     int tm, tn;
     const int split = blockIdx.y;
     tile_of(blockIdx.x, tiles_m, tiles_n, tm, tn);
@@ -319,6 +367,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void fp8_matmul_tile_kernel(Matmul
     const int last_x = a.m - 1 - m0, last_w = a.n - 1 - n0;
     const int whole = a.k / kBlock, last_piece = (a.k - whole * kBlock) / 16 - 1;  // of a last block in part
     const int first = (int)((int64_t)a.blocks * split / splits), end = (int)((int64_t)a.blocks * (split + 1) / splits);
+    const int turns = (end - first + GROUPS - 1) / GROUPS, mine = (end - first - group + GROUPS - 1) / GROUPS;  // blocks
+    auto block = [&](int i) { return first + group + i * GROUPS; };
 
     // 8 rows of a tile in turn: this lane's piece of them
     auto row_of = [&](int turn) { return (turn * kWaves + wave) * 8 + (lane >> 3); };
@@ -362,13 +412,13 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void fp8_matmul_tile_kernel(Matmul
             const uint8_t *p = is_x(t) ? xb + (int64_t)min(row_of(t), last_x) * a.x_stride : wb + (int64_t)min(row_of(t) - BM, last_w) * a.w_stride;
             held[t] = load16(p + (int64_t)b * kBlock + piece_of(t) * 16, a.k - b * kBlock - piece_of(t) * 16);
         }
-        if ((int)threadIdx.x < BM) held_scale = xsb[(int64_t)min((int)threadIdx.x, last_x) * a.blocks + b];
+        if (thread < BM) held_scale = xsb[(int64_t)min(thread, last_x) * a.blocks + b];
     };
     auto put = [&](int stage) {
         char *to = lds + stage * kStage;
 #pragma unroll
         for (int t = 0; t < (DIRECT ? 1 : kTurns); ++t) *reinterpret_cast<int4v *>(to + (t * kWaves + wave) * 1024 + lane * 16) = held[t];
-        if ((int)threadIdx.x < BM) reinterpret_cast<float *>(to + kScales)[threadIdx.x] = held_scale;
+        if (thread < BM) reinterpret_cast<float *>(to + kScales)[thread] = held_scale;
     };
 
     float4v sum[TM][TN];
@@ -413,29 +463,43 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void fp8_matmul_tile_kernel(Matmul
 
     if (DIRECT) {
         for (int u = 0; u < STAGES - 1; ++u)
-            if (first + u < end) start(first + u, u, 2);
-        int stage = 0, b = first;
-        for (; b < min(end, whole); ++b) {
-            // block b is there for all waves, and block b - 1 has been read by all
-            if (STAGES > 2 && b + STAGES - 2 < end)
+            if (u < mine) start(block(u), u, 2);
+        int stage = 0, i = 0;
+        for (; i < mine && block(i) < whole; ++i) {
+            // block i is there for all waves, and block i - 1 has been read by all
+            if (STAGES > 2 && i + STAGES - 2 < mine)
                 wait_for_tiles<(kTurns + 1) * (STAGES - 2)>();
             else
                 wait_for_tiles<0>();
-            compute(b, stage, b + STAGES - 1 < end ? b + STAGES - 1 : -1, stage ? stage - 1 : STAGES - 1, all_of_it);
+            const int next = i + STAGES - 1;
+            compute(block(i), stage, next < mine ? block(next) : -1, stage ? stage - 1 : STAGES - 1, all_of_it);
             stage = stage + 1 == STAGES ? 0 : stage + 1;
         }
-        if (b < end) {
+        for (; i < turns; ++i) {  // at most one, for the group's partial block or for the others
             wait_for_tiles<0>();
-            compute(b, stage, -1, 0, in_part);
+            if (i < mine) compute(block(i), stage, -1, 0, in_part);
         }
     } else {
-        fetch(first);
-        for (int b = first; b < end; ++b) {
-            put(b & 1);
+        if (mine) fetch(block(0));
+        for (int i = 0; i < turns; ++i) {
+            if (i < mine) put(i & 1);
             __syncthreads();
-            if (b + 1 < end) fetch(b + 1);
-            compute(b, b & 1, -1, 0, all_of_it);
+            if (i + 1 < mine) fetch(block(i + 1));
+            if (i < mine) compute(block(i), i & 1, -1, 0, all_of_it);
         }
+    }
+    if (GROUPS > 1) {
+        float *sums = reinterpret_cast<float *>(all_lds) + wave * TM * TN * 256 + lane;
+        __syncthreads();
+        if (group)
+#pragma unroll
+            for (int i = 0; i < TM * TN * 4; ++i) sums[(group - 1) * BM * BN + i * 64] = sum[i / 4 / TN][i / 4 % TN][i % 4];
+        __syncthreads();
+        if (group) return;
+#pragma unroll
+        for (int g = 1; g < GROUPS; ++g)
+#pragma unroll
+            for (int i = 0; i < TM * TN * 4; ++i) sum[i / 4 / TN][i / 4 % TN][i % 4] += sums[(g - 1) * BM * BN + i * 64];
     }
     auto write = [&](auto type, void *y, int64_t stride) {
         const int col = n0 + wn * (BN / WN) + part * 4 * TN;
@@ -476,16 +540,17 @@ __global__ __launch_bounds__(256) void fp8_matmul_join_kernel(MatmulArgs a, int 
         store_row<QUAMBA_BF16>(a.y, to, out, a.n - col);
 }
 
-template <int BM, int BN, int WM, int WN, int STAGES, bool DIRECT>
+template <int BM, int BN, int WM, int WN, int GROUPS, int STAGES, bool DIRECT>
 hipError_t launch_tiles(const MatmulArgs &a, int splits, float *partial, hipStream_t stream)
 {
-    constexpr auto kernel = &fp8_matmul_tile_kernel<BM, BN, WM, WN, STAGES, DIRECT>;
+    constexpr auto kernel = &fp8_matmul_tile_kernel<BM, BN, WM, WN, GROUPS, STAGES, DIRECT>;
     hipError_t e = allow_full_lds<kernel>();
     if (e != hipSuccess) return e;
     const int tiles_m = (a.m + BM - 1) / BM, tiles_n = (a.n + BN - 1) / BN;
     const int64_t columns = ((int64_t)a.n + 3) / 4 * 4;
-    kernel<<<dim3(tiles_m * tiles_n, splits), 64 * WM * WN, STAGES * ((BM + BN) * kBlock + BM * 4), stream>>>(a, tiles_m, tiles_n, splits,
-                                                                                                             partial, columns);
+    constexpr int kLds = GROUPS * STAGES * ((BM + BN) * kBlock + BM * 4);
+    static_assert(kLds <= (int)kLdsPerCu, "");
+    kernel<<<dim3(tiles_m * tiles_n, splits), 64 * WM * WN * GROUPS, kLds, stream>>>(a, tiles_m, tiles_n, splits, partial, columns);
     e = hipGetLastError();
     if (e != hipSuccess || splits == 1) return e;
     fp8_matmul_join_kernel<<<dim3((a.n + 1023) / 1024, a.m), 256, 0, stream>>>(a, splits, partial, columns);
@@ -505,47 +570,83 @@ hipError_t launch_rows_as(const MatmulArgs &a, hipStream_t stream)
     return hipGetLastError();
 }
 
+// Waves of a workgroup for up to 64 rows: the depth in more parts where a unit has no more than one workgroup.
+int rows_waves(int32_t m, int32_t n, int32_t blocks) { return m <= 32 && (n + 15) / 16 <= compute_units() && blocks >= 16 ? 8 : 4; }
+
 template <int MF>
 hipError_t launch_rows(const MatmulArgs &a, bool direct, hipStream_t stream)
 {
-    if (MF < 4 && (a.n + 15) / 16 <= compute_units() && a.blocks >= 16)  // the depth in more parts where a unit has no more than one workgroup
+    if (MF < 4 && rows_waves(a.m, a.n, a.blocks) == 8)
         return direct ? launch_rows_as<MF, MF < 4 ? 8 : 4, true>(a, stream) : launch_rows_as<MF, MF < 4 ? 8 : 4, false>(a, stream);
     return direct ? launch_rows_as<MF, 4, true>(a, stream) : launch_rows_as<MF, 4, false>(a, stream);
 }
 
-// How a product is made: rings of rows up to 32 rows, tiles of size x size else, the depth in `splits` parts.
-struct Plan {
-    int tile;  // 0: rows
-    int splits;
-};
+}  // namespace
 
-Plan plan_of(int32_t m, int32_t n, int32_t blocks, bool workspace)
+// The form that is estimated to be done first, from what a round of workgroups takes in us on 256 units: a fixed time and one for each
+// turn (a block of 128 of the depth, or two where two groups of waves share them).
+//
+//   form                                 fixed  turn   measured                            next best
+//   rows, 17 to 32 rows of x             3.5    0.7    32 x 18560 x 4096           28      64 x 128            23 (taken)
+//   rows, 33 to 64                       3.5    0.95   64 x 2560 x 5120            11.2    64 x 64 in 4 parts  12.3
+//   64 x 64, two groups                  3      0.76   128 x 4096 x 8192, 2 parts  19.9    in one part         27
+//   64 x 128, two groups                 3.8    1.17   500 x 4096 x 4096           24      64 x 64             33
+//   128 x 128, two groups, one workgroup
+//     to a unit                          4.2    1.85   1000 x 4096 x 8192          66      two to a unit       77
+//   128 x 128, one group, two to a unit  4.9    1.87   8192 x 3352 x 768           56      256 x 256           63
+//   256 x 256                            10     3.35   16384 x 18560 x 4096        2110    128 x 128           2230
+//
+// Up to 16 rows rings of rows are bound by memory and always taken.
+Fp8Plan fp8_matmul_plan(int32_t m, int32_t n, int32_t blocks, bool workspace)
 {
+    if (m <= 16) return {Fp8Form::rows, 1};
     const int units = compute_units();
-    auto tiles = [&](int size) { return ((int64_t)m + size - 1) / size * (((int64_t)n + size - 1) / size); };
-    if (m <= 32 || (m <= 64 && !workspace)) return {0, 1};
-    if (const char *e = getenv("PLAN")) { Plan p; sscanf(e, "%d,%d", &p.tile, &p.splits); if (!workspace) p.splits = 1; return p; }
-    if (m > 128 && tiles(256) >= units * 3 / 4) return {256, 1};
-    if (m > 128 && tiles(128) >= units * 3 / 4) return {128, 1};
-    int splits = 1;
-    if (workspace) while (tiles(64) * splits < 2 * units && blocks / (2 * splits) >= 4) splits *= 2;
-    return {64, splits};
+    auto tiles = [&](int rows, int columns) { return ((int64_t)m + rows - 1) / rows * (((int64_t)n + columns - 1) / columns); };
+    auto rounds = [&](int64_t workgroups) { return (double)((workgroups + units - 1) / units); };
+    auto pairs = [&](int splits) { return (blocks + 2 * splits - 1) / (2 * splits); };
+    Fp8Plan best{Fp8Form::tiles256, 1};
+    double least = 1.0 + rounds(tiles(256, 256)) * (10.0 + 3.35 * blocks);
+    auto offer = [&](Fp8Form form, int splits, double time) {
+        if (time < least) {
+            best = {form, splits};
+            least = time;
+        }
+    };
+    const int64_t t128 = tiles(128, 128);
+    // a unit's second workgroup fills the gaps of the first, and a last round that is half empty is half as long
+    offer(Fp8Form::tiles128_two, 1,
+          t128 <= units ? 5.0 + 1.05 * blocks : 3.0 + (rounds(t128) + (double)t128 / units) / 4 * (4.9 + 1.87 * blocks));
+    offer(Fp8Form::tiles128_one, 1, 1.0 + rounds(t128) * (4.2 + 1.85 * pairs(1)));
+    offer(Fp8Form::tiles64x128, 1, 1.0 + rounds(tiles(64, 128)) * (3.8 + 1.17 * pairs(1)));
+    for (int s = 1; s == 1 || (workspace && s <= 16 && blocks / s >= 4); s *= 2)
+        offer(Fp8Form::tiles64, s, 2.0 + rounds(tiles(64, 64) * s) * (3.0 + 0.76 * pairs(s)) + (s > 1 ? 2.5 + 1e-6 * s * m * n : 0.0));
+    if (m <= 64) {
+        const int64_t parts = ((int64_t)n + 15) / 16;
+        offer(Fp8Form::rows, 1, 3.5 + (m <= 32 ? 0.7 : 0.95) * rounds(parts) * ((blocks - 1) / rows_waves(m, n, blocks) + 1));
+    }
+    return best;
 }
+
+namespace {
 
 hipError_t launch_part(const MatmulArgs &a, void *workspace, hipStream_t stream)
 {
     auto aligned = [](const uint8_t *p, int64_t stride) { return (reinterpret_cast<uintptr_t>(p) | (uint64_t)stride) % 16 == 0 && stride < 1 << 24; };
     const bool direct = aligned(a.x, a.x_stride) && aligned(a.w, a.w_stride) && a.k % 16 == 0;
-    const Plan plan = plan_of(a.m, a.n, a.blocks, workspace);
+    const Fp8Plan plan = fp8_matmul_plan(a.m, a.n, a.blocks, workspace);
     float *partial = static_cast<float *>(workspace);
-    switch (plan.tile) {
-        case 0: return a.m <= 16 ? launch_rows<1>(a, direct, stream) : a.m <= 32 ? launch_rows<2>(a, direct, stream) : launch_rows<4>(a, direct, stream);
-        case 64: return direct ? launch_tiles<64, 64, 2, 2, 4, true>(a, plan.splits, partial, stream)
-                               : launch_tiles<64, 64, 2, 2, 2, false>(a, plan.splits, partial, stream);
-        case 256:
-            if (direct) return launch_tiles<256, 256, 2, 4, 2, true>(a, 1, nullptr, stream);
-        default: return direct ? launch_tiles<128, 128, 2, 2, 2, true>(a, plan.splits, partial, stream)
-                               : launch_tiles<128, 128, 2, 2, 2, false>(a, plan.splits, partial, stream);
+    if (plan.form == Fp8Form::rows)
+        return a.m <= 16 ? launch_rows<1>(a, direct, stream) : a.m <= 32 ? launch_rows<2>(a, direct, stream) : launch_rows<4>(a, direct, stream);
+    if (!direct) {
+        if (plan.form == Fp8Form::tiles64) return launch_tiles<64, 64, 2, 2, 2, 2, false>(a, plan.splits, partial, stream);
+        return launch_tiles<128, 128, 2, 2, 1, 2, false>(a, 1, nullptr, stream);
+    }
+    switch (plan.form) {
+        case Fp8Form::tiles64: return launch_tiles<64, 64, 2, 2, 2, 4, true>(a, plan.splits, partial, stream);
+        case Fp8Form::tiles64x128: return launch_tiles<64, 128, 2, 2, 2, 3, true>(a, 1, nullptr, stream);
+        case Fp8Form::tiles128_one: return launch_tiles<128, 128, 2, 2, 2, 2, true>(a, 1, nullptr, stream);
+        case Fp8Form::tiles128_two: return launch_tiles<128, 128, 2, 2, 1, 2, true>(a, 1, nullptr, stream);
+        default: return launch_tiles<256, 256, 2, 4, 1, 2, true>(a, 1, nullptr, stream);
     }
 }
 
@@ -553,13 +654,13 @@ hipError_t launch_part(const MatmulArgs &a, void *workspace, hipStream_t stream)
 
 size_t fp8_matmul_workspace_bytes(int32_t m, int32_t n, int32_t k)
 {
-    const int splits = plan_of(m, n, (k + kBlock - 1) / kBlock, true).splits;
+    const int splits = fp8_matmul_plan(m, n, (k + kBlock - 1) / kBlock, true).splits;
     return splits > 1 ? (size_t)splits * m * (((size_t)n + 3) / 4 * 4) * sizeof(float) : 0;
 }
 
 hipError_t launch_fp8_matmul(const MatmulArgs &a, void *workspace, hipStream_t stream)
 {
-    // launches of fewer than 2^22 tiles of 128 x 128 (n has at most 2^19, m any number): threads and tiles fit 32 bits
+    // launches of fewer than 2^22 tiles of 128 x 128 (n has at most 2^19, m any number; 4 times as many of 64 x 64): threads and tiles fit 32 bits
     const int64_t tiles_n = ((int64_t)a.n + 127) / 128;
     const int64_t rows = std::max<int64_t>(1, ((int64_t)1 << 22) / tiles_n) * 128;
     for (int64_t first = 0; first < a.m; first += rows) {

@@ -408,6 +408,13 @@ struct MatmulArgs {
     int32_t blocks;      // of the depth
     int32_t y_type;
 };
+// How a product is made, and in how many parts of the depth.
+enum class Fp8Form : int { rows, tiles64, tiles64x128, tiles128_one, tiles128_two, tiles256 };
+struct Fp8Plan {
+    Fp8Form form;
+    int splits;
+};
+Fp8Plan fp8_matmul_plan(int32_t m, int32_t n, int32_t blocks, bool workspace);
 size_t fp8_matmul_workspace_bytes(int32_t m, int32_t n, int32_t k);
 hipError_t launch_fp8_matmul(const MatmulArgs &a, void *workspace, hipStream_t stream);
 

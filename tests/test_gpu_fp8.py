@@ -134,6 +134,23 @@ def test_matmul(gpu_lib, m, n, k):
     assert np.array_equal(_matmul(gpu_lib, ops, "fp32"), _matmul(gpu_lib, ops, "fp32"))
 
 
+# A size of each form of the product (test_operator_refusals.py checks which), with a depth of whole blocks, of a partial one, and of one
+# whose rows lie at odd addresses; ragged in rows and columns.
+FORMS = {"rows": [(5, 300, 2048), (30, 300, 2064), (60, 300, 400)], "tiles64": [(100, 500, 4112), (130, 4000, 1024)],
+         "tiles64x128": [(500, 4001, 1040)], "tiles128_one": [(600, 4095, 400), (1000, 3901, 768)], "tiles128_two": [(2000, 2501, 400)],
+         "tiles256": [(4090, 4003, 1296)]}
+
+
+@pytest.mark.parametrize("m,n,k", [s for sizes in FORMS.values() for s in sizes])
+def test_matmul_of_every_form(gpu_lib, m, n, k):
+    for depth in (k, k // 128 * 128, k + 3):
+        ops = _operands(m, n, depth, m + depth)
+        y, top = oracle.ref_fp8_matmul(*ops)
+        for kind in ("fp32", "bf16"):
+            off = np.abs(_matmul(gpu_lib, ops, kind, pad=5) - y) / _bound(y, top, depth, kind)
+            assert off.max() <= 1.0, (depth, kind, off.max(), np.argwhere(off > 1)[:5])
+
+
 @pytest.mark.parametrize("m,n,k", [(1, 200, 512), (20, 200, 512), (70, 300, 640), (300, 520, 384)])
 def test_matmul_strides_and_alignment(gpu_lib, m, n, k):
     """Operands cut out of wider tensors: rows at multiples of 16 bytes, of 4 and at odd places, and of another width."""

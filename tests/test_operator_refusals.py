@@ -48,6 +48,25 @@ def test_matmul(p):
         assert q.quamba_fp8_matmul_workspace_size(*sizes) == 0
 
 
+def test_every_form_of_the_product_has_a_size_that_is_tested():
+    """The form that a size takes, as it is planned without a GPU, for 256 compute units."""
+    from test_gpu_fp8 import FORMS
+
+    class Plan(C.Structure):
+        _fields_ = [("form", C.c_int), ("splits", C.c_int)]
+    plan = getattr(q.load_library(), "_ZN6quamba15fp8_matmul_planEiiib")      # library-internal
+    plan.restype, plan.argtypes = Plan, [C.c_int32] * 3 + [C.c_bool]
+    for form, sizes in enumerate(FORMS.values()):
+        for m, n, k in sizes:
+            got = plan(m, n, -(-k // 128), True)
+            assert got.form == form, (m, n, k, got.form)
+            size = q.quamba_fp8_matmul_workspace_size(m, n, k)
+            assert (size > 0) == (got.splits > 1) and size == (got.splits * m * -(-n // 4) * 16 if size else 0)
+            without = plan(m, n, -(-k // 128), False)
+            assert without.splits == 1
+    assert plan(100, 500, 33, True).splits > 1
+
+
 def test_select(p):
     f = q.load_library().quamba_beam_select
     size = q.quamba_beam_select_workspace_size(1, 2, 10, 4)
