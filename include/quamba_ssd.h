@@ -466,7 +466,7 @@ int quamba_fp8_matmul(int64_t m, int64_t n, int64_t k, const uint8_t *x, int64_t
  *               must not overlap.
  * batch = 0: nothing is launched.
  * Errors: ENULL, ESHAPE (sizes not positive, beams > 64, count > 128, vocab > 2^30, beams * vocab > 2^32 - 1, 2^24 or more
- * pieces of 16384 logits in all, stride), EINVAL (type, pad_token out of the vocabulary), EWORKSPACE (missing, too small or not aligned), EHIP.
+ * pieces of 8192 logits in all, stride), EINVAL (type, pad_token out of the vocabulary), EWORKSPACE (missing, too small or not aligned), EHIP.
  */
 size_t quamba_beam_select_workspace_size(int32_t batch, int32_t beams, int32_t vocab, int32_t count);
 int quamba_beam_select(int32_t batch, int32_t beams, int32_t vocab, int32_t count, const void *logits, int32_t type,

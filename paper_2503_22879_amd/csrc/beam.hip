@@ -37,39 +37,48 @@ __device__ __forceinline__ float wave_max(float v)
 
 struct Chooser {
     uint64_t gathered[kGathered];
-    uint32_t tops[kThreads];
     uint64_t wave_best[2][kWaves];
+    uint32_t tops[kThreads];
     int n;
 };
 
-// The `count` largest of the workgroup's keys, key(e) for e < E in every thread, 0 for none and otherwise all different: out[0 ..
-// count - 1], largest first, 0 where there are no more.  `top` is the upper half of the thread's largest key, and from(bound) gives
-// the test, for e, whether key(e)'s upper half is at least `bound`.  `out` is written by some threads; the caller waits before
-// it is read elsewhere.
-//
-// `count` threads have a key at least as large as the count-th largest of the threads' own largest ones, so nothing below that
-// is among the best: what is left is mostly little more than `count` keys, which are ranked by counting.  The bound is sought bit
-// by bit, by every wave for itself, in the upper 16 of a key's bits (for floats the sign, the exponent and 7 bits more: the
-// last bits would spare few keys).
-template <int E, typename From, typename Key, typename Out>
-__device__ __forceinline__ void choose(Chooser &c, int count, uint32_t top, const From &from, const Key &key, const Out &out)
+// A bound that at least `count` of the threads' tops reach, where so many are above 0, and few more: the largest of those whose lower
+// 32 - BITS bits are 0.  Bit by bit, by every wave for itself.
+template <int BITS>
+__device__ __forceinline__ uint32_t bound_of(Chooser &c, int count, uint32_t top)
 {
-    const int t = threadIdx.x, lane = t & 63;
-    c.tops[t] = top;
-    if (t == 0) c.n = 0;
+    c.tops[threadIdx.x] = top;
+    if (threadIdx.x == 0) c.n = 0;
     __syncthreads();
     uint32_t mine[kWaves], bound = 0;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) mine[w] = c.tops[w * 64 + lane];
+    for (int w = 0; w < kWaves; ++w) mine[w] = c.tops[w * 64 + (threadIdx.x & 63)];
 #pragma unroll
-    for (int bit = 31; bit >= 16; --bit) {
+    for (int bit = 31; bit >= 32 - BITS; --bit) {
         const uint32_t higher = bound | 1u << bit;
         int n = 0;
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) n += __builtin_popcountll(__builtin_amdgcn_ballot_w64(mine[w] >= higher));
         bound = n >= count ? higher : bound;
     }
-    bound = max(bound, 1u);
+    return max(bound, 1u);
+}
+
+// The `count` largest of the workgroup's keys, key(e) for e < E in every thread, 0 for none and otherwise all different: out[0 ..
+// count - 1], largest first, 0 where there are no more.  `top` is the upper half of the thread's largest key, and from(bound) gives
+// the test, for e, whether key(e)'s upper half is at least `bound`.  `out` is written by some threads; the caller waits before
+// it is read elsewhere, and before it calls again.
+//
+// `count` threads have a key at least as large as the count-th largest of the threads' own largest ones, so nothing below that
+// is among the best: what is left is mostly little more than `count` keys, which are ranked by counting.  The bound is sought in
+// the upper 16 of a key's bits (for floats the sign, the exponent and 7 bits more: the last bits would spare few keys).  Where
+// the best keys lie in a few threads (the frequent tokens of a vocabulary side by side) more are left; as long as they are more than
+// threads, they are dealt out to all of them and bounded again.
+template <int E, typename From, typename Key, typename Out>
+__device__ __forceinline__ void choose(Chooser &c, int count, uint32_t top, const From &from, const Key &key, const Out &out)
+{
+    const int t = threadIdx.x, lane = t & 63;
+    const uint32_t bound = bound_of<16>(c, count, top);
     if (top >= bound) {
         const auto candidate = from(bound);
 #pragma unroll
@@ -80,11 +89,29 @@ __device__ __forceinline__ void choose(Chooser &c, int count, uint32_t top, cons
             }
     }
     __syncthreads();
-    const int n = c.n;
+    int n = c.n;
     if (n <= kGathered) {
+        for (int before = kGathered + 1; n > kThreads && n < before;) {
+            uint64_t mine[kGathered / kThreads];
+            uint32_t most = 0;
+#pragma unroll
+            for (int i = 0; i < kGathered / kThreads; ++i) {
+                mine[i] = i * kThreads + t < n ? c.gathered[i * kThreads + t] : 0;
+                most = max(most, (uint32_t)(mine[i] >> 32));
+            }
+            __syncthreads();  // all know n
+            const uint32_t least = bound_of<32>(c, count, most);
+#pragma unroll
+            for (int i = 0; i < kGathered / kThreads; ++i)
+                if ((uint32_t)(mine[i] >> 32) >= least) c.gathered[atomicAdd(&c.n, 1)] = mine[i];
+            __syncthreads();
+            before = n;
+            n = c.n;
+        }
         for (int i = t; i < n; i += kThreads) {
             const uint64_t k = c.gathered[i];
             int rank = 0;
+#pragma unroll 8
             for (int j = 0; j < n; ++j) rank += c.gathered[j] > k;
             if (rank < count) out(rank, k);
         }
@@ -124,59 +151,63 @@ __device__ __forceinline__ bool offers(const SelectArgs &a, int row)
     return __builtin_fabsf(s) < __builtin_inff();
 }
 
+// Sixteen bytes of logits.
 template <int TYPE>
-__device__ __forceinline__ float logit_of(const char *p)
-{
-    if (TYPE == QUAMBA_F32) {
-        float v;
-        __builtin_memcpy(&v, p, 4);
-        return v;
+struct Logits {
+    static constexpr int kBytes = TYPE == QUAMBA_F32 ? 4 : 2, kCount = 16 / kBytes;
+    uint32_t w[4];
+    __device__ __forceinline__ float operator[](int i) const
+    {
+        if (TYPE == QUAMBA_F32) return from_bits(w[i]);
+        const uint32_t h = i & 1 ? w[i / 2] >> 16 : w[i / 2] & 0xffffu;
+        return TYPE == QUAMBA_BF16 ? from_bits(h << 16) : (float)__builtin_bit_cast(_Float16, (uint16_t)h);
     }
-    uint16_t h;
-    __builtin_memcpy(&h, p, 2);
-    return TYPE == QUAMBA_BF16 ? from_bits((uint32_t)h << 16) : (float)__builtin_bit_cast(_Float16, h);
-}
+    __device__ __forceinline__ void load(const char *p) { __builtin_memcpy(w, p, 16); }
+    __device__ __forceinline__ void load(const char *p, int left)  // the first `left`, -infinity behind them
+    {
+        if (left >= kCount) {
+            load(p);
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = TYPE == QUAMBA_F32 ? 0xff800000u : TYPE == QUAMBA_BF16 ? 0xff80ff80u : 0xfc00fc00u;
+#pragma unroll
+        for (int i = 0; i < kCount; ++i)
+            if (i < left) {
+                if (kBytes == 4) {
+                    __builtin_memcpy(&w[i], p + 4 * i, 4);
+                } else {
+                    uint16_t h;
+                    __builtin_memcpy(&h, p + 2 * i, 2);
+                    w[i / 2] = i & 1 ? (w[i / 2] & 0xffffu) | (uint32_t)h << 16 : (w[i / 2] & 0xffff0000u) | h;
+                }
+            }
+    }
+};
 
-// A piece of 256 E logits to a workgroup.
+// A piece of 256 E logits of a row to a workgroup.
 template <int TYPE, int E>
-__global__ __launch_bounds__(kThreads) void beam_pieces_kernel(SelectArgs a, int pieces, Divisor by_pieces, uint64_t *best,
-                                                               Piece *piece)
+__global__ __launch_bounds__(kThreads) void beam_pieces_kernel(SelectArgs a, int pieces, Divisor by_pieces, uint64_t *best, Piece *piece)
 {
+    constexpr int kVec = Logits<TYPE>::kCount, VECTORS = E / kVec, kPiece = kThreads * E;
     __shared__ Chooser chooser;
     __shared__ float wave_f[2][kWaves];
-    const int row = quotient((int)blockIdx.x, by_pieces), part = blockIdx.x - row * pieces;
+    const int t = threadIdx.x, row = quotient((int)blockIdx.x, by_pieces), first = ((int)blockIdx.x - row * pieces) * kPiece;
     if (!offers(a, row) || (a.finished && a.finished[row])) return;  // the second launch does not read it
-    constexpr int kBytes = TYPE == QUAMBA_F32 ? 4 : 2, kVec = 16 / kBytes;
-    const char *p = static_cast<const char *>(a.logits) + (int64_t)row * a.stride * kBytes;
-    const int t = threadIdx.x;
-    float x[E];
-    const int first = part * (kThreads * E);
-    auto token = [&](int e) { return first + (e / kVec * kThreads + t) * kVec + e % kVec; };
-    if (first + kThreads * E <= a.vocab) {
-        char raw[E / kVec][16];
+    const char *p = static_cast<const char *>(a.logits) + ((int64_t)row * a.stride + first) * Logits<TYPE>::kBytes + t * 16;
+    Logits<TYPE> x[VECTORS];
+    if (first + kPiece <= a.vocab) {
 #pragma unroll
-        for (int v = 0; v < E / kVec; ++v) __builtin_memcpy(raw[v], p + (int64_t)token(v * kVec) * kBytes, 16);
-#pragma unroll
-        for (int e = 0; e < E; ++e) x[e] = logit_of<TYPE>(raw[e / kVec] + e % kVec * kBytes);
+        for (int v = 0; v < VECTORS; ++v) x[v].load(p + v * kThreads * 16);
     } else {
 #pragma unroll
-        for (int v = 0; v < E / kVec; ++v) {
-            const int at = token(v * kVec);
-            if (at + kVec <= a.vocab) {
-                char raw[16];
-                __builtin_memcpy(raw, p + (int64_t)at * kBytes, 16);
-#pragma unroll
-                for (int i = 0; i < kVec; ++i) x[v * kVec + i] = logit_of<TYPE>(raw + i * kBytes);
-            } else {
-#pragma unroll
-                for (int i = 0; i < kVec; ++i)
-                    x[v * kVec + i] = at + i < a.vocab ? logit_of<TYPE>(p + (int64_t)(at + i) * kBytes) : -__builtin_inff();
-            }
-        }
+        for (int v = 0; v < VECTORS; ++v) x[v].load(p + v * kThreads * 16, a.vocab - first - (v * kThreads + t) * kVec);
     }
+    auto logit = [&](int e) { return x[e / kVec][e % kVec]; };
+    auto token = [&](int e) { return first + (e / kVec * kThreads + t) * kVec + e % kVec; };
     float mine = -__builtin_inff();  // past a NaN, which the sum shows
 #pragma unroll
-    for (int e = 0; e < E; ++e) mine = fmaxf(mine, x[e]);
+    for (int e = 0; e < E; ++e) mine = fmaxf(mine, logit(e));
     float top = wave_max(mine);
     if (t % 64 == 0) wave_f[0][t / 64] = top;
     __syncthreads();
@@ -184,21 +215,24 @@ __global__ __launch_bounds__(kThreads) void beam_pieces_kernel(SelectArgs a, int
     const float against = top > -__builtin_inff() ? top : 0.0f;
     float sum = 0.0f;
 #pragma unroll
-    for (int e = 0; e < E; ++e) sum += __expf(x[e] - against);
+    for (int e = 0; e < E; ++e) sum += __expf(logit(e) - against);
     sum = group_sum<64>(sum);
     if (t % 64 == 0) wave_f[1][t / 64] = sum;
     uint64_t *to = best + (int64_t)blockIdx.x * a.count;
     choose<E>(
         chooser, a.count, mine > -__builtin_inff() ? ordered(mine + 0.0f) : 0u,  // -0 is 0
         [&](uint32_t bound) {
-            const float least = max(of_ordered(bound), -__FLT_MAX__);
-            return [&x, least](int e) { return x[e] >= least; };
+            const float least = fmaxf(of_ordered(bound), -__FLT_MAX__);
+            return [logit, least](int e) { return logit(e) >= least; };
         },
-        [&](int e) { return x[e] > -__builtin_inff() ? (uint64_t)ordered(x[e] + 0.0f) << 32 | (uint32_t)~token(e) : (uint64_t)0; },
+        [&](int e) {
+            const float v = logit(e);
+            return v > -__builtin_inff() ? (uint64_t)ordered(v + 0.0f) << 32 | (uint32_t)~token(e) : (uint64_t)0;
+        },
         [&](int i, uint64_t k) { to[i] = k; });
     if (t == 0) {
-        const float all = (wave_f[1][0] + wave_f[1][1]) + (wave_f[1][2] + wave_f[1][3]);
-        piece[blockIdx.x] = {top, top < __builtin_inff() ? all : __builtin_nanf("")};
+        const float total = (wave_f[1][0] + wave_f[1][1]) + (wave_f[1][2] + wave_f[1][3]);
+        piece[blockIdx.x] = {top, top < __builtin_inff() ? total : __builtin_nanf("")};
     }
 }
 
@@ -289,7 +323,7 @@ __global__ __launch_bounds__(kThreads) void beam_join_kernel(SelectArgs a, int p
 // Logits of a piece for each of its 256 threads: as many as still give the device enough workgroups.
 int piece_values(int64_t rows, int32_t vocab)
 {
-    int e = 64;
+    int e = 32;
     while (e > 8 && rows * ((vocab + kThreads * e - 1) / (kThreads * e)) < 4 * compute_units()) e /= 2;
     return e;
 }
@@ -301,12 +335,12 @@ void launch_pieces(const SelectArgs &a, int e, int pieces, uint64_t *best, Piece
 {
     const int grid = a.batch * a.beams * pieces;
     const Divisor d = divisor((uint32_t)pieces);
-    switch (e) {
-        case 8: beam_pieces_kernel<TYPE, 8><<<grid, kThreads, 0, stream>>>(a, pieces, d, best, piece); break;
-        case 16: beam_pieces_kernel<TYPE, 16><<<grid, kThreads, 0, stream>>>(a, pieces, d, best, piece); break;
-        case 32: beam_pieces_kernel<TYPE, 32><<<grid, kThreads, 0, stream>>>(a, pieces, d, best, piece); break;
-        default: beam_pieces_kernel<TYPE, 64><<<grid, kThreads, 0, stream>>>(a, pieces, d, best, piece); break;
-    }
+    if (e == 8)
+        beam_pieces_kernel<TYPE, 8><<<grid, kThreads, 0, stream>>>(a, pieces, d, best, piece);
+    else if (e == 16)
+        beam_pieces_kernel<TYPE, 16><<<grid, kThreads, 0, stream>>>(a, pieces, d, best, piece);
+    else
+        beam_pieces_kernel<TYPE, 32><<<grid, kThreads, 0, stream>>>(a, pieces, d, best, piece);
 }
 
 // ---- the caches ----
