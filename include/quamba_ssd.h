@@ -486,7 +486,7 @@ typedef struct quamba_beam_cache_t {
  *   parents device int32 [batch, beams];  caches HOST array of n_caches structs, read before the call returns
  * A beam that stays where it is is neither read (but by others) nor written.  An index outside 0 .. beams - 1 leaves its
  * beam as it is.  Caches must not overlap.  batch = 0, no caches, or caches of 0 bytes: nothing is done for them.
- * Errors: ENULL, ESHAPE (negative sizes, no beams, beams > 64, more than 2^34 bytes of a beam), EHIP.
+ * Errors: ENULL, ESHAPE (negative sizes, no beams, beams > 64, more than 2^33 bytes of a beam), EHIP.
  */
 int quamba_beam_reorder(int32_t batch, int32_t beams, const int32_t *parents, int32_t n_caches,
                         const quamba_beam_cache_t *caches, void *hip_stream);

@@ -364,28 +364,40 @@ struct Parents {
 };
 
 // Beams K and above: every load stands before every store.
-template <int K, int BEAMS, typename Vec>
+template <int K, int BEAMS, typename Vec, bool PAST>
 __device__ __forceinline__ void move_beams(char *base, int64_t bytes, const Parents<BEAMS> &parents, uint64_t &moved)
 {
     Vec v;
-    if (moved >> K & 1) v = *reinterpret_cast<const Vec *>(base + parents[K] * bytes);
+    if (moved >> K & 1) {
+        const Vec *from = reinterpret_cast<const Vec *>(base + parents[K] * bytes);
+        v = PAST ? __builtin_nontemporal_load(from) : *from;
+    }
     if constexpr (K + 1 < BEAMS)
-        move_beams<K + 1, BEAMS, Vec>(base, bytes, parents, moved);
+        move_beams<K + 1, BEAMS, Vec, PAST>(base, bytes, parents, moved);
     else  // the same conditions again, but not to the compiler, which would make a path of its own for each set of beams
         asm volatile("" : "+s"(moved));
-    if (moved >> K & 1) *reinterpret_cast<Vec *>(base + K * bytes) = v;
+    if (moved >> K & 1) {
+        Vec *to = reinterpret_cast<Vec *>(base + K * bytes);
+        if (PAST)
+            __builtin_nontemporal_store(v, to);
+        else
+            *to = v;
+    }
 }
 
 // A workgroup moves one slice of every beam of a sequence: all loads stand before the stores, and no other thread touches the
-// bytes, so the move is in place whatever the order of the beams.  BEAMS: at least as many as there are.
-template <int BEAMS>
-__global__ __launch_bounds__(kThreads) void beam_reorder_kernel(ReorderArgs a)
+// bytes, so the move is in place whatever the order of the beams.  BEAMS: at least as many as there are.  PAST: the bytes are not to stay in
+// a cache.  A wave to a workgroup: 4 layers of 32 x 8 beams of 8-bit states, past the caches, take 281 us so (5.85 TB/s), and 299 us in
+// workgroups of 256; through the caches 310 and 332.
+constexpr int kMovers = 64;
+template <int BEAMS, bool PAST>
+__global__ __launch_bounds__(kMovers) void beam_reorder_kernel(ReorderArgs a)
 {
     constexpr int kBytes = move_bytes(BEAMS);
     typedef uint32_t Vec __attribute__((ext_vector_type(kBytes / 4), aligned(1)));  // caches may lie at any address
     const int b = blockIdx.y;
     // lane k knows beam k's parent
-    const int lane = threadIdx.x & 63, parent = a.parents[(int64_t)b * a.beams + min(lane, a.beams - 1)];
+    const int lane = threadIdx.x, parent = a.parents[(int64_t)b * a.beams + min(lane, a.beams - 1)];
     const bool moves = lane < a.beams && (uint32_t)parent < (uint32_t)a.beams && parent != lane;
     uint64_t moved = __builtin_amdgcn_ballot_w64(moves);
     // read here, where every lane is active: a lane's registers are not its own any more behind a branch that it does not take
@@ -396,24 +408,27 @@ __global__ __launch_bounds__(kThreads) void beam_reorder_kernel(ReorderArgs a)
         parents.four[k / 4] = k % 4 ? parents.four[k / 4] | p << k % 4 * 8 : p;
     }
     const int c = __builtin_popcountll(__builtin_amdgcn_ballot_w64(lane < a.n && (int)blockIdx.x >= a.first[lane])) - 1;
-    const int64_t bytes = a.cache[c].bytes, at = ((int64_t)((int)blockIdx.x - a.first[c]) * kThreads + threadIdx.x) * kBytes;
+    const int64_t bytes = a.cache[c].bytes, at = ((int64_t)((int)blockIdx.x - a.first[c]) * kMovers + threadIdx.x) * kBytes;
     if (at >= bytes) return;
     char *base = static_cast<char *>(a.cache[c].data) + (int64_t)b * a.beams * bytes + at;
     if (at + kBytes <= bytes) {
-        move_beams<0, BEAMS, Vec>(base, bytes, parents, moved);
+        move_beams<0, BEAMS, Vec, PAST>(base, bytes, parents, moved);
     } else {
 #pragma unroll 1
         for (int i = 0; at + i < bytes; ++i) {  // the last bytes one by one
             uint64_t m = moved;
-            move_beams<0, BEAMS, uint8_t>(base + i, bytes, parents, m);
+            move_beams<0, BEAMS, uint8_t, false>(base + i, bytes, parents, m);
         }
     }
 }
 
 template <int BEAMS>
-void launch_slices(const ReorderArgs &a, int slices, hipStream_t stream)
+void launch_slices(const ReorderArgs &a, int slices, bool past, hipStream_t stream)
 {
-    beam_reorder_kernel<BEAMS><<<dim3(slices, a.batch), kThreads, 0, stream>>>(a);
+    if (past)
+        beam_reorder_kernel<BEAMS, true><<<dim3(slices, a.batch), kMovers, 0, stream>>>(a);
+    else
+        beam_reorder_kernel<BEAMS, false><<<dim3(slices, a.batch), kMovers, 0, stream>>>(a);
 }
 
 }  // namespace
@@ -450,12 +465,17 @@ hipError_t launch_beam_select(const SelectArgs &a, void *workspace, hipStream_t 
 hipError_t launch_beam_reorder(int32_t batch, int32_t beams, const int32_t *parents, int32_t n, const quamba_beam_cache_t *caches,
                                hipStream_t stream)
 {
-    // launches of up to kCaches caches, as many slices as the longest cache has (2^24 at most), and 65535 sequences
+    // launches of up to kCaches caches, as many slices as the longest cache has (2^25 at most), and 65535 sequences
     if (beams == 1) return hipSuccess;
     const auto launch = beams <= 2 ? launch_slices<2> : beams <= 4 ? launch_slices<4> : beams <= 8 ? launch_slices<8>
                       : beams <= 16 ? launch_slices<16> : beams <= 32 ? launch_slices<32> : launch_slices<64>;
-    const int64_t slice = kThreads * (beams <= 16 ? move_bytes(16) : beams <= 32 ? move_bytes(32) : move_bytes(64));
+    const int64_t slice = kMovers * (beams <= 16 ? move_bytes(16) : beams <= 32 ? move_bytes(32) : move_bytes(64));
     const int64_t most = kMaxCacheBytes / slice;
+    // What fits the last cache (256 MiB) is left there for the step that reads the states next: 24 layers of 4 beams, 75 MB, take 15.0 us,
+    // past the caches 17.0.
+    double bytes = 0.0;
+    for (int32_t i = 0; i < n; ++i) bytes += (double)caches[i].bytes * beams * batch;
+    const bool past = bytes > 256.0 * 1024 * 1024;
     for (int32_t s0 = 0; s0 < batch; s0 += kMaxGridY) {
         const int sequences = std::min(batch - s0, kMaxGridY);
         ReorderArgs a;
@@ -465,7 +485,7 @@ hipError_t launch_beam_reorder(int32_t batch, int32_t beams, const int32_t *pare
         a.n = 0;
         int64_t slices = 0;
         auto flush = [&] {
-            if (a.n) launch(a, (int)slices, stream);
+            if (a.n) launch(a, (int)slices, past, stream);
             a.n = 0;
             slices = 0;
             return hipGetLastError();

@@ -421,7 +421,7 @@ hipError_t launch_fp8_matmul(const MatmulArgs &a, void *workspace, hipStream_t s
 // ---- beams ----
 constexpr int kMaxBeams = 64;
 constexpr int kMaxChoices = 128;
-constexpr int64_t kMaxCacheBytes = (int64_t)1 << 34;  // of a beam
+constexpr int64_t kMaxCacheBytes = (int64_t)1 << 33;  // of a beam
 struct SelectArgs {
     const void *logits;
     int64_t stride;      // values from row to row
