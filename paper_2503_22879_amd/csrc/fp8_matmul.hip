@@ -350,7 +350,7 @@ __global__ __launch_bounds__(64 * WM * WN * GROUPS, GROUPS > 2 ? 4 : 2) void fp8
 {
     constexpr int kWaves = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
     constexpr int kRows = BM + BN, kScales = kRows * kBlock, kStage = kScales + BM * 4, kTurns = kRows / 8 / kWaves;
-    static_assert(kTurns * 8 * kWaves == kRows && kTurns % 2 == 0 && BM % 64 == 0 && BM / 64 <= kWaves && kBlock % (BN / WN) == 0, "");
+    static_assert(kTurns * 8 * kWaves == kRows && kTurns % 2 == 0 && BM / 8 % kWaves == 0 && BM % 64 == 0 && BM / 64 <= kWaves && kBlock % (BN / WN) == 0, "");
     static_assert((GROUPS - 1) * BM * BN * 4 <= GROUPS * STAGES * kStage, "");
     extern __shared__ __align__(16) char all_lds[];
     const int lane = threadIdx.x & 63, r = lane & 15, part = lane >> 4, any_wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -378,29 +378,33 @@ __global__ __launch_bounds__(64 * WM * WN * GROUPS, GROUPS > 2 ? 4 : 2) void fp8
         return is_x(turn) ? row >> 1 & 7 : (row >> 1 & 1) | (row / (4 * TN) & 3) << 1;
     };
     auto piece_of = [&](int turn) { return (lane & 7) ^ order(turn); };
-    uint32_t offset[DIRECT ? kTurns : 1], scale_offset = 0;
-    if (DIRECT) {
-#pragma unroll
-        for (int t = 0; t < kTurns; ++t)
-            offset[t] = is_x(t) ? (uint32_t)min(row_of(t), last_x) * (uint32_t)a.x_stride + piece_of(t) * 16
-                                : (uint32_t)min(row_of(t) - BM, last_w) * (uint32_t)a.w_stride + piece_of(t) * 16;
-        scale_offset = (uint32_t)min(wave % (BM / 64) * 64 + lane, last_x) * (uint32_t)a.blocks * 4;
-    }
+    // A lane's place in the first rows of x or w that its wave takes in turn: the others are as many rows on.
+    auto first_offset = [&](int turn, int64_t stride) { return (uint32_t)(wave * 8 + (lane >> 3)) * (uint32_t)stride + piece_of(turn) * 16; };
+    const uint32_t scale_offset = (uint32_t)min(wave % (BM / 64) * 64 + lane, last_x) * (uint32_t)a.blocks * 4;
+    const bool inside = last_x >= BM - 1 && last_w >= BN - 1;  // the tile lies in y
     const uint32_t base = lds_address(lds);
-    // DIRECT: a half of block b (2: all of it) on its way into a stage; the pieces behind the depth repeat the last one.  Every wave
-    // issues as many loads as the others (the scales more than once).
+    // DIRECT: a half of block b (2: all of it) on its way into a stage.  Every wave issues as many loads as the others (the scales more
+    // than once).
     auto start = [&](int b, int stage, int half) {
         const uint32_t to = base + stage * kStage;
         const uint8_t *x = xb + (int64_t)b * kBlock, *w = wb + (int64_t)b * kBlock;
-        if (b < whole) {
+        if (b < whole && inside) {
 #pragma unroll
             for (int t = 0; t < kTurns; ++t)
-                if (half == 2 || half == t / (kTurns / 2)) load_to_lds16(is_x(t) ? x : w, offset[t], to + (t * kWaves + wave) * 1024);
-        } else {
+                if (half == 2 || half == t / (kTurns / 2)) {
+                    const int on = (is_x(t) ? t : t - BM / 8 / kWaves) * kWaves * 8;
+                    load_to_lds16(is_x(t) ? x + on * a.x_stride : w + on * a.w_stride, first_offset(t, is_x(t) ? a.x_stride : a.w_stride),
+                                  to + (t * kWaves + wave) * 1024);
+                }
+        } else {  // rows over the edge repeat the last one, pieces behind the depth too
+            const int most = b < whole ? 7 : last_piece;
 #pragma unroll
             for (int t = 0; t < kTurns; ++t)
                 if (half == 2 || half == t / (kTurns / 2))
-                    load_to_lds16(is_x(t) ? x : w, offset[t] - max(piece_of(t) - last_piece, 0) * 16, to + (t * kWaves + wave) * 1024);
+                    load_to_lds16(is_x(t) ? x : w,
+                                  (is_x(t) ? (uint32_t)min(row_of(t), last_x) * (uint32_t)a.x_stride
+                                           : (uint32_t)min(row_of(t) - BM, last_w) * (uint32_t)a.w_stride) + min(piece_of(t), most) * 16,
+                                  to + (t * kWaves + wave) * 1024);
         }
         if (half != 1) load_to_lds4(xsb + b, scale_offset, to + kScales + wave % (BM / 64) * 256);
     };
@@ -599,18 +603,14 @@ hipError_t launch_rows(const MatmulArgs &a, bool direct, hipStream_t stream)
 // Up to 16 rows rings of rows are bound by memory and always taken.
 Fp8Plan fp8_matmul_plan(int32_t m, int32_t n, int32_t blocks, bool workspace)
 {
-    if (m <= 16) return {Fp8Form::rows, 1};
+    if (m <= 16) return {Fp8Form::rows, 1, 0.0};
     const int units = compute_units();
     auto tiles = [&](int rows, int columns) { return ((int64_t)m + rows - 1) / rows * (((int64_t)n + columns - 1) / columns); };
     auto rounds = [&](int64_t workgroups) { return (double)((workgroups + units - 1) / units); };
     auto pairs = [&](int splits) { return (blocks + 2 * splits - 1) / (2 * splits); };
-    Fp8Plan best{Fp8Form::tiles256, 1};
-    double least = 1.0 + rounds(tiles(256, 256)) * (10.0 + 3.35 * blocks);
+    Fp8Plan best{Fp8Form::tiles256, 1, 1.0 + rounds(tiles(256, 256)) * (10.0 + 3.35 * blocks)};
     auto offer = [&](Fp8Form form, int splits, double time) {
-        if (time < least) {
-            best = {form, splits};
-            least = time;
-        }
+        if (time < best.us) best = {form, splits, time};
     };
     const int64_t t128 = tiles(128, 128);
     // a unit's second workgroup fills the gaps of the first, and a last round that is half empty is half as long
@@ -634,6 +634,25 @@ hipError_t launch_part(const MatmulArgs &a, void *workspace, hipStream_t stream)
     auto aligned = [](const uint8_t *p, int64_t stride) { return (reinterpret_cast<uintptr_t>(p) | (uint64_t)stride) % 16 == 0 && stride < 1 << 24; };
     const bool direct = aligned(a.x, a.x_stride) && aligned(a.w, a.w_stride) && a.k % 16 == 0;
     const Fp8Plan plan = fp8_matmul_plan(a.m, a.n, a.blocks, workspace);
+    if (plan.form == Fp8Form::tiles256 && direct) {
+        // A last round with few tiles takes as long as a full one: the rows that make whole rounds, and then the others in a form of
+        // their own where that is estimated to be shorter (16384 x 18560 x 4096: 18.25 rounds).
+        const int64_t tiles_m = (a.m + 255) / 256, tiles_n = (a.n + 255) / 256, units = compute_units();
+        const int64_t rows = tiles_m * tiles_n / units * units / tiles_n * 256;
+        if (rows > 0 && rows < a.m) {
+            const double first = fp8_matmul_plan((int32_t)rows, a.n, a.blocks, false).us, then = fp8_matmul_plan(a.m - (int32_t)rows, a.n, a.blocks, false).us;
+            if (first + then < plan.us) {
+                MatmulArgs top = a, rest = a;
+                top.m = (int32_t)rows;
+                rest.m = a.m - (int32_t)rows;
+                rest.x = a.x + rows * a.x_stride;
+                rest.x_scales = a.x_scales + rows * a.blocks;
+                rest.y = static_cast<char *>(a.y) + rows * a.y_stride * (a.y_type == QUAMBA_F32 ? 4 : 2);
+                const hipError_t e = launch_tiles<256, 256, 2, 4, 1, 2, true>(top, 1, nullptr, stream);
+                return e == hipSuccess ? launch_part(rest, nullptr, stream) : e;
+            }
+        }
+    }
     float *partial = static_cast<float *>(workspace);
     if (plan.form == Fp8Form::rows)
         return a.m <= 16 ? launch_rows<1>(a, direct, stream) : a.m <= 32 ? launch_rows<2>(a, direct, stream) : launch_rows<4>(a, direct, stream);

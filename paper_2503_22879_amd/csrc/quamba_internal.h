@@ -408,11 +408,12 @@ struct MatmulArgs {
     int32_t blocks;      // of the depth
     int32_t y_type;
 };
-// How a product is made, and in how many parts of the depth.
+// How a product is made, in how many parts of the depth, and how long that may take.
 enum class Fp8Form : int { rows, tiles64, tiles64x128, tiles128_one, tiles128_two, tiles256 };
 struct Fp8Plan {
     Fp8Form form;
     int splits;
+    double us;  // estimated; 0 up to 16 rows
 };
 Fp8Plan fp8_matmul_plan(int32_t m, int32_t n, int32_t blocks, bool workspace);
 size_t fp8_matmul_workspace_bytes(int32_t m, int32_t n, int32_t k);

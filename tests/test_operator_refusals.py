@@ -53,7 +53,7 @@ def test_every_form_of_the_product_has_a_size_that_is_tested():
     from test_gpu_fp8 import FORMS
 
     class Plan(C.Structure):
-        _fields_ = [("form", C.c_int), ("splits", C.c_int)]
+        _fields_ = [("form", C.c_int), ("splits", C.c_int), ("us", C.c_double)]
     plan = getattr(q.load_library(), "_ZN6quamba15fp8_matmul_planEiiib")      # library-internal
     plan.restype, plan.argtypes = Plan, [C.c_int32] * 3 + [C.c_bool]
     for form, sizes in enumerate(FORMS.values()):
