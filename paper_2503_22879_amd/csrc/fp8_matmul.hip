@@ -79,6 +79,12 @@ __device__ __forceinline__ void store(void *y, int type, int64_t at, float v)
         static_cast<__bf16 *>(y)[at] = (__bf16)v;
 }
 
+template <int TYPE>
+__device__ __forceinline__ uint16_t half_bits(float v)
+{
+    return TYPE == QUAMBA_F16 ? f32_to_f16_bits(v) : __builtin_bit_cast(uint16_t, (__bf16)v);
+}
+
 // N adjacent values of a row at `at`, of which the first `left` belong to it.
 template <int TYPE, int N>
 __device__ __forceinline__ void store_row(void *y, int64_t at, const float (&v)[N], int left)
@@ -97,7 +103,7 @@ __device__ __forceinline__ void store_row(void *y, int64_t at, const float (&v)[
         uint16_t *p = static_cast<uint16_t *>(y) + at;
         uint16_t h[N];
 #pragma unroll
-        for (int i = 0; i < N; ++i) h[i] = TYPE == QUAMBA_F16 ? f32_to_f16_bits(v[i]) : __builtin_bit_cast(uint16_t, (__bf16)v[i]);
+        for (int i = 0; i < N; ++i) h[i] = half_bits<TYPE>(v[i]);
         if (left >= N) {
 #pragma unroll
             for (int i = 0; i < N; i += 8) __builtin_memcpy(p + i, &h[i], N < 8 ? 2 * N : 16);
@@ -351,7 +357,7 @@ __global__ __launch_bounds__(64 * WM * WN * GROUPS, GROUPS > 2 ? 4 : 2) void fp8
     constexpr int kWaves = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
     constexpr int kRows = BM + BN, kScales = kRows * kBlock, kStage = kScales + BM * 4, kTurns = kRows / 8 / kWaves;
     static_assert(kTurns * 8 * kWaves == kRows && kTurns % 2 == 0 && BM / 8 % kWaves == 0 && BM % 64 == 0 && BM / 64 <= kWaves && kBlock % (BN / WN) == 0, "");
-    static_assert((GROUPS - 1) * BM * BN * 4 <= GROUPS * STAGES * kStage, "");
+    static_assert((GROUPS - 1) * BM * BN * 4 + kWaves * 16 * (64 * TN + 16) <= GROUPS * STAGES * kStage, "");
     extern __shared__ __align__(16) char all_lds[];
     const int lane = threadIdx.x & 63, r = lane & 15, part = lane >> 4, any_wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int group = any_wave / kWaves, wave = any_wave % kWaves, thread = wave * 64 + lane;
@@ -505,15 +511,44 @@ __global__ __launch_bounds__(64 * WM * WN * GROUPS, GROUPS > 2 ? 4 : 2) void fp8
 #pragma unroll
             for (int i = 0; i < TM * TN * 4; ++i) sum[i / 4 / TN][i / 4 % TN][i % 4] += sums[(g - 1) * BM * BN + i * 64];
     }
+    // A lane has 4 TN adjacent columns of a row and its neighbours have other rows, so 16 rows at a time pass through LDS, from where
+    // lanes take 16 bytes side by side (rows padded by 16 bytes: writes and reads spread over the banks).
+    if (GROUPS == 1) __syncthreads();
+    char *turn = all_lds + (GROUPS - 1) * BM * BN * 4 + wave * 16 * (64 * TN + 16);
     auto write = [&](auto type, void *y, int64_t stride) {
-        const int col = n0 + wn * (BN / WN) + part * 4 * TN;
+        constexpr int kType = decltype(type)::value, kBytes = kType == QUAMBA_F32 ? 4 : 2, kVec = 16 / kBytes;
+        constexpr int kRow = 16 * TN * kBytes + 16, kLanes = 16 * TN * kBytes / 16;  // bytes of a row in LDS, lanes to it
+        const int col = n0 + wn * (BN / WN) + lane % kLanes * kVec;
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
-            const int row = m0 + wm * (BM / WM) + i * 16 + r;
-            float v[4 * TN];
+            uint32_t v[TN * kBytes];
 #pragma unroll
-            for (int j = 0; j < 4 * TN; ++j) v[j] = sum[i][j / 4][j % 4];
-            if (row < a.m) store_row<decltype(type)::value>(y, row * stride + col, v, a.n - col);
+            for (int j = 0; j < TN * kBytes; ++j) {
+                const int at = kBytes == 4 ? j : 2 * j;  // of the lane's columns
+                const float lo = sum[i][at / 4][at % 4], hi = kBytes == 4 ? 0.0f : sum[i][at / 4][(at + 1) % 4];
+                v[j] = kBytes == 4 ? __builtin_bit_cast(uint32_t, lo) : (uint32_t)half_bits<kType>(lo) | (uint32_t)half_bits<kType>(hi) << 16;
+            }
+#pragma unroll
+            for (int j = 0; j < TN * kBytes / 4; ++j)
+                *reinterpret_cast<int4v *>(turn + r * kRow + part * 4 * TN * kBytes + j * 16) = int4v{(int)v[4 * j], (int)v[4 * j + 1], (int)v[4 * j + 2], (int)v[4 * j + 3]};
+#pragma unroll
+            for (int q = 0; q < kLanes / 4; ++q) {
+                const int in = q * (64 / kLanes) + lane / kLanes, row = m0 + wm * (BM / WM) + i * 16 + in;
+                const int4v w = *reinterpret_cast<const int4v *>(turn + in * kRow + lane % kLanes * 16);
+                char *to = static_cast<char *>(y) + (row * stride + col) * kBytes;
+                if (row < a.m && col + kVec <= a.n) {
+                    __builtin_memcpy(to, &w, 16);
+                } else if (row < a.m) {
+#pragma unroll
+                    for (int e = 0; e < kVec; ++e)
+                        if (col + e < a.n) {
+                            if (kBytes == 4)
+                                reinterpret_cast<int *>(to)[e] = w[e];
+                            else
+                                reinterpret_cast<uint16_t *>(to)[e] = (uint16_t)((uint32_t)w[e / 2] >> e % 2 * 16);
+                        }
+                }
+            }
         }
     };
     if (splits > 1)
