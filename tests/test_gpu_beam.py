@@ -83,6 +83,25 @@ def test_select_large_batch(gpu_lib, kind):
     _check(gpu_lib, _logits(b, K, V, kind, 3), -5 - np.abs(r.standard_normal((b, K)) * 3), fin.astype(bool), pad=V - 1, count=8)
 
 
+@pytest.mark.parametrize("kind", ["fp32", "bf16"])
+@pytest.mark.parametrize("count", [1, 8, 128])
+def test_select_from_rows_in_order(gpu_lib, count, kind):
+    """Many rows, each in few long pieces: rising logits (every piece better than all before it), falling ones, few different ones,
+    one, and rows whose first piece is forbidden or that hold their best, or all that is allowed, at one end."""
+    import torch
+    b, V = 1024, 17003
+    x = _logits(b, 1, V, kind, 21)
+    x[::8] = x[::8].sort(dim=-1).values
+    x[1::8] = x[1::8].sort(dim=-1, descending=True).values
+    x[2::8] = x[2::8].round()
+    x[3::8, :, :9000] = -float("inf")
+    x[4::8, :, 12:] = -float("inf")
+    x[5::8, :, :16990] = torch.finfo(x.dtype).min
+    x[6::8] = 0.25
+    x[7::8, :, 8000:] += 30
+    _check(gpu_lib, x, np.full((b, 1), -1.0), count=count)
+
+
 @pytest.mark.parametrize("kind", TYPES)
 @pytest.mark.parametrize("V,count", [(1000, 6), (40000, 128), (2500, 65)])
 def test_select_ties(gpu_lib, V, count, kind):
