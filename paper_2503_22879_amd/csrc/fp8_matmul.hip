@@ -7,6 +7,7 @@
 // depth 13 bits below the largest of them: sums of 128 normal values are off by 1.6e-5 of themselves, and by 5e-5 where the
 // values' sizes spread, against 1e-8 here.
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "quamba_internal.h"
@@ -612,13 +613,14 @@ hipError_t launch_rows_as(const MatmulArgs &a, hipStream_t stream)
 // Waves of a workgroup for up to 64 rows: the depth in more parts where a unit has no more than one workgroup.
 int rows_waves(int32_t m, int32_t n, int32_t blocks) { return m <= 32 && (n + 15) / 16 <= compute_units() && blocks >= 16 ? 8 : 4; }
 
-template <int MF>
-hipError_t launch_rows(const MatmulArgs &a, bool direct, hipStream_t stream)
+template <int MF, bool DIRECT>
+hipError_t launch_rows(const MatmulArgs &a, hipStream_t stream)
 {
-    if (MF < 4 && rows_waves(a.m, a.n, a.blocks) == 8)
-        return direct ? launch_rows_as<MF, MF < 4 ? 8 : 4, true>(a, stream) : launch_rows_as<MF, MF < 4 ? 8 : 4, false>(a, stream);
-    return direct ? launch_rows_as<MF, 4, true>(a, stream) : launch_rows_as<MF, 4, false>(a, stream);
+    if (MF < 4 && rows_waves(a.m, a.n, a.blocks) == 8) return launch_rows_as<MF, MF < 4 ? 8 : 4, DIRECT>(a, stream);
+    return launch_rows_as<MF, 4, DIRECT>(a, stream);
 }
+
+constexpr int kMostSplits = 16;  // parts of the depth
 
 }  // namespace
 
@@ -653,11 +655,28 @@ Fp8Plan fp8_matmul_plan(int32_t m, int32_t n, int32_t blocks, bool workspace)
           t128 <= units ? 5.0 + 1.05 * blocks : 3.0 + (rounds(t128) + (double)t128 / units) / 4 * (4.9 + 1.87 * blocks));
     offer(Fp8Form::tiles128_one, 1, 1.0 + rounds(t128) * (4.2 + 1.85 * pairs(1)));
     offer(Fp8Form::tiles64x128, 1, 1.0 + rounds(tiles(64, 128)) * (3.8 + 1.17 * pairs(1)));
-    for (int s = 1; s == 1 || (workspace && s <= 16 && blocks / s >= 4); s *= 2)
+    for (int s = 1; s == 1 || (workspace && s <= kMostSplits && blocks / s >= 4); s *= 2)
         offer(Fp8Form::tiles64, s, 2.0 + rounds(tiles(64, 64) * s) * (3.0 + 0.76 * pairs(s)) + (s > 1 ? 2.5 + 1e-6 * s * m * n : 0.0));
     if (m <= 64) {
         const int64_t parts = ((int64_t)n + 15) / 16;
         offer(Fp8Form::rows, 1, 3.5 + (m <= 32 ? 0.7 : 0.95) * rounds(parts) * ((blocks - 1) / rows_waves(m, n, blocks) + 1));
+    }
+    return best;
+}
+
+// The same where rows do not lie at multiples of 16 bytes or the depth ends inside a piece, so that operands go through registers and
+// more workgroups to a unit hide their way better than more stages do.  A turn of a unit with w workgroups of 64 x 64 takes 0.25 + 0.55 w
+// us, with one of 128 x 128 1.95 and with w of them 1.65 w: 90 x 11640 x 7641 takes 57 us in 2 parts of 64 x 64 (66 in one, 118 in
+// 128 x 128), 1967 x 3304 x 3967 99 us in 128 x 128 (128 in 64 x 64), 50 x 4096 x 8191 23 us in 4 parts (34 with rings of rows).
+Fp8Plan fp8_matmul_plan_unaligned(int32_t m, int32_t n, int32_t blocks, int most_splits)
+{
+    if (m <= 16) return {Fp8Form::rows, 1, 0.0};
+    auto to_a_unit = [&](int size) { return (double)(((int64_t)m + size - 1) / size * (((int64_t)n + size - 1) / size)) / compute_units(); };
+    const double w128 = to_a_unit(128);
+    Fp8Plan best{Fp8Form::tiles128_two, 1, 3.0 + blocks * (w128 <= 1 ? 1.95 : 0.825 * (std::ceil(w128) + w128))};
+    for (int s = 1; s == 1 || (s <= most_splits && blocks / s >= 4); s *= 2) {
+        const double time = 3.0 + (blocks + s - 1) / s * (0.25 + 0.55 * std::max(1.0, to_a_unit(64) * s)) + (s > 1 ? 2.5 + 1e-6 * s * m * n : 0.0);
+        if (time < best.us) best = {Fp8Form::tiles64, s, time};
     }
     return best;
 }
@@ -669,7 +688,14 @@ hipError_t launch_part(const MatmulArgs &a, void *workspace, hipStream_t stream)
     auto aligned = [](const uint8_t *p, int64_t stride) { return (reinterpret_cast<uintptr_t>(p) | (uint64_t)stride) % 16 == 0 && stride < 1 << 24; };
     const bool direct = aligned(a.x, a.x_stride) && aligned(a.w, a.w_stride) && a.k % 16 == 0;
     const Fp8Plan plan = fp8_matmul_plan(a.m, a.n, a.blocks, workspace);
-    if (plan.form == Fp8Form::tiles256 && direct) {
+    float *partial = static_cast<float *>(workspace);
+    if (!direct) {  // the workspace has room for the splits of the depth's own plan
+        const Fp8Plan other = fp8_matmul_plan_unaligned(a.m, a.n, a.blocks, !workspace ? 1 : a.k % 16 ? kMostSplits : plan.splits);
+        if (other.form == Fp8Form::rows) return launch_rows<1, false>(a, stream);
+        if (other.form == Fp8Form::tiles64) return launch_tiles<64, 64, 2, 2, 1, 2, false>(a, other.splits, partial, stream);
+        return launch_tiles<128, 128, 2, 2, 1, 2, false>(a, 1, nullptr, stream);
+    }
+    if (plan.form == Fp8Form::tiles256) {
         // A last round with few tiles takes as long as a full one: the rows that make whole rounds, and then the others in a form of
         // their own where that is estimated to be shorter (16384 x 18560 x 4096: 18.25 rounds).
         const int64_t tiles_m = (a.m + 255) / 256, tiles_n = (a.n + 255) / 256, units = compute_units();
@@ -688,14 +714,9 @@ hipError_t launch_part(const MatmulArgs &a, void *workspace, hipStream_t stream)
             }
         }
     }
-    float *partial = static_cast<float *>(workspace);
-    if (plan.form == Fp8Form::rows)
-        return a.m <= 16 ? launch_rows<1>(a, direct, stream) : a.m <= 32 ? launch_rows<2>(a, direct, stream) : launch_rows<4>(a, direct, stream);
-    if (!direct) {
-        if (plan.form == Fp8Form::tiles64) return launch_tiles<64, 64, 2, 2, 2, 2, false>(a, plan.splits, partial, stream);
-        return launch_tiles<128, 128, 2, 2, 1, 2, false>(a, 1, nullptr, stream);
-    }
     switch (plan.form) {
+        case Fp8Form::rows:
+            return a.m <= 16 ? launch_rows<1, true>(a, stream) : a.m <= 32 ? launch_rows<2, true>(a, stream) : launch_rows<4, true>(a, stream);
         case Fp8Form::tiles64: return launch_tiles<64, 64, 2, 2, 2, 4, true>(a, plan.splits, partial, stream);
         case Fp8Form::tiles64x128: return launch_tiles<64, 128, 2, 2, 2, 3, true>(a, 1, nullptr, stream);
         case Fp8Form::tiles128_one: return launch_tiles<128, 128, 2, 2, 2, 2, true>(a, 1, nullptr, stream);
@@ -708,7 +729,8 @@ hipError_t launch_part(const MatmulArgs &a, void *workspace, hipStream_t stream)
 
 size_t fp8_matmul_workspace_bytes(int32_t m, int32_t n, int32_t k)
 {
-    const int splits = fp8_matmul_plan(m, n, (k + kBlock - 1) / kBlock, true).splits;
+    const int32_t blocks = (k + kBlock - 1) / kBlock;
+    const int splits = k % 16 ? fp8_matmul_plan_unaligned(m, n, blocks, kMostSplits).splits : fp8_matmul_plan(m, n, blocks, true).splits;
     return splits > 1 ? (size_t)splits * m * (((size_t)n + 3) / 4 * 4) * sizeof(float) : 0;
 }
 

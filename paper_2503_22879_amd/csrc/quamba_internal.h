@@ -416,6 +416,7 @@ struct Fp8Plan {
     double us;  // estimated; 0 up to 16 rows
 };
 Fp8Plan fp8_matmul_plan(int32_t m, int32_t n, int32_t blocks, bool workspace);
+Fp8Plan fp8_matmul_plan_unaligned(int32_t m, int32_t n, int32_t blocks, int most_splits);
 size_t fp8_matmul_workspace_bytes(int32_t m, int32_t n, int32_t k);
 hipError_t launch_fp8_matmul(const MatmulArgs &a, void *workspace, hipStream_t stream);
 

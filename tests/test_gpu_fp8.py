@@ -151,6 +151,27 @@ def test_matmul_of_every_form(gpu_lib, m, n, k):
             assert off.max() <= 1.0, (depth, kind, off.max(), np.argwhere(off > 1)[:5])
 
 
+UNALIGNED = {"rows": [(9, 300, 517)], "tiles64": [(20, 300, 2101), (100, 500, 4113), (333, 4001, 90)], "tiles128_two": [(2000, 2501, 401)]}
+
+
+@pytest.mark.parametrize("m,n,k", [s for sizes in UNALIGNED.values() for s in sizes])
+def test_matmul_of_unaligned_rows(gpu_lib, m, n, k):
+    """A depth that no alignment fits, and a whole number of pieces in rows at odd distances (whose workspace is that of aligned
+    rows); with the workspace and without."""
+    import torch
+    for depth, pad in ((k, 0), (k // 16 * 16, 3)):
+        ops = _operands(m, n, depth, m + depth)
+        y, top = oracle.ref_fp8_matmul(*ops)
+        x, xs, w, ws = (torch.from_numpy(a).cuda() for a in ops)
+        xb, wb = (torch.full((a.shape[0], depth + pad), 0x7f, dtype=torch.uint8, device="cuda") for a in (x, w))  # NaN between the rows
+        xb[:, :depth], wb[:, :depth] = x, w
+        size = gpu_lib.quamba_fp8_matmul_workspace_size(m, n, depth)
+        for space in [None] + [torch.full((size,), 0xff, dtype=torch.uint8, device="cuda")] * (size > 0):
+            out = torch.full((m, n), float("nan"), device="cuda")
+            gpu_lib.quamba_fp8_matmul(xb[:, :depth], xs, wb[:, :depth], ws, out, workspace=space)
+            assert (np.abs(out.double().cpu().numpy() - y) <= _bound(y, top, depth, "fp32")).all(), (depth, size)
+
+
 @pytest.mark.parametrize("m,n,k", [(1, 200, 512), (20, 200, 512), (70, 300, 640), (300, 520, 384)])
 def test_matmul_strides_and_alignment(gpu_lib, m, n, k):
     """Operands cut out of wider tensors: rows at multiples of 16 bytes, of 4 and at odd places, and of another width."""

@@ -67,6 +67,23 @@ def test_every_form_of_the_product_has_a_size_that_is_tested():
     assert plan(100, 500, 33, True).splits > 1
 
 
+def test_every_form_of_the_product_of_unaligned_rows_has_a_size_that_is_tested():
+    from test_gpu_fp8 import FORMS, UNALIGNED
+
+    class Plan(C.Structure):
+        _fields_ = [("form", C.c_int), ("splits", C.c_int), ("us", C.c_double)]
+    plan = getattr(q.load_library(), "_ZN6quamba25fp8_matmul_plan_unalignedEiiii")      # library-internal
+    plan.restype, plan.argtypes = Plan, [C.c_int32] * 4
+    for form, sizes in UNALIGNED.items():
+        for m, n, k in sizes:
+            got = plan(m, n, -(-k // 128), 16)
+            assert got.form == list(FORMS).index(form), (m, n, k, got.form)
+            size = q.quamba_fp8_matmul_workspace_size(m, n, k)
+            assert size == (got.splits * m * -(-n // 4) * 16 if got.splits > 1 and k % 16 else size)
+            assert plan(m, n, -(-k // 128), 1).splits == 1
+    assert plan(100, 500, 33, 16).splits > 1 and plan(100, 500, 33, 2).splits <= 2
+
+
 def test_select(p):
     f = q.load_library().quamba_beam_select
     size = q.quamba_beam_select_workspace_size(1, 2, 10, 4)
