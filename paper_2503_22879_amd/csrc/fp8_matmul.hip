@@ -22,19 +22,29 @@ typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 
 constexpr int kBlock = 128;
 
-// 16 codes at p, of which the first `left` belong to the row; the others count as zeros.
-__device__ __forceinline__ int4v load16(const uint8_t *p, int left)
+// 16 codes `at` of a row, of which the first `left` belong to it; the others count as zeros.  A row's end is read with the codes in front
+// of it, in one access (322 x 12227 x 90: 10.1 us, and 14.1 us byte by byte).
+__device__ __forceinline__ int4v load16(const uint8_t *row, int at, int left)
 {
-    int4v w;
-    if (left >= 16) {
-        __builtin_memcpy(&w, p, 16);
-    } else {
+    int4v w{0, 0, 0, 0};
+    if (left >= 16 || (left > 0 && at >= 16)) {
+        const int before = max(0, 16 - left);
+        __builtin_memcpy(&w, row + at - before, 16);
+        if (before) {
+            uint64_t v[2];
+            __builtin_memcpy(v, &w, 16);
+            const int bits = before % 8 * 8;
+            v[0] = before < 8 ? v[0] >> bits | v[1] << 1 << (63 - bits) : v[1] >> bits;
+            v[1] = before < 8 ? v[1] >> bits : 0;
+            __builtin_memcpy(&w, v, 16);
+        }
+    } else if (left > 0) {  // a row of fewer than 16
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             uint32_t v = 0;
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                if (4 * i + j < left) v |= (uint32_t)p[4 * i + j] << 8 * j;
+                if (4 * i + j < left) v |= (uint32_t)row[4 * i + j] << 8 * j;
             w[i] = (int)v;
         }
     }
@@ -191,11 +201,16 @@ __global__ __launch_bounds__(64 * kWaves) void fp8_matmul_rows_kernel(MatmulArgs
     int4v held[kTurns];
     float held_scale;
     auto fetch = [&](int n0, int b) {  // any block, to registers
+        auto row = [&](int t) {
+            return t < 2 ? a.w + (int64_t)min(n0 + t * 8 + (lane >> 3), a.n - 1) * a.w_stride
+                         : a.x + (int64_t)min((t - 2) * 8 + (lane >> 3), a.m - 1) * a.x_stride;
+        };
+        if (b < whole) {
 #pragma unroll
-        for (int t = 0; t < kTurns; ++t) {
-            const uint8_t *p = t < 2 ? a.w + (int64_t)min(n0 + t * 8 + (lane >> 3), a.n - 1) * a.w_stride
-                                     : a.x + (int64_t)min((t - 2) * 8 + (lane >> 3), a.m - 1) * a.x_stride;
-            held[t] = load16(p + (int64_t)b * kBlock + piece_of(t) * 16, a.k - b * kBlock - piece_of(t) * 16);
+            for (int t = 0; t < kTurns; ++t) __builtin_memcpy(&held[t], row(t) + (int64_t)b * kBlock + piece_of(t) * 16, 16);
+        } else {
+#pragma unroll
+            for (int t = 0; t < kTurns; ++t) held[t] = load16(row(t), b * kBlock + piece_of(t) * 16, a.k - b * kBlock - piece_of(t) * 16);
         }
         held_scale = a.x_scales[(int64_t)min(lane, a.m - 1) * a.blocks + b];
     };
@@ -418,10 +433,14 @@ __global__ __launch_bounds__(64 * WM * WN * GROUPS, GROUPS > 2 ? 4 : 2) void fp8
     int4v held[DIRECT ? 1 : kTurns];
     float held_scale = 0.0f;
     auto fetch = [&](int b) {  // any block, to registers
+        constexpr int kHeld = DIRECT ? 1 : kTurns;
+        auto row = [&](int t) { return is_x(t) ? xb + (int64_t)min(row_of(t), last_x) * a.x_stride : wb + (int64_t)min(row_of(t) - BM, last_w) * a.w_stride; };
+        if (b < whole) {
 #pragma unroll
-        for (int t = 0; t < (DIRECT ? 1 : kTurns); ++t) {
-            const uint8_t *p = is_x(t) ? xb + (int64_t)min(row_of(t), last_x) * a.x_stride : wb + (int64_t)min(row_of(t) - BM, last_w) * a.w_stride;
-            held[t] = load16(p + (int64_t)b * kBlock + piece_of(t) * 16, a.k - b * kBlock - piece_of(t) * 16);
+            for (int t = 0; t < kHeld; ++t) __builtin_memcpy(&held[t], row(t) + (int64_t)b * kBlock + piece_of(t) * 16, 16);
+        } else {
+#pragma unroll
+            for (int t = 0; t < kHeld; ++t) held[t] = load16(row(t), b * kBlock + piece_of(t) * 16, a.k - b * kBlock - piece_of(t) * 16);
         }
         if (thread < BM) held_scale = xsb[(int64_t)min(thread, last_x) * a.blocks + b];
     };
@@ -635,7 +654,7 @@ constexpr int kMostSplits = 16;  // parts of the depth
 //   128 x 128, two groups, one workgroup
 //     to a unit                          4.2    1.85   1000 x 4096 x 8192          66      two to a unit       77
 //   128 x 128, one group, two to a unit  4.9    1.87   8192 x 3352 x 768           56      256 x 256           63
-//   256 x 256                            10     3.35   16384 x 18560 x 4096        2110    128 x 128           2230
+//   256 x 256                            10     3.35   16384 x 18560 x 4096        2050    128 x 128           2200
 //
 // Up to 16 rows rings of rows are bound by memory and always taken.
 Fp8Plan fp8_matmul_plan(int32_t m, int32_t n, int32_t blocks, bool workspace)
@@ -666,8 +685,8 @@ Fp8Plan fp8_matmul_plan(int32_t m, int32_t n, int32_t blocks, bool workspace)
 
 // The same where rows do not lie at multiples of 16 bytes or the depth ends inside a piece, so that operands go through registers and
 // more workgroups to a unit hide their way better than more stages do.  A turn of a unit with w workgroups of 64 x 64 takes 0.25 + 0.55 w
-// us, with one of 128 x 128 1.95 and with w of them 1.65 w: 90 x 11640 x 7641 takes 57 us in 2 parts of 64 x 64 (66 in one, 118 in
-// 128 x 128), 1967 x 3304 x 3967 99 us in 128 x 128 (128 in 64 x 64), 50 x 4096 x 8191 23 us in 4 parts (34 with rings of rows).
+// us, with one of 128 x 128 1.95 and with w of them 1.65 w: 90 x 11640 x 7641 takes 65 us in 64 x 64 (118 in
+// 128 x 128), 1967 x 3304 x 3967 86 us in 128 x 128 (128 in 64 x 64), 50 x 4096 x 8191 18 us in 4 parts (34 with rings of rows).
 Fp8Plan fp8_matmul_plan_unaligned(int32_t m, int32_t n, int32_t blocks, int most_splits)
 {
     if (m <= 16) return {Fp8Form::rows, 1, 0.0};
