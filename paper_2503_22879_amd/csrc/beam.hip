@@ -16,6 +16,7 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kGathered = 1024;  // candidates that are ranked against each other
+constexpr int kJoined = 2048;    // candidates of a round of the second launch
 
 // Floats as whole numbers of the same order; 0 is below all (the place of what is no candidate).
 __device__ __forceinline__ uint32_t ordered(float v)
@@ -243,21 +244,33 @@ __device__ __forceinline__ float row_max(float v)  // of 16 lanes
     return row_step_max<0x140>(row_step_max<0x141>(row_step_max<0x4E>(row_step_max<0xB1>(v))));
 }
 
-// A workgroup to a sequence: 16 lanes join a beam's pieces, then all take the best of the pieces' best.
-__global__ __launch_bounds__(kThreads) void beam_join_kernel(SelectArgs a, int pieces, Divisor by_beam, const uint64_t *best,
-                                                             const Piece *piece)
+// A workgroup to a sequence: 16 lanes join a beam's pieces, then all take the best of the pieces' best.  These are gone through place by
+// place, the first ones of all pieces, then the second ones: each piece's fall, so there are no better ones left once a place of every
+// piece brought none, mostly after the first round (1 sequence of 16 beams, 200000 logits each, 32 choices: 112 us in the order of the
+// pieces with pieces of 2048 logits, 19 so with 8192).  Where one round holds them all, they are taken as they lie.
+__global__ __launch_bounds__(kThreads) void beam_join_kernel(SelectArgs a, int pieces, int places, int lists, int per_beam, Divisor by_place,
+                                                             Divisor by_beam, const uint64_t *best, const Piece *piece)
 {
-    constexpr int E = 8;
+    constexpr int E = kJoined / kThreads;
     __shared__ Chooser chooser;
     __shared__ float score[kMaxBeams], row_top[kMaxBeams], row_log[kMaxBeams];
     __shared__ uint8_t kind[kMaxBeams];  // 0: offers nothing, 1: its pieces' tokens, 2: finished
     __shared__ uint64_t list[kMaxChoices];
     const int t = threadIdx.x, b = blockIdx.x;
-    const int per_beam = pieces * a.count, all = a.beams * per_beam;
+    const int all = lists * places;
     const uint64_t *candidates = best + (int64_t)b * all;
+    auto candidate = [&](int i) {
+        const int place = quotient(i, by_place);
+        return candidates[(i - place * lists) * places + place];
+    };
     uint64_t c[E];
+    if (places == 1) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) c[e] = candidates[min(e * kThreads + t, all - 1)];
+        for (int e = 0; e < E; ++e) c[e] = candidates[min(e * kThreads + t, all - 1)];
+    } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) c[e] = candidate(min(e * kThreads + t, all - 1));
+    }
     for (int k = t / 16; k < a.beams; k += kThreads / 16) {
         const int row = b * a.beams + k;
         const Piece *p = piece + (int64_t)row * pieces;
@@ -277,7 +290,8 @@ __global__ __launch_bounds__(kThreads) void beam_join_kernel(SelectArgs a, int p
     }
     for (int i = t; i < kMaxChoices; i += kThreads) list[i] = 0;
     __syncthreads();
-    for (int first = 0; first < all; first += kThreads * E) {
+    int quiet = 0;  // candidates since the last one that was among the best
+    for (int first = 0; first < all && quiet < lists; first += kThreads * E) {
         uint64_t key[E + 1];
         uint32_t top = 0;
 #pragma unroll
@@ -285,7 +299,7 @@ __global__ __launch_bounds__(kThreads) void beam_join_kernel(SelectArgs a, int p
             key[e] = 0;
             const int i = first + e * kThreads + t;
             if (i < all) {
-                const int k = quotient(i, by_beam);
+                const int from = places == 1 ? i : i - quotient(i, by_place) * lists, k = quotient(from, by_beam);
                 uint32_t token = ~(uint32_t)c[e];
                 float v = -__builtin_inff();
                 if (kind[k] == 1) {
@@ -297,10 +311,15 @@ __global__ __launch_bounds__(kThreads) void beam_join_kernel(SelectArgs a, int p
                 if (v > -__builtin_inff())
                     key[e] = (uint64_t)ordered(v + 0.0f) << 32 | ~((uint32_t)k * (uint32_t)a.vocab + token);
                 const int64_t next = (int64_t)i + kThreads * E;
-                if (next < all) c[e] = candidates[next];
+                if (next < all) c[e] = candidate((int)next);
             }
             top = max(top, (uint32_t)(key[e] >> 32));
         }
+        if (first && !__syncthreads_or(top >= max((uint32_t)(list[a.count - 1] >> 32), 1u))) {
+            quiet += kThreads * E;
+            continue;
+        }
+        quiet = 0;
         key[E] = t < kMaxChoices ? list[t] : 0;
         top = max(top, (uint32_t)(key[E] >> 32));
         __syncthreads();
@@ -320,12 +339,11 @@ __global__ __launch_bounds__(kThreads) void beam_join_kernel(SelectArgs a, int p
     }
 }
 
-// Logits of a piece for each of its 256 threads: as many as still give the device enough workgroups.
+// Logits of a piece for each of its 256 threads: 16 where 32 leave most of the device without a piece (1 x 4 beams of 50021: 9.1 us with 16,
+// 10.0 with 32; 8 x 8 of 50021: 12.2 and 11.9; 32 x 8 of 128000: 39.2 and 38.0; pieces of 8 gain nothing on small ones).
 int piece_values(int64_t rows, int32_t vocab)
 {
-    int e = 32;
-    while (e > 8 && rows * ((vocab + kThreads * e - 1) / (kThreads * e)) < 4 * compute_units()) e /= 2;
-    return e;
+    return rows * ((vocab + kThreads * 32 - 1) / (kThreads * 32)) < compute_units() / 2 ? 16 : 32;
 }
 
 int64_t piece_count(int32_t vocab, int e) { return ((int64_t)vocab + kThreads * e - 1) / (kThreads * e); }
@@ -335,9 +353,7 @@ void launch_pieces(const SelectArgs &a, int e, int pieces, uint64_t *best, Piece
 {
     const int grid = a.batch * a.beams * pieces;
     const Divisor d = divisor((uint32_t)pieces);
-    if (e == 8)
-        beam_pieces_kernel<TYPE, 8><<<grid, kThreads, 0, stream>>>(a, pieces, d, best, piece);
-    else if (e == 16)
+    if (e == 16)
         beam_pieces_kernel<TYPE, 16><<<grid, kThreads, 0, stream>>>(a, pieces, d, best, piece);
     else
         beam_pieces_kernel<TYPE, 32><<<grid, kThreads, 0, stream>>>(a, pieces, d, best, piece);
@@ -458,7 +474,9 @@ hipError_t launch_beam_select(const SelectArgs &a, void *workspace, hipStream_t 
     }
     hipError_t err = hipGetLastError();
     if (err != hipSuccess) return err;
-    beam_join_kernel<<<a.batch, kThreads, 0, stream>>>(a, pieces, divisor((uint32_t)(pieces * a.count)), best, piece);
+    const bool one_round = a.beams * pieces * a.count <= kJoined;
+    const int places = one_round ? 1 : a.count, per_beam = one_round ? pieces * a.count : pieces, lists = a.beams * per_beam;
+    beam_join_kernel<<<a.batch, kThreads, 0, stream>>>(a, pieces, places, lists, per_beam, divisor((uint32_t)lists), divisor((uint32_t)per_beam), best, piece);
     return hipGetLastError();
 }
 

@@ -83,6 +83,27 @@ def test_select_large_batch(gpu_lib, kind):
     _check(gpu_lib, _logits(b, K, V, kind, 3), -5 - np.abs(r.standard_normal((b, K)) * 3), fin.astype(bool), pad=V - 1, count=8)
 
 
+@pytest.mark.parametrize("kind", ["fp32", "fp16"])
+@pytest.mark.parametrize("K,V,count", [(64, 30011, 128), (20, 70001, 128), (64, 264001, 3), (5, 3000, 128)])
+def test_select_of_many_candidates(gpu_lib, K, V, count, kind):
+    """Many pieces and many choices of a sequence: the best spread over all beams, all in one beam, all in one piece of one beam, and
+    finished beams among the last ones whose candidates are the best."""
+    x = _logits(1, K, V, kind, 31)
+    r = np.random.default_rng(6)
+    even = -3 - r.random((1, K))
+    _check(gpu_lib, x, even, count=count)
+    fin = np.zeros((1, K), np.uint8)
+    fin[0, K - 1] = fin[0, K // 2] = 1
+    _check(gpu_lib, x, even + 2 * fin, fin, pad=V - 1, count=count)
+    if V > 100000:
+        return
+    alone = even - 60
+    alone[0, K - 2] = -1.0
+    _check(gpu_lib, x, alone, count=count)
+    x[0, K - 2, V // 2:V // 2 + 200] += 12
+    _check(gpu_lib, x, alone, count=count)
+
+
 @pytest.mark.parametrize("kind", ["fp32", "bf16"])
 @pytest.mark.parametrize("count", [1, 8, 128])
 def test_select_from_rows_in_order(gpu_lib, count, kind):
