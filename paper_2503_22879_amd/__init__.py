@@ -1,5 +1,8 @@
 """MI355X-native 8-bit Mamba2 selective scan (the SSD hot path of Quamba2, arXiv 2503.22879).
 
+Beside the scan and the steps around it: projections in 8-bit floating point (quamba_fp8_quantize, quamba_fp8_matmul) and beam search
+(quamba_beam_select, quamba_beam_reorder); examples/beam_search.py runs them together.
+
 A thin binding over libquamba_ssd.so (C ABI in include/quamba_ssd.h).  Every step of the path runs in the
 library's HIP kernels; this package only marshals arguments.  There is no CPU fallback: calls raise if the
 library has not been built.
