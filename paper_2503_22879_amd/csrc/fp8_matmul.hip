@@ -654,7 +654,8 @@ constexpr int kMostSplits = 16;  // parts of the depth
 //   128 x 128, two groups, one workgroup
 //     to a unit                          4.2    1.85   1000 x 4096 x 8192          66      two to a unit       77
 //   128 x 128, one group, two to a unit  4.9    1.87   8192 x 3352 x 768           56      256 x 256           63
-//   256 x 256                            10     3.35   16384 x 18560 x 4096        2050    128 x 128           2200
+//   256 x 256                            9      3.35   16384 x 18560 x 4096        2050    128 x 128           2200
+//                                                      256 x 50021 x 2560          74      128 x 128           79
 //
 // Up to 16 rows rings of rows are bound by memory and always taken.
 Fp8Plan fp8_matmul_plan(int32_t m, int32_t n, int32_t blocks, bool workspace)
@@ -664,7 +665,7 @@ Fp8Plan fp8_matmul_plan(int32_t m, int32_t n, int32_t blocks, bool workspace)
     auto tiles = [&](int rows, int columns) { return ((int64_t)m + rows - 1) / rows * (((int64_t)n + columns - 1) / columns); };
     auto rounds = [&](int64_t workgroups) { return (double)((workgroups + units - 1) / units); };
     auto pairs = [&](int splits) { return (blocks + 2 * splits - 1) / (2 * splits); };
-    Fp8Plan best{Fp8Form::tiles256, 1, 1.0 + rounds(tiles(256, 256)) * (10.0 + 3.35 * blocks)};
+    Fp8Plan best{Fp8Form::tiles256, 1, 1.0 + rounds(tiles(256, 256)) * (9.0 + 3.35 * blocks)};
     auto offer = [&](Fp8Form form, int splits, double time) {
         if (time < best.us) best = {form, splits, time};
     };
