@@ -55,10 +55,10 @@ __device__ __forceinline__ int4v load16(const uint8_t *row, int at, int left)
 struct Part {
     half8 h[4];
     __device__ __forceinline__ Part() {}
-    __device__ __forceinline__ Part(const int4v &lo, const int4v &hi)
+    __device__ __forceinline__ Part(const int4v &lo, const int4v &hi, int n = 4)  // the first n of h
     {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < n; ++i) {
             int4v v;
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
@@ -72,11 +72,11 @@ struct Part {
 };
 
 // Lane l's part is row l % 16, codes 32 (l / 16) on; of the 16 x 16 sums it gets a's rows 4 (l / 16) + e against b's row l % 16.
-__device__ __forceinline__ float4v multiply(const Part &a, const Part &b)
+__device__ __forceinline__ float4v multiply(const Part &a, const Part &b, int n = 4)
 {
     float4v p{0, 0, 0, 0};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) p = __builtin_amdgcn_mfma_f32_16x16x32_f16(a.h[i], b.h[i], p, 0, 0, 0);
+    for (int i = 0; i < n; ++i) p = __builtin_amdgcn_mfma_f32_16x16x32_f16(a.h[i], b.h[i], p, 0, 0, 0);
     return p;
 }
 
@@ -459,17 +459,20 @@ __global__ __launch_bounds__(64 * WM * WN * GROUPS, GROUPS > 2 ? 4 : 2) void fp8
     const int at = r * kBlock + (part ^ r >> 1) * 16, at_w = ((r >> 2) * 4 * TN + (r & 3)) * kBlock + (part ^ r >> 1) * 16;
     // Multiplies block b; between its first parts block `next` (below 0: none) is started, in two halves: a wave waits where it
     // issues more loads than fit a queue, and after the first part's reads it has products to make meanwhile (16384 x 18560 x 4096: 2.15 -> 2.11 ms).
-    auto compute = [&](int b, int stage, int next, int next_stage, auto in_part) {
+    // codes_of_it: how many there may be in the block; parts that hold none are not multiplied.
+    auto compute = [&](int b, int stage, int next, int next_stage, auto codes_of_it) {
+        constexpr int kCodes = decltype(codes_of_it)::value, kHalves = kCodes == 64 ? 2 : 4;
         const char *x = lds + stage * kStage + wm * (BM / WM) * kBlock, *w = lds + stage * kStage + (BM + wn * (BN / WN)) * kBlock;
         const float *xs = reinterpret_cast<const float *>(lds + stage * kStage + kScales) + wm * (BM / WM) + r;
         const float wsc = ws[b];
         auto codes = [&](const char *p, int to) {
-            int4v c0 = *reinterpret_cast<const int4v *>(p + to), c1 = *reinterpret_cast<const int4v *>(p + (to ^ 64));
-            if (in_part.value) {  // what stands behind the depth counts as zeros
+            int4v c0 = *reinterpret_cast<const int4v *>(p + to), c1 = c0;
+            if (kCodes > 64) c1 = *reinterpret_cast<const int4v *>(p + (to ^ 64));
+            if (kCodes < kBlock) {  // what stands behind the depth counts as zeros
                 c0 = part <= last_piece ? c0 : int4v{0, 0, 0, 0};
                 c1 = part + 4 <= last_piece ? c1 : int4v{0, 0, 0, 0};
             }
-            return Part(c0, c1);
+            return Part(c0, c1, kHalves);
         };
         Part wf[TN];
 #pragma unroll
@@ -481,15 +484,16 @@ __global__ __launch_bounds__(64 * WM * WN * GROUPS, GROUPS > 2 ? 4 : 2) void fp8
             const float s = xs[i * 16] * wsc;
             float4v p[TN];
 #pragma unroll
-            for (int j = 0; j < TN; ++j) p[j] = multiply(wf[j], xf);
+            for (int j = 0; j < TN; ++j) p[j] = multiply(wf[j], xf, kHalves);
 #pragma unroll
             for (int j = 0; j < TN; ++j)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) sum[i][j][e] = fmaf(p[j][e], s, sum[i][j][e]);
         }
     };
-    const std::false_type all_of_it;
-    const std::true_type in_part;
+    const std::integral_constant<int, kBlock> all_of_it;
+    const std::integral_constant<int, kBlock - 16> most_of_it;  // at most
+    const std::integral_constant<int, 64> half_of_it;
 
     if (DIRECT) {
         for (int u = 0; u < STAGES - 1; ++u)
@@ -507,7 +511,10 @@ __global__ __launch_bounds__(64 * WM * WN * GROUPS, GROUPS > 2 ? 4 : 2) void fp8
         }
         for (; i < turns; ++i) {  // at most one, for the group's partial block or for the others
             wait_for_tiles<0>();
-            if (i < mine) compute(block(i), stage, -1, 0, in_part);
+            if (TM * TN < 32 && i < mine && last_piece < 4)  // (no registers for it where the sums take half of them)
+                compute(block(i), stage, -1, 0, half_of_it);
+            else if (i < mine)
+                compute(block(i), stage, -1, 0, most_of_it);
         }
     } else {
         if (mine) fetch(block(0));
@@ -641,6 +648,13 @@ hipError_t launch_rows(const MatmulArgs &a, hipStream_t stream)
 
 constexpr int kMostSplits = 16;  // parts of the depth
 
+// Tiles of 256 x 256, see below.
+double tiles256_us(int32_t m, int32_t n, int32_t blocks)
+{
+    const int64_t tiles = ((int64_t)m + 255) / 256 * (((int64_t)n + 255) / 256), units = compute_units();
+    return 1.0 + (double)((tiles + units - 1) / units) * (9.0 + 3.35 * blocks);
+}
+
 }  // namespace
 
 // The form that is estimated to be done first, from what a round of workgroups takes in us on 256 units: a fixed time and one for each
@@ -652,8 +666,9 @@ constexpr int kMostSplits = 16;  // parts of the depth
 //   64 x 64, two groups                  3      0.76   128 x 4096 x 8192, 2 parts  19.9    in one part         27
 //   64 x 128, two groups                 3.8    1.17   500 x 4096 x 4096           24      64 x 64             33
 //   128 x 128, two groups, one workgroup
-//     to a unit                          4.2    1.85   1000 x 4096 x 8192          66      two to a unit       77
-//   128 x 128, one group, two to a unit  4.9    1.87   8192 x 3352 x 768           56      256 x 256           63
+//     to a unit                          4.2    1.85   1000 x 4096 x 8192          75      two to a unit       88
+//   128 x 128, one group, two to a unit  3.5    2.0    8192 x 3352 x 768           55      256 x 256           59
+//                                                      16331 x 4559 x 320          78      256 x 256           90
 //   256 x 256                            9      3.35   16384 x 18560 x 4096        2050    128 x 128           2200
 //                                                      256 x 50021 x 2560          74      128 x 128           79
 //
@@ -665,14 +680,14 @@ Fp8Plan fp8_matmul_plan(int32_t m, int32_t n, int32_t blocks, bool workspace)
     auto tiles = [&](int rows, int columns) { return ((int64_t)m + rows - 1) / rows * (((int64_t)n + columns - 1) / columns); };
     auto rounds = [&](int64_t workgroups) { return (double)((workgroups + units - 1) / units); };
     auto pairs = [&](int splits) { return (blocks + 2 * splits - 1) / (2 * splits); };
-    Fp8Plan best{Fp8Form::tiles256, 1, 1.0 + rounds(tiles(256, 256)) * (9.0 + 3.35 * blocks)};
+    Fp8Plan best{Fp8Form::tiles256, 1, tiles256_us(m, n, blocks)};
     auto offer = [&](Fp8Form form, int splits, double time) {
         if (time < best.us) best = {form, splits, time};
     };
     const int64_t t128 = tiles(128, 128);
     // a unit's second workgroup fills the gaps of the first, and a last round that is half empty is half as long
     offer(Fp8Form::tiles128_two, 1,
-          t128 <= units ? 5.0 + 1.05 * blocks : 3.0 + (rounds(t128) + (double)t128 / units) / 4 * (4.9 + 1.87 * blocks));
+          t128 <= units ? 5.0 + 1.05 * blocks : 3.0 + (rounds(t128) + (double)t128 / units) / 4 * (3.5 + 2.0 * blocks));
     offer(Fp8Form::tiles128_one, 1, 1.0 + rounds(t128) * (4.2 + 1.85 * pairs(1)));
     offer(Fp8Form::tiles64x128, 1, 1.0 + rounds(tiles(64, 128)) * (3.8 + 1.17 * pairs(1)));
     for (int s = 1; s == 1 || (workspace && s <= kMostSplits && blocks / s >= 4); s *= 2)
@@ -715,24 +730,20 @@ hipError_t launch_part(const MatmulArgs &a, void *workspace, hipStream_t stream)
         if (other.form == Fp8Form::tiles64) return launch_tiles<64, 64, 2, 2, 1, 2, false>(a, other.splits, partial, stream);
         return launch_tiles<128, 128, 2, 2, 1, 2, false>(a, 1, nullptr, stream);
     }
-    if (plan.form == Fp8Form::tiles256) {
-        // A last round with few tiles takes as long as a full one: the rows that make whole rounds, and then the others in a form of
-        // their own where that is estimated to be shorter (16384 x 18560 x 4096: 18.25 rounds).
-        const int64_t tiles_m = (a.m + 255) / 256, tiles_n = (a.n + 255) / 256, units = compute_units();
-        const int64_t rows = tiles_m * tiles_n / units * units / tiles_n * 256;
-        if (rows > 0 && rows < a.m) {
-            const double first = fp8_matmul_plan((int32_t)rows, a.n, a.blocks, false).us, then = fp8_matmul_plan(a.m - (int32_t)rows, a.n, a.blocks, false).us;
-            if (first + then < plan.us) {
-                MatmulArgs top = a, rest = a;
-                top.m = (int32_t)rows;
-                rest.m = a.m - (int32_t)rows;
-                rest.x = a.x + rows * a.x_stride;
-                rest.x_scales = a.x_scales + rows * a.blocks;
-                rest.y = static_cast<char *>(a.y) + rows * a.y_stride * (a.y_type == QUAMBA_F32 ? 4 : 2);
-                const hipError_t e = launch_tiles<256, 256, 2, 4, 1, 2, true>(top, 1, nullptr, stream);
-                return e == hipSuccess ? launch_part(rest, nullptr, stream) : e;
-            }
-        }
+    // A last round of 256 x 256 with few tiles takes as long as a full one: the rows that make whole rounds so, and the others in a form of
+    // their own, where that is estimated to be shorter (16384 x 18560 x 4096: 18.25 rounds; 16148 x 4224 x 7488: 4.25).
+    const int64_t tiles_m = (a.m + 255) / 256, tiles_n = (a.n + 255) / 256, units = compute_units();
+    const int64_t rows = tiles_m * tiles_n / units * units / tiles_n * 256;
+    if (rows > 0 && rows < a.m &&
+        tiles256_us((int32_t)rows, a.n, a.blocks) + fp8_matmul_plan(a.m - (int32_t)rows, a.n, a.blocks, false).us < plan.us) {
+        MatmulArgs top = a, rest = a;
+        top.m = (int32_t)rows;
+        rest.m = a.m - (int32_t)rows;
+        rest.x = a.x + rows * a.x_stride;
+        rest.x_scales = a.x_scales + rows * a.blocks;
+        rest.y = static_cast<char *>(a.y) + rows * a.y_stride * (a.y_type == QUAMBA_F32 ? 4 : 2);
+        const hipError_t e = launch_tiles<256, 256, 2, 4, 1, 2, true>(top, 1, nullptr, stream);
+        return e == hipSuccess ? launch_part(rest, nullptr, stream) : e;
     }
     switch (plan.form) {
         case Fp8Form::rows:
