@@ -367,7 +367,7 @@ __device__ __forceinline__ void tile_of(int id, int tiles_m, int tiles_n, int &t
 // wait for memory and LDS where tiles are small.  `splits`: workgroups to a tile, each with a part of the depth, whose sums go to
 // `partial` [splits, m, columns].
 template <int BM, int BN, int WM, int WN, int GROUPS, int STAGES, bool DIRECT>
-__global__ __launch_bounds__(64 * WM * WN * GROUPS, GROUPS > 2 ? 4 : 2) void fp8_matmul_tile_kernel(MatmulArgs a, int tiles_m, int tiles_n, int splits, float *partial,
+__global__ __launch_bounds__(64 * WM * WN * GROUPS, 2) void fp8_matmul_tile_kernel(MatmulArgs a, int tiles_m, int tiles_n, int splits, float *partial,
                                                                           int64_t columns)
 {
     constexpr int kWaves = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
