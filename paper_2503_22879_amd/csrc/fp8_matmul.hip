@@ -357,6 +357,15 @@ __device__ __forceinline__ void tile_of(int id, int tiles_m, int tiles_n, int &t
     tm = first + in_band - tn * rows;
 }
 
+// The row of w's scales that wave `wn` of the tile at column n0 takes.  A wave's columns lie in one block of 128; one that has
+// none in y takes the last row that there is.
+template <int BN, int WN>
+__host__ __device__ __forceinline__ int32_t scale_row(int32_t n0, int wn, int32_t n)
+{
+    const int32_t column = n0 + wn * (BN / WN);
+    return (column < n ? column : n - 1) / kBlock;
+}
+
 // BM x BN outputs to a workgroup of WM x WN waves.  LDS holds STAGES blocks (128 codes deep) of BM + BN rows and the scales of x's rows;
 // blocks arrive while earlier ones are multiplied.  A lane takes pieces l / 16 and l / 16 + 4 of the 8 of 16 bytes that a row has (any
 // order along the depth will do that is the same for x and w), and piece c of row r lies at c ^ (r / 2 % 8), so that the lanes that
@@ -385,7 +394,7 @@ __global__ __launch_bounds__(64 * WM * WN * GROUPS, 2) void fp8_matmul_tile_kern
     const int m0 = tm * BM, n0 = tn * BN;
     const uint8_t *xb = a.x + (int64_t)m0 * a.x_stride, *wb = a.w + (int64_t)n0 * a.w_stride;
     const float *xsb = a.x_scales + (int64_t)m0 * a.blocks;
-    const auto *ws = (const __attribute__((address_space(4))) float *)(a.w_scales + (int64_t)((n0 + wn * (BN / WN)) / kBlock) * a.blocks);
+    const auto *ws = (const __attribute__((address_space(4))) float *)(a.w_scales + (int64_t)scale_row<BN, WN>(n0, wn, a.n) * a.blocks);
     const int last_x = a.m - 1 - m0, last_w = a.n - 1 - n0;
     const int whole = a.k / kBlock, last_piece = (a.k - whole * kBlock) / 16 - 1;  // of a last block in part
     const int first = (int)((int64_t)a.blocks * split / splits), end = (int)((int64_t)a.blocks * (split + 1) / splits);
@@ -714,6 +723,29 @@ Fp8Plan fp8_matmul_plan_unaligned(int32_t m, int32_t n, int32_t blocks, int most
         if (time < best.us) best = {Fp8Form::tiles64, s, time};
     }
     return best;
+}
+
+namespace {
+
+template <int BN, int WN>
+int32_t last_scale_row(int32_t n)
+{
+    int32_t last = 0;
+    for (int64_t n0 = 0; n0 < n; n0 += BN)
+        for (int wn = 0; wn < WN; ++wn) last = std::max(last, scale_row<BN, WN>((int32_t)n0, wn, n));
+    return last;
+}
+
+}  // namespace
+
+int32_t fp8_matmul_last_scale_row(Fp8Form form, int32_t n)
+{
+    switch (form) {
+        case Fp8Form::rows: return (n - 1) / kBlock;
+        case Fp8Form::tiles64: return last_scale_row<64, 2>(n);
+        case Fp8Form::tiles256: return last_scale_row<256, 4>(n);
+        default: return last_scale_row<128, 2>(n);
+    }
 }
 
 namespace {

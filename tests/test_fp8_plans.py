@@ -1,0 +1,38 @@
+"""What the launches of the 8-bit floating-point products read and how they are cut, by the library's own arithmetic (no GPU)."""
+import ctypes as C
+
+import pytest
+
+import paper_2503_22879_amd as q
+
+FORMS = {"rows": 0, "tiles64": 1, "tiles64x128": 2, "tiles128_one": 3, "tiles128_two": 4, "tiles256": 5}
+
+
+def _internal(name, restype, *argtypes):
+    f = getattr(q.load_library(), name)      # library-internal
+    f.restype, f.argtypes = restype, argtypes
+    return f
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_no_wave_reads_behind_the_scales_of_w(form):
+    """w's scales have ceil(n / 128) rows.  A 256 x 256 tile spans two of them: where 1 to 128 of its columns are left, the waves of its right
+    half have none of their own."""
+    last = _internal("_ZN6quamba25fp8_matmul_last_scale_rowENS_7Fp8FormEi", C.c_int32, C.c_int, C.c_int32)
+    for n in [*range(1, 1100), 3352, 10576, 18560, 50021, 50280, 151936, 2 ** 20 + 1, 2 ** 26 - 200, 2 ** 26]:
+        assert last(FORMS[form], n) == -(-n // 128) - 1, n
+
+
+class Plan(C.Structure):
+    _fields_ = [("form", C.c_int), ("splits", C.c_int), ("us", C.c_double)]
+
+
+def _plan(m, n, k, workspace=True):
+    f = _internal("_ZN6quamba15fp8_matmul_planEiiib", Plan, C.c_int32, C.c_int32, C.c_int32, C.c_bool)
+    return f(m, n, -(-k // 128), workspace)
+
+
+def test_half_filled_large_tiles_have_sizes_that_are_tested():
+    from test_gpu_fp8 import HALF_FILLED
+    for m, n, k in HALF_FILLED:
+        assert _plan(m, n, k).form == FORMS["tiles256"] and 1 <= n % 256 <= 128

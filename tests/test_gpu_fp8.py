@@ -287,3 +287,14 @@ def test_quantize_and_multiply_on_another_stream(gpu_lib):
         ops = oracle.quantize_fp8(x.float().cpu().numpy(), 1) + (wq.cpu().numpy(), ws.cpu().numpy())
         want, top = oracle.ref_fp8_matmul(*ops)
         assert (np.abs(got.double().cpu().numpy() - want) <= _bound(want, top, k, "fp32")).all()
+
+
+# 256 x 256 tiles whose last ones hold 1 to 128 columns, in one block of w's scales (test_fp8_plans.py checks the form).
+HALF_FILLED = [(3321, 4137, 640), (3840, 4200, 1296)]
+
+
+@pytest.mark.parametrize("m,n,k", HALF_FILLED)
+def test_matmul_of_half_filled_large_tiles(gpu_lib, m, n, k):
+    ops = _operands(m, n, k, m + k)
+    y, top = oracle.ref_fp8_matmul(*ops)
+    assert (np.abs(_matmul(gpu_lib, ops, "fp32", pad=5) - y) <= _bound(y, top, k, "fp32")).all()
