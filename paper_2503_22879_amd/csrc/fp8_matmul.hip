@@ -588,7 +588,7 @@ __global__ __launch_bounds__(64 * WM * WN * GROUPS, 2) void fp8_matmul_tile_kern
         }
     };
     if (splits > 1)
-        write(std::integral_constant<int, QUAMBA_F32>(), partial + split * a.m * columns, columns);
+        write(std::integral_constant<int, QUAMBA_F32>(), partial + (int64_t)split * a.m * columns, columns);
     else if (a.y_type == QUAMBA_F32)
         write(std::integral_constant<int, QUAMBA_F32>(), a.y, a.y_stride);
     else if (a.y_type == QUAMBA_F16)
@@ -597,22 +597,24 @@ __global__ __launch_bounds__(64 * WM * WN * GROUPS, 2) void fp8_matmul_tile_kern
         write(std::integral_constant<int, QUAMBA_BF16>(), a.y, a.y_stride);
 }
 
-// y of the splits' sums, in their order; 4 columns to a thread.
+// y of the splits' sums, in their order; 4 columns to a thread, every gridDim.y-th row to a workgroup.
 __global__ __launch_bounds__(256) void fp8_matmul_join_kernel(MatmulArgs a, int splits, const float *partial, int64_t columns)
 {
-    const int col = ((int)blockIdx.x * 256 + (int)threadIdx.x) * 4, row = blockIdx.y;
+    const int col = ((int)blockIdx.x * 256 + (int)threadIdx.x) * 4;
     if (col >= a.n) return;
-    const float *p = partial + row * columns + col;
-    float4v v = *reinterpret_cast<const float4v *>(p);
-    for (int s = 1; s < splits; ++s) v += *reinterpret_cast<const float4v *>(p + s * a.m * columns);
-    const float out[4] = {v[0], v[1], v[2], v[3]};
-    const int64_t to = row * a.y_stride + col;
-    if (a.y_type == QUAMBA_F32)
-        store_row<QUAMBA_F32>(a.y, to, out, a.n - col);
-    else if (a.y_type == QUAMBA_F16)
-        store_row<QUAMBA_F16>(a.y, to, out, a.n - col);
-    else
-        store_row<QUAMBA_BF16>(a.y, to, out, a.n - col);
+    for (int64_t row = blockIdx.y; row < a.m; row += gridDim.y) {
+        const float *p = partial + row * columns + col;
+        float4v v = *reinterpret_cast<const float4v *>(p);
+        for (int s = 1; s < splits; ++s) v += *reinterpret_cast<const float4v *>(p + (int64_t)s * a.m * columns);
+        const float out[4] = {v[0], v[1], v[2], v[3]};
+        const int64_t to = row * a.y_stride + col;
+        if (a.y_type == QUAMBA_F32)
+            store_row<QUAMBA_F32>(a.y, to, out, a.n - col);
+        else if (a.y_type == QUAMBA_F16)
+            store_row<QUAMBA_F16>(a.y, to, out, a.n - col);
+        else
+            store_row<QUAMBA_BF16>(a.y, to, out, a.n - col);
+    }
 }
 
 template <int BM, int BN, int WM, int WN, int GROUPS, int STAGES, bool DIRECT>
@@ -628,7 +630,7 @@ hipError_t launch_tiles(const MatmulArgs &a, int splits, float *partial, hipStre
     kernel<<<dim3(tiles_m * tiles_n, splits), 64 * WM * WN * GROUPS, kLds, stream>>>(a, tiles_m, tiles_n, splits, partial, columns);
     e = hipGetLastError();
     if (e != hipSuccess || splits == 1) return e;
-    fp8_matmul_join_kernel<<<dim3((a.n + 1023) / 1024, a.m), 256, 0, stream>>>(a, splits, partial, columns);
+    fp8_matmul_join_kernel<<<dim3((a.n + 1023) / 1024, fp8_matmul_join_rows(a.m)), 256, 0, stream>>>(a, splits, partial, columns);
     return hipGetLastError();
 }
 
@@ -747,6 +749,8 @@ int32_t fp8_matmul_last_scale_row(Fp8Form form, int32_t n)
         default: return last_scale_row<128, 2>(n);
     }
 }
+
+int32_t fp8_matmul_join_rows(int32_t m) { return std::min(m, kMaxGridY); }
 
 namespace {
 

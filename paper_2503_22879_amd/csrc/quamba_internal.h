@@ -419,6 +419,8 @@ Fp8Plan fp8_matmul_plan(int32_t m, int32_t n, int32_t blocks, bool workspace);
 Fp8Plan fp8_matmul_plan_unaligned(int32_t m, int32_t n, int32_t blocks, int most_splits);
 // The last row of w's scales that the waves of a form read, over all of its tiles.
 int32_t fp8_matmul_last_scale_row(Fp8Form form, int32_t n);
+// Rows of workgroups that join the parts of m rows' sums.
+int32_t fp8_matmul_join_rows(int32_t m);
 size_t fp8_matmul_workspace_bytes(int32_t m, int32_t n, int32_t k);
 hipError_t launch_fp8_matmul(const MatmulArgs &a, void *workspace, hipStream_t stream);
 

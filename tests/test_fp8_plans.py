@@ -36,3 +36,13 @@ def test_half_filled_large_tiles_have_sizes_that_are_tested():
     from test_gpu_fp8 import HALF_FILLED
     for m, n, k in HALF_FILLED:
         assert _plan(m, n, k).form == FORMS["tiles256"] and 1 <= n % 256 <= 128
+
+
+def test_the_parts_of_many_rows_are_joined_by_a_launch_that_fits():
+    """A launch has at most 65535 workgroups along its second axis; the sizes are planned in parts."""
+    from test_gpu_fp8 import TALL_SPLIT
+    rows = _internal("_ZN6quamba20fp8_matmul_join_rowsEi", C.c_int32, C.c_int32)
+    for m in (1, 17, 65535, 65536, 66096, 10 ** 6, 2 ** 29, 2 ** 31 - 1):
+        assert rows(m) == min(m, 65535)
+    for m, n, k in TALL_SPLIT:
+        assert m > 65535 and q.quamba_fp8_matmul_workspace_size(m, n, k) > 0

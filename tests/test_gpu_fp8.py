@@ -298,3 +298,21 @@ def test_matmul_of_half_filled_large_tiles(gpu_lib, m, n, k):
     ops = _operands(m, n, k, m + k)
     y, top = oracle.ref_fp8_matmul(*ops)
     assert (np.abs(_matmul(gpu_lib, ops, "fp32", pad=5) - y) <= _bound(y, top, k, "fp32")).all()
+
+
+# More rows than a launch has workgroups along an axis, and a depth in parts (test_fp8_plans.py checks that): aligned rows, and others.
+TALL_SPLIT = [(16 * 4131, 3, 10240), (16 * 4131, 3, 5117)]
+
+
+@pytest.mark.parametrize("m,n,k", TALL_SPLIT)
+def test_matmul_of_many_rows_in_parts(gpu_lib, m, n, k):
+    import torch
+    x, xs, w, ws = _operands(16, n, k, 14)
+    y, top = oracle.ref_fp8_matmul(x, xs, w, ws)
+    xt, st = (torch.from_numpy(v).cuda().repeat(m // 16, 1) for v in (x, xs))
+    out = torch.full((m, n), float("nan"), device="cuda")
+    space = torch.full((gpu_lib.quamba_fp8_matmul_workspace_size(m, n, k),), 0xFF, dtype=torch.uint8, device="cuda")
+    gpu_lib.quamba_fp8_matmul(xt, st, torch.from_numpy(w).cuda(), torch.from_numpy(ws).cuda(), out, workspace=space)
+    got = out.view(-1, 16, n)
+    assert (got == got[0]).all()
+    assert (np.abs(got[0].double().cpu().numpy() - y) <= _bound(y, top, k, "fp32")).all()
