@@ -458,10 +458,11 @@ int quamba_fp8_matmul(int64_t m, int64_t n, int64_t k, const uint8_t *x, int64_t
  * in fp32, max_k the largest logit of the beam; a finished beam has one candidate, (k, pad_token), worth scores[k].  A logit of
  * -infinity forbids its token.  A beam offers nothing whose score is not finite (a place that is still empty), which has a
  * logit of NaN or +infinity, or none above -infinity.
- *   out_scores  device fp32  [batch, count]  the values of the best candidates, best first; equal ones by rising beam, then token
+ *   out_scores  device fp32  [batch, count]  the values of the best candidates, best first; equal ones by rising beam,
+ *                                        those of one beam by falling logit, then by rising token
  *   out_parents device int32 [batch, count]  their beams            out_tokens device int32 [batch, count]  their tokens
  * Where fewer candidates than `count` are left, the places behind them get the value -infinity, the beam (place mod beams) and
- * pad_token.  Candidates of one beam are told apart by their logits.
+ * pad_token.
  *   workspace   device scratch of at least quamba_beam_select_workspace_size bytes, 16-byte aligned.  Calls that share it
  *               must not overlap.
  * batch = 0: nothing is launched.

@@ -3,6 +3,9 @@
 //
 //   value(k, v) = score_k + ((x_kv - max_k) - log sum_u exp(x_ku - max_k))
 //
+// Equal values go by rising beam, and in a beam, whose logits may differ where their values round to one number, by falling logit and
+// rising token: the order in which a piece keeps its best, so that the pieces' borders decide nothing.
+//
 // A first launch reads the logits once: a workgroup takes a piece of one beam's row into registers and leaves its largest
 // logit, its sum of exponentials against that and its best `count` logits.  A second one, a workgroup to a sequence, joins
 // the pieces' sums, turns the pieces' best logits into values and takes the best of them.  Bound: HBM for large batches, two launches for
@@ -16,7 +19,7 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kGathered = 1024;  // candidates that are ranked against each other
-constexpr int kJoined = 2048;    // candidates of a round of the second launch
+constexpr int kJoined = 1024;    // candidates of a round of the second launch
 
 // Floats as whole numbers of the same order; 0 is below all (the place of what is no candidate).
 __device__ __forceinline__ uint32_t ordered(float v)
@@ -36,17 +39,28 @@ __device__ __forceinline__ float wave_max(float v)
     return v;
 }
 
+// A key's uppermost 32 bits, an ordered float, decide first; 0 is no candidate.
+typedef unsigned __int128 uint128_t;
+__device__ __forceinline__ uint32_t upper(uint64_t key) { return (uint32_t)(key >> 32); }
+__device__ __forceinline__ uint32_t upper(uint128_t key) { return (uint32_t)(key >> 96); }
+__device__ __forceinline__ uint64_t from_lane(uint64_t key, int d) { return (uint64_t)__shfl_xor((long long)key, d, 64); }
+__device__ __forceinline__ uint128_t from_lane(uint128_t key, int d)
+{
+    return (uint128_t)from_lane((uint64_t)(key >> 64), d) << 64 | from_lane((uint64_t)key, d);
+}
+
+template <typename K>
 struct Chooser {
-    uint64_t gathered[kGathered];
-    uint64_t wave_best[2][kWaves];
+    K gathered[kGathered];
+    K wave_best[2][kWaves];
     uint32_t tops[kThreads];
     int n;
 };
 
 // A bound that at least `count` of the threads' tops reach, where so many are above 0, and few more: the largest of those whose lower
 // 32 - BITS bits are 0.  Bit by bit, by every wave for itself.
-template <int BITS>
-__device__ __forceinline__ uint32_t bound_of(Chooser &c, int count, uint32_t top)
+template <int BITS, typename K>
+__device__ __forceinline__ uint32_t bound_of(Chooser<K> &c, int count, uint32_t top)
 {
     c.tops[threadIdx.x] = top;
     if (threadIdx.x == 0) c.n = 0;
@@ -66,20 +80,21 @@ __device__ __forceinline__ uint32_t bound_of(Chooser &c, int count, uint32_t top
 }
 
 // The `count` largest of the workgroup's keys, key(e) for e < E in every thread, 0 for none and otherwise all different: out[0 ..
-// count - 1], largest first, 0 where there are no more.  `top` is the upper half of the thread's largest key, and from(bound) gives
-// the test, for e, whether key(e)'s upper half is at least `bound`.  `out` is written by some threads; the caller waits before
+// count - 1], largest first, 0 where there are no more.  `top` is the upper() of the thread's largest key, and from(bound) gives
+// the test, for e, whether key(e)'s upper() is at least `bound`.  `out` is written by some threads; the caller waits before
 // it is read elsewhere, and before it calls again.
 //
 // `count` threads have a key at least as large as the count-th largest of the threads' own largest ones, so nothing below that
 // is among the best: what is left is mostly little more than `count` keys, which are ranked by counting.  The bound is sought in
-// the upper 16 of a key's bits (for floats the sign, the exponent and 7 bits more: the last bits would spare few keys).  Where
+// the uppermost BITS of a key: 16 for logits (the sign, the exponent and 7 bits more: the last bits would spare few keys), 24 for values, which
+// share their first bits where a score is low (32 x 8 beams of 128000, 16 choices, scores of -1000: 56 us with 16, 35 with 24).  Where
 // the best keys lie in a few threads (the frequent tokens of a vocabulary side by side) more are left; as long as they are more than
 // threads, they are dealt out to all of them and bounded again.
-template <int E, typename From, typename Key, typename Out>
-__device__ __forceinline__ void choose(Chooser &c, int count, uint32_t top, const From &from, const Key &key, const Out &out)
+template <int E, int BITS, typename K, typename From, typename Key, typename Out>
+__device__ __forceinline__ void choose(Chooser<K> &c, int count, uint32_t top, const From &from, const Key &key, const Out &out)
 {
     const int t = threadIdx.x, lane = t & 63;
-    const uint32_t bound = bound_of<16>(c, count, top);
+    const uint32_t bound = bound_of<BITS>(c, count, top);
     if (top >= bound) {
         const auto candidate = from(bound);
 #pragma unroll
@@ -93,48 +108,48 @@ __device__ __forceinline__ void choose(Chooser &c, int count, uint32_t top, cons
     int n = c.n;
     if (n <= kGathered) {
         for (int before = kGathered + 1; n > kThreads && n < before;) {
-            uint64_t mine[kGathered / kThreads];
+            K mine[kGathered / kThreads];
             uint32_t most = 0;
 #pragma unroll
             for (int i = 0; i < kGathered / kThreads; ++i) {
-                mine[i] = i * kThreads + t < n ? c.gathered[i * kThreads + t] : 0;
-                most = max(most, (uint32_t)(mine[i] >> 32));
+                mine[i] = i * kThreads + t < n ? c.gathered[i * kThreads + t] : K(0);
+                most = max(most, upper(mine[i]));
             }
             __syncthreads();  // all know n
             const uint32_t least = bound_of<32>(c, count, most);
 #pragma unroll
             for (int i = 0; i < kGathered / kThreads; ++i)
-                if ((uint32_t)(mine[i] >> 32) >= least) c.gathered[atomicAdd(&c.n, 1)] = mine[i];
+                if (upper(mine[i]) >= least) c.gathered[atomicAdd(&c.n, 1)] = mine[i];
             __syncthreads();
             before = n;
             n = c.n;
         }
         for (int i = t; i < n; i += kThreads) {
-            const uint64_t k = c.gathered[i];
+            const K k = c.gathered[i];
             int rank = 0;
 #pragma unroll 8
             for (int j = 0; j < n; ++j) rank += c.gathered[j] > k;
             if (rank < count) out(rank, k);
         }
-        for (int i = n + t; i < count; i += kThreads) out(i, (uint64_t)0);
+        for (int i = n + t; i < count; i += kThreads) out(i, K(0));
     } else {  // many equal ones: one after the other
-        uint64_t last = ~(uint64_t)0;
+        K last = ~K(0);
         for (int i = 0; i < count; ++i) {
-            uint64_t best = 0;
+            K best = 0;
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                const uint64_t k = key(e);
+                const K k = key(e);
                 if (k < last && k > best) best = k;
             }
 #pragma unroll
             for (int d = 32; d; d >>= 1) {
-                const uint64_t o = (uint64_t)__shfl_xor((long long)best, d, 64);
-                best = max(best, o);
+                const K o = from_lane(best, d);
+                best = o > best ? o : best;
             }
             if (lane == 0) c.wave_best[i & 1][t / 64] = best;
             __syncthreads();
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) best = max(best, c.wave_best[i & 1][w]);
+            for (int w = 0; w < kWaves; ++w) best = c.wave_best[i & 1][w] > best ? c.wave_best[i & 1][w] : best;
             last = best;
             if (t == 0) out(i, best);
         }
@@ -191,7 +206,7 @@ template <int TYPE, int E>
 __global__ __launch_bounds__(kThreads) void beam_pieces_kernel(SelectArgs a, int pieces, Divisor by_pieces, uint64_t *best, Piece *piece)
 {
     constexpr int kVec = Logits<TYPE>::kCount, VECTORS = E / kVec, kPiece = kThreads * E;
-    __shared__ Chooser chooser;
+    __shared__ Chooser<uint64_t> chooser;
     __shared__ float wave_f[2][kWaves];
     const int t = threadIdx.x, row = quotient((int)blockIdx.x, by_pieces), first = ((int)blockIdx.x - row * pieces) * kPiece;
     if (!offers(a, row) || (a.finished && a.finished[row])) return;  // the second launch does not read it
@@ -220,7 +235,7 @@ __global__ __launch_bounds__(kThreads) void beam_pieces_kernel(SelectArgs a, int
     sum = group_sum<64>(sum);
     if (t % 64 == 0) wave_f[1][t / 64] = sum;
     uint64_t *to = best + (int64_t)blockIdx.x * a.count;
-    choose<E>(
+    choose<E, 16>(
         chooser, a.count, mine > -__builtin_inff() ? ordered(mine + 0.0f) : 0u,  // -0 is 0
         [&](uint32_t bound) {
             const float least = fmaxf(of_ordered(bound), -__FLT_MAX__);
@@ -247,15 +262,15 @@ __device__ __forceinline__ float row_max(float v)  // of 16 lanes
 // A workgroup to a sequence: 16 lanes join a beam's pieces, then all take the best of the pieces' best.  These are gone through place by
 // place, the first ones of all pieces, then the second ones: each piece's fall, so there are no better ones left once a place of every
 // piece brought none, mostly after the first round (1 sequence of 16 beams, 200000 logits each, 32 choices: 112 us in the order of the
-// pieces with pieces of 2048 logits, 19 so with 8192).  Where one round holds them all, they are taken as they lie.
+// pieces with pieces of 2048 logits, 17 so with 8192).  Where one round holds them all, they are taken as they lie.
 __global__ __launch_bounds__(kThreads) void beam_join_kernel(SelectArgs a, int pieces, int places, int lists, int per_beam, Divisor by_place,
                                                              Divisor by_beam, const uint64_t *best, const Piece *piece)
 {
     constexpr int E = kJoined / kThreads;
-    __shared__ Chooser chooser;
+    __shared__ Chooser<uint128_t> chooser;
     __shared__ float score[kMaxBeams], row_top[kMaxBeams], row_log[kMaxBeams];
     __shared__ uint8_t kind[kMaxBeams];  // 0: offers nothing, 1: its pieces' tokens, 2: finished
-    __shared__ uint64_t list[kMaxChoices];
+    __shared__ uint128_t list[kMaxChoices];
     const int t = threadIdx.x, b = blockIdx.x;
     const int all = lists * places;
     const uint64_t *candidates = best + (int64_t)b * all;
@@ -292,7 +307,7 @@ __global__ __launch_bounds__(kThreads) void beam_join_kernel(SelectArgs a, int p
     __syncthreads();
     int quiet = 0;  // candidates since the last one that was among the best
     for (int first = 0; first < all && quiet < lists; first += kThreads * E) {
-        uint64_t key[E + 1];
+        uint128_t key[E + 1];  // value, complement of the beam, logit, complement of the token
         uint32_t top = 0;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
@@ -300,42 +315,40 @@ __global__ __launch_bounds__(kThreads) void beam_join_kernel(SelectArgs a, int p
             const int i = first + e * kThreads + t;
             if (i < all) {
                 const int from = places == 1 ? i : i - quotient(i, by_place) * lists, k = quotient(from, by_beam);
-                uint32_t token = ~(uint32_t)c[e];
+                uint64_t in_beam = c[e];
                 float v = -__builtin_inff();
                 if (kind[k] == 1) {
                     if (c[e]) v = score[k] + ((of_ordered((uint32_t)(c[e] >> 32)) - row_top[k]) - row_log[k]);
                 } else if (kind[k] == 2 && i == k * per_beam) {
-                    token = (uint32_t)a.pad;
+                    in_beam = (uint32_t)~a.pad;
                     v = score[k];
                 }
                 if (v > -__builtin_inff())
-                    key[e] = (uint64_t)ordered(v + 0.0f) << 32 | ~((uint32_t)k * (uint32_t)a.vocab + token);
+                    key[e] = (uint128_t)((uint64_t)ordered(v + 0.0f) << 32 | (uint32_t)~k) << 64 | in_beam;
                 const int64_t next = (int64_t)i + kThreads * E;
                 if (next < all) c[e] = candidate((int)next);
             }
-            top = max(top, (uint32_t)(key[e] >> 32));
+            top = max(top, upper(key[e]));
         }
-        if (first && !__syncthreads_or(top >= max((uint32_t)(list[a.count - 1] >> 32), 1u))) {
+        if (first && !__syncthreads_or(top >= max(upper(list[a.count - 1]), 1u))) {
             quiet += kThreads * E;
             continue;
         }
         quiet = 0;
-        key[E] = t < kMaxChoices ? list[t] : 0;
-        top = max(top, (uint32_t)(key[E] >> 32));
+        key[E] = t < kMaxChoices ? list[t] : uint128_t(0);
+        top = max(top, upper(key[E]));
         __syncthreads();
-        choose<E + 1>(
-            chooser, a.count, top, [&](uint32_t bound) { return [&key, bound](int e) { return (uint32_t)(key[e] >> 32) >= bound; }; },
-            [&](int e) { return key[e]; }, [&](int i, uint64_t k) { list[i] = k; });
+        choose<E + 1, 24>(
+            chooser, a.count, top, [&](uint32_t bound) { return [&key, bound](int e) { return upper(key[e]) >= bound; }; },
+            [&](int e) { return key[e]; }, [&](int i, uint128_t k) { list[i] = k; });
         __syncthreads();
     }
     for (int i = t; i < a.count; i += kThreads) {
-        const uint64_t chosen = list[i];
-        const uint32_t at = ~(uint32_t)chosen;
-        const uint32_t k = at / (uint32_t)a.vocab;
+        const uint128_t chosen = list[i];
         const int64_t o = (int64_t)b * a.count + i;
-        a.out_scores[o] = chosen ? of_ordered((uint32_t)(chosen >> 32)) : -__builtin_inff();
-        a.out_parents[o] = chosen ? (int32_t)k : i % a.beams;
-        a.out_tokens[o] = chosen ? (int32_t)(at - k * (uint32_t)a.vocab) : a.pad;
+        a.out_scores[o] = chosen ? of_ordered(upper(chosen)) : -__builtin_inff();
+        a.out_parents[o] = chosen ? (int32_t)~(uint32_t)(chosen >> 64) : i % a.beams;
+        a.out_tokens[o] = chosen ? (int32_t)~(uint32_t)chosen : a.pad;
     }
 }
 

@@ -283,3 +283,42 @@ def test_reorder_offsets_beyond_32_bits_and_many_sequences(gpu_lib):
     want = small[torch.arange(b, device="cuda")[:, None], p.long()].clone()
     gpu_lib.quamba_beam_reorder(p, [small])
     assert torch.equal(small, want)
+
+
+@pytest.mark.parametrize("count", [1, 2, 3, 16])
+@pytest.mark.parametrize("b", [1, 70])
+def test_select_tells_candidates_of_a_beam_apart_by_their_logits(gpu_lib, b, count):
+    """Logits of a beam that differ while their values round to the same fp32 number: the larger one comes first, in one piece of a row
+    and across two, in short pieces (1 sequence) and in long ones (70)."""
+    import torch
+    V = 9001
+    near = [1.0, 1.00001, 1.00002]
+    for places in ((5, 77, 4000), (5, 5000, 8999), (8999, 5000, 5), (4095, 4096, 4097), (8191, 8192, 8193), (3, 2, 8500)):
+        x = _logits(b, 1, V, "fp32", 41) - 20
+        x[..., list(places)] = torch.tensor(near, device="cuda")
+        _check(gpu_lib, x, np.full((b, 1), -1000.0), count=count, gap=False)
+
+
+@pytest.mark.parametrize("b,K,V,count", [(1, 1, 20011, 128), (100, 1, 20011, 128), (1, 1, 20011, 7), (100, 1, 20011, 7), (3, 3, 50, 120),
+                                         (1, 1, 4096, 40), (1, 1, 300000, 64)])
+def test_select_from_logits_closer_than_the_scores_resolution(gpu_lib, b, K, V, count):
+    """Every logit of a beam within some units of the values' last place, beams far apart."""
+    x = _logits(b, K, V, "fp32", V + b, spread=1e-3)
+    scores = -10000.0 - 100 * np.tile(np.arange(K), (b, 1))
+    _check(gpu_lib, x, scores, count=count, gap=False)
+
+
+@pytest.mark.parametrize("kind", ["fp32", "bf16"])
+@pytest.mark.parametrize("b,K,V,count", [(1, 2, 100, 128), (100, 2, 100, 128), (1, 3, 20011, 128), (64, 3, 20011, 9), (1, 1, 5, 8)])
+def test_select_where_all_values_are_equal(gpu_lib, b, K, V, count, kind):
+    """Scores so large that every candidate's value is the score: by rising beam, then by falling logit, then by token."""
+    x = _logits(b, K, V, kind, V, spread=0.1)
+    x = (x.float() * 50).round().div(50).to(x.dtype)                   # some equal ones
+    scores = np.full((b, K), -2.0 ** 30, np.float32)
+    got = _select(gpu_lib, x, scores, None, 0, count)
+    x = x.float().cpu().numpy()
+    for i in range(b):
+        order = [(k, t) for k in range(K) for t in np.argsort(-x[i, k], kind="stable")][:count]
+        n = len(order)
+        assert (got[0][i, :n] == -2.0 ** 30).all() and (got[0][i, n:] == -np.inf).all()
+        assert [*zip(got[1][i, :n].tolist(), got[2][i, :n].tolist())] == [(k, int(t)) for k, t in order]
