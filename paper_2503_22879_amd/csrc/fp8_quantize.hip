@@ -170,31 +170,42 @@ void launch(const QuantizeArgs &a, bool squares, hipStream_t stream)
 
 }  // namespace
 
+// Launches of whole rows of blocks, or of a part of one: at most 2^31 threads and 2^23 blocks, so that threads and indices fit 32 bits.
+QuantizeCut fp8_quantize_cut(int64_t row_blocks, int32_t block_rows)
+{
+    const int64_t most = block_rows > 1 ? ((int64_t)1 << 31) / kSquareThreads : (int64_t)1 << 23;
+    return {std::max<int64_t>(1, most / row_blocks), std::min(row_blocks, most)};
+}
+
+int64_t fp8_quantize_threads(int64_t blocks, int32_t block_rows)
+{
+    return block_rows > 1 ? blocks * kSquareThreads : (blocks + 15) / 16 * 256;
+}
+
 hipError_t launch_fp8_quantize(QuantizeArgs a, int32_t block_rows, int32_t x_type, hipStream_t stream)
 {
-    const int64_t row_blocks = (a.cols + kBlock - 1) / kBlock;
-    a.row_blocks = (int32_t)row_blocks;
-    a.by_row_blocks = divisor((uint32_t)row_blocks);
-    // launches of whole rows of blocks, at most 2^23 blocks or one row (a row has at most 2^23): indices and threads fit 32 bits
-    const int64_t all = (a.rows + block_rows - 1) / block_rows, most = std::max<int64_t>(1, ((int64_t)1 << 23) / row_blocks);
-    const int64_t rows = a.rows;
-    const char *x = static_cast<const char *>(a.x);
-    for (int64_t first = 0; first < all; first += most) {
-        const int64_t n = std::min(most, all - first);
-        QuantizeArgs p = a;
-        p.x = x + first * block_rows * a.x_stride * (x_type == QUAMBA_F32 ? 4 : 2);
-        p.q = a.q + first * block_rows * a.q_stride;
-        p.scales = a.scales + first * row_blocks;
-        p.rows = std::min(rows - first * block_rows, n * block_rows);
-        p.blocks = (int32_t)(n * row_blocks);
-        switch (x_type) {
-            case QUAMBA_F32: launch<QUAMBA_F32>(p, block_rows > 1, stream); break;
-            case QUAMBA_F16: launch<QUAMBA_F16>(p, block_rows > 1, stream); break;
-            default: launch<QUAMBA_BF16>(p, block_rows > 1, stream); break;
+    const int64_t row_blocks = (a.cols + kBlock - 1) / kBlock, all = (a.rows + block_rows - 1) / block_rows;
+    const QuantizeCut cut = fp8_quantize_cut(row_blocks, block_rows);
+    for (int64_t row = 0; row < all; row += cut.rows)
+        for (int64_t column = 0; column < row_blocks; column += cut.columns) {
+            const int64_t rows = std::min(cut.rows, all - row), columns = std::min(cut.columns, row_blocks - column);
+            QuantizeArgs p = a;
+            p.x = static_cast<const char *>(a.x) + (row * block_rows * a.x_stride + column * kBlock) * (x_type == QUAMBA_F32 ? 4 : 2);
+            p.q = a.q + row * block_rows * a.q_stride + column * kBlock;
+            p.scales = a.scales + row * row_blocks + column;  // a part of a row of blocks: there is no other row in the launch
+            p.rows = std::min(a.rows - row * block_rows, rows * block_rows);
+            p.cols = std::min(a.cols - column * kBlock, columns * kBlock);
+            p.row_blocks = (int32_t)columns;
+            p.by_row_blocks = divisor((uint32_t)columns);
+            p.blocks = (int32_t)(rows * columns);
+            switch (x_type) {
+                case QUAMBA_F32: launch<QUAMBA_F32>(p, block_rows > 1, stream); break;
+                case QUAMBA_F16: launch<QUAMBA_F16>(p, block_rows > 1, stream); break;
+                default: launch<QUAMBA_BF16>(p, block_rows > 1, stream); break;
+            }
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
         }
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-    }
     return hipSuccess;
 }
 

@@ -398,6 +398,12 @@ struct QuantizeArgs {
     int32_t row_blocks;  // blocks along a row
     int32_t blocks;      // of the launch
 };
+// How many rows of blocks and blocks of a row a launch has, and the threads of one.
+struct QuantizeCut {
+    int64_t rows, columns;
+};
+QuantizeCut fp8_quantize_cut(int64_t row_blocks, int32_t block_rows);
+int64_t fp8_quantize_threads(int64_t blocks, int32_t block_rows);
 hipError_t launch_fp8_quantize(QuantizeArgs a, int32_t block_rows, int32_t x_type, hipStream_t stream);
 struct MatmulArgs {
     const uint8_t *x, *w;

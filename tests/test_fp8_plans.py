@@ -46,3 +46,20 @@ def test_the_parts_of_many_rows_are_joined_by_a_launch_that_fits():
         assert rows(m) == min(m, 65535)
     for m, n, k in TALL_SPLIT:
         assert m > 65535 and q.quamba_fp8_matmul_workspace_size(m, n, k) > 0
+
+
+class Cut(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("columns", C.c_int64)]
+
+
+@pytest.mark.parametrize("block_rows", [1, 128])
+def test_the_quantizers_launches_fit_32_bits(block_rows):
+    """Threads of a launch are counted in 32 bits, and block numbers go through a division of 31; a launch of several rows of blocks holds them
+    whole."""
+    cut = _internal("_ZN6quamba16fp8_quantize_cutEli", Cut, C.c_int64, C.c_int32)
+    threads = _internal("_ZN6quamba20fp8_quantize_threadsEli", C.c_int64, C.c_int64, C.c_int32)
+    for row_blocks in (1, 2, 3, 64, 1000, 2 ** 21 + 1, 2 ** 22, 2 ** 22 + 1, 2 ** 23):
+        got = cut(row_blocks, block_rows)
+        assert got.rows >= 1 and 1 <= got.columns <= row_blocks and (got.rows == 1 or got.columns == row_blocks)
+        assert got.rows * got.columns <= 2 ** 23 and threads(got.rows * got.columns, block_rows) < 2 ** 32, row_blocks
+        assert 2 * got.rows * got.columns >= min(row_blocks, 2 ** 20)                # and there are few of them

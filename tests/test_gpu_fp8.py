@@ -316,3 +316,21 @@ def test_matmul_of_many_rows_in_parts(gpu_lib, m, n, k):
     got = out.view(-1, 16, n)
     assert (got == got[0]).all()
     assert (np.abs(got[0].double().cpu().numpy() - y) <= _bound(y, top, k, "fp32")).all()
+
+
+@pytest.mark.parametrize("rows,cols", [(1 << 30, 1), (1, 1 << 30)])
+@pytest.mark.parametrize("block_rows", [1, 128])
+def test_quantizer_of_more_blocks_than_a_launch_takes(gpu_lib, rows, cols, block_rows):
+    """As many rows, or columns, as fit: the same 2^17 values again and again, the first against the oracle."""
+    import torch
+    period = 1 << 17
+    shape = (period, 1) if cols == 1 else (1, period)
+    x = torch.from_numpy(_values(1, period, 22).reshape(shape)).half()
+    want, ws = oracle.quantize_fp8(x.float().numpy(), block_rows)
+    xt = x.cuda().view(-1).repeat((rows * cols) // period).view(rows, cols)
+    codes = torch.full((rows, cols), 0xA5, dtype=torch.uint8, device="cuda")
+    scales = torch.full((-(-rows // block_rows), -(-cols // 128)), -7.0, device="cuda")
+    gpu_lib.quamba_fp8_quantize(xt, codes, scales, block_rows=block_rows)
+    for got, first in ((codes.view(-1), want), (scales.view(-1), ws)):
+        got = got.view(-1, first.size)
+        assert np.array_equal(got[0].cpu().numpy(), first.reshape(-1)) and bool((got == got[0]).all())
