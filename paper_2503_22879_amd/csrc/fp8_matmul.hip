@@ -710,7 +710,18 @@ Fp8Plan fp8_matmul_plan(int32_t m, int32_t n, int32_t blocks, bool workspace)
     return best;
 }
 
-// The same where rows do not lie at multiples of 16 bytes or the depth ends inside a piece, so that operands go through registers and
+// A last round of 256 x 256 with few tiles takes as long as a full one: the rows that make whole rounds so, where these and a form of
+// their own for the others are estimated to take less than `us` (16384 x 18560 x 4096: 18.25 rounds; 16148 x 4224 x 7488: 4.25); else 0.
+int32_t fp8_matmul_whole_rounds(int32_t m, int32_t n, int32_t blocks, double us)
+{
+    const int64_t tiles_m = ((int64_t)m + 255) / 256, tiles_n = ((int64_t)n + 255) / 256, units = compute_units();
+    const int64_t rows = tiles_m * tiles_n / units * units / tiles_n * 256;
+    if (rows == 0 || rows >= m) return 0;
+    const double both = tiles256_us((int32_t)rows, n, blocks) + fp8_matmul_plan(m - (int32_t)rows, n, blocks, false).us;
+    return both < us ? (int32_t)rows : 0;
+}
+
+// The plan where rows do not lie at multiples of 16 bytes or the depth ends inside a piece, so that operands go through registers and
 // more workgroups to a unit hide their way better than more stages do.  A turn of a unit with w workgroups of 64 x 64 takes 0.25 + 0.55 w
 // us, with one of 128 x 128 1.95 and with w of them 1.65 w: 90 x 11640 x 7641 takes 65 us in 64 x 64 (118 in
 // 128 x 128), 1967 x 3304 x 3967 86 us in 128 x 128 (128 in 64 x 64), 50 x 4096 x 8191 18 us in 4 parts (34 with rings of rows).
@@ -766,17 +777,12 @@ hipError_t launch_part(const MatmulArgs &a, void *workspace, hipStream_t stream)
         if (other.form == Fp8Form::tiles64) return launch_tiles<64, 64, 2, 2, 1, 2, false>(a, other.splits, partial, stream);
         return launch_tiles<128, 128, 2, 2, 1, 2, false>(a, 1, nullptr, stream);
     }
-    // A last round of 256 x 256 with few tiles takes as long as a full one: the rows that make whole rounds so, and the others in a form of
-    // their own, where that is estimated to be shorter (16384 x 18560 x 4096: 18.25 rounds; 16148 x 4224 x 7488: 4.25).
-    const int64_t tiles_m = (a.m + 255) / 256, tiles_n = (a.n + 255) / 256, units = compute_units();
-    const int64_t rows = tiles_m * tiles_n / units * units / tiles_n * 256;
-    if (rows > 0 && rows < a.m &&
-        tiles256_us((int32_t)rows, a.n, a.blocks) + fp8_matmul_plan(a.m - (int32_t)rows, a.n, a.blocks, false).us < plan.us) {
+    if (const int32_t rows = fp8_matmul_whole_rounds(a.m, a.n, a.blocks, plan.us)) {
         MatmulArgs top = a, rest = a;
-        top.m = (int32_t)rows;
-        rest.m = a.m - (int32_t)rows;
+        top.m = rows;
+        rest.m = a.m - rows;
         rest.x = a.x + rows * a.x_stride;
-        rest.x_scales = a.x_scales + rows * a.blocks;
+        rest.x_scales = a.x_scales + (int64_t)rows * a.blocks;
         rest.y = static_cast<char *>(a.y) + rows * a.y_stride * (a.y_type == QUAMBA_F32 ? 4 : 2);
         const hipError_t e = launch_tiles<256, 256, 2, 4, 1, 2, true>(top, 1, nullptr, stream);
         return e == hipSuccess ? launch_part(rest, nullptr, stream) : e;

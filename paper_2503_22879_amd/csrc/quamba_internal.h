@@ -423,6 +423,8 @@ struct Fp8Plan {
 };
 Fp8Plan fp8_matmul_plan(int32_t m, int32_t n, int32_t blocks, bool workspace);
 Fp8Plan fp8_matmul_plan_unaligned(int32_t m, int32_t n, int32_t blocks, int most_splits);
+// Rows that go in 256 x 256 tiles on their own, in front of the others.
+int32_t fp8_matmul_whole_rounds(int32_t m, int32_t n, int32_t blocks, double us);
 // The last row of w's scales that the waves of a form read, over all of its tiles.
 int32_t fp8_matmul_last_scale_row(Fp8Form form, int32_t n);
 // Rows of workgroups that join the parts of m rows' sums.

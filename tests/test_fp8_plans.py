@@ -63,3 +63,15 @@ def test_the_quantizers_launches_fit_32_bits(block_rows):
         assert got.rows >= 1 and 1 <= got.columns <= row_blocks and (got.rows == 1 or got.columns == row_blocks)
         assert got.rows * got.columns <= 2 ** 23 and threads(got.rows * got.columns, block_rows) < 2 ** 32, row_blocks
         assert 2 * got.rows * got.columns >= min(row_blocks, 2 ** 20)                # and there are few of them
+
+
+def test_whole_rounds_and_every_form_behind_them_have_a_size_that_is_tested():
+    from test_gpu_fp8 import WHOLE_ROUNDS
+    whole = _internal("_ZN6quamba23fp8_matmul_whole_roundsEiiid", C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_double)
+    for form, (m, n, k) in WHOLE_ROUNDS.items():
+        rows = whole(m, n, -(-k // 128), _plan(m, n, k).us)
+        assert 0 < rows < m and rows % 256 == 0 and _plan(m - rows, n, k, False).form == FORMS[form], (m, n, k, rows)
+    assert set(WHOLE_ROUNDS) == set(FORMS) - {"tiles256"}       # its rounds would not be a rest
+    for m, n, k in ((16384, 18560, 4096), (8192, 3352, 768), (2048, 18560, 4096)):
+        assert whole(m, n, -(-k // 128), _plan(m, n, k).us) > 0
+    assert whole(256, 50021, 20, _plan(256, 50021, 2560).us) == 0 and whole(1, 10, 1, 0.0) == 0

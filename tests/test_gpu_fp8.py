@@ -334,3 +334,26 @@ def test_quantizer_of_more_blocks_than_a_launch_takes(gpu_lib, rows, cols, block
     for got, first in ((codes.view(-1), want), (scales.view(-1), ws)):
         got = got.view(-1, first.size)
         assert np.array_equal(got[0].cpu().numpy(), first.reshape(-1)) and bool((got == got[0]).all())
+
+
+# Rows that make whole rounds of 256 x 256 tiles go so, the others in a form of their own: a size for each of these
+# (test_fp8_plans.py checks which).
+WHOLE_ROUNDS = {"rows": (4100, 4000, 400), "tiles64": (4180, 4000, 768), "tiles64x128": (4200, 4224, 1024), "tiles128_one": (4240, 4500, 768),
+                "tiles128_two": (4500, 4500, 768)}
+
+
+@pytest.mark.parametrize("m,n,k", WHOLE_ROUNDS.values())
+def test_matmul_in_whole_rounds_and_the_rest(gpu_lib, m, n, k):
+    """Rows of x and y further apart than they are long, what lies between is neither read nor written."""
+    import torch
+    ops = _operands(m, n, k, m)
+    y, top = oracle.ref_fp8_matmul(*ops)
+    x, xs, w, ws = (torch.from_numpy(a).cuda() for a in ops)
+    xb = torch.full((m, k + 48), 0x7f, dtype=torch.uint8, device="cuda")
+    xb[:, :k] = x
+    for kind in ("fp32", "fp16"):
+        out = torch.full((m, n + 24), 77.0, dtype=_torch_type(kind), device="cuda")
+        gpu_lib.quamba_fp8_matmul(xb[:, :k], xs, w, ws, out[:, :n])
+        assert (out[:, n:] == 77.0).all()
+        off = np.abs(out[:, :n].double().cpu().numpy() - y) / _bound(y, top, k, kind)
+        assert off.max() <= 1.0, (kind, off.max(), np.argwhere(off > 1)[:5])
