@@ -75,3 +75,23 @@ def test_whole_rounds_and_every_form_behind_them_have_a_size_that_is_tested():
     for m, n, k in ((16384, 18560, 4096), (8192, 3352, 768), (2048, 18560, 4096)):
         assert whole(m, n, -(-k // 128), _plan(m, n, k).us) > 0
     assert whole(256, 50021, 20, _plan(256, 50021, 2560).us) == 0 and whole(1, 10, 1, 0.0) == 0
+
+
+def test_every_form_has_depths_with_a_last_block_in_part():
+    from test_gpu_fp8 import TAILS, TAIL_DEPTHS
+    assert {d % 128 for d in TAIL_DEPTHS} == {64, 80, 112} and {d // 128 % 2 for d in TAIL_DEPTHS} == {0, 1}
+    for form, sizes in TAILS.items():
+        for m, n in sizes:
+            assert all(_plan(m, n, k).form == FORMS[form] for k in TAIL_DEPTHS), (form, m, n)
+
+
+def test_no_workspace_where_the_depth_is_not_split():
+    unaligned = _internal("_ZN6quamba25fp8_matmul_plan_unalignedEiiii", Plan, C.c_int32, C.c_int32, C.c_int32, C.c_int32)
+    split = set()
+    for m in (1, 9, 17, 100, 333, 2000):
+        for n in (300, 4001):
+            for k in (90, 401, 517, 2101, 4113, 4112, 2048, 272):
+                splits = (unaligned(m, n, -(-k // 128), 16) if k % 16 else _plan(m, n, k)).splits
+                assert q.quamba_fp8_matmul_workspace_size(m, n, k) == (splits * m * -(-n // 4) * 16 if splits > 1 else 0), (m, n, k)
+                split.add((splits > 1, k % 16 > 0))
+    assert len(split) == 4

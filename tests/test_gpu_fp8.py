@@ -357,3 +357,30 @@ def test_matmul_in_whole_rounds_and_the_rest(gpu_lib, m, n, k):
         assert (out[:, n:] == 77.0).all()
         off = np.abs(out[:, :n].double().cpu().numpy() - y) / _bound(y, top, k, kind)
         assert off.max() <= 1.0, (kind, off.max(), np.argwhere(off > 1)[:5])
+
+
+# Depths whose last block holds 64 codes (the most of which half are multiplied), 80 and 112 (the least and the most of which all are), behind 3 and 8
+# whole blocks, so that either group of waves gets it; a size of each form (test_fp8_plans.py checks which).
+TAILS = {"rows": [(5, 300), (30, 300), (60, 300)], "tiles64": [(100, 500)], "tiles64x128": [(500, 4001)], "tiles128_one": [(600, 4095)],
+         "tiles128_two": [(2000, 2501)], "tiles256": [(4090, 4003)]}
+TAIL_DEPTHS = [whole * 128 + codes for whole in (3, 8) for codes in (64, 80, 112)]
+
+
+@pytest.mark.parametrize("m,n", [s for sizes in TAILS.values() for s in sizes])
+def test_matmul_of_a_last_block_in_part(gpu_lib, m, n):
+    """The codes behind the depth, which are read or repeated by no product, are NaN."""
+    import torch
+    ops = _operands(m, n, TAIL_DEPTHS[-1], m + 17)
+    for depth in TAIL_DEPTHS:
+        blocks = -(-depth // 128)
+        x, xs, w, ws = (ops[i][:, :depth] if i % 2 == 0 else ops[i][:, :blocks].copy() for i in range(4))
+        y, top = oracle.ref_fp8_matmul(x, xs, w, ws)
+        xb, wb = (torch.full((v.shape[0], depth + 128), 0x7f, dtype=torch.uint8, device="cuda") for v in (x, w))
+        xb[:, :depth], wb[:, :depth] = torch.from_numpy(x.copy()).cuda(), torch.from_numpy(w.copy()).cuda()
+        for space in (True, False):
+            size = gpu_lib.quamba_fp8_matmul_workspace_size(m, n, depth) if space else 0
+            out = torch.full((m, n), float("nan"), device="cuda")
+            gpu_lib.quamba_fp8_matmul(xb[:, :depth], torch.from_numpy(xs).cuda(), wb[:, :depth], torch.from_numpy(ws).cuda(), out,
+                                      workspace=torch.full((size,), 0xFF, dtype=torch.uint8, device="cuda") if size else None)
+            off = np.abs(out.double().cpu().numpy() - y) / _bound(y, top, depth, "fp32")
+            assert off.max() <= 1.0, (depth, space, off.max(), np.argwhere(off > 1)[:5])
