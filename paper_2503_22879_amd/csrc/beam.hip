@@ -86,8 +86,8 @@ __device__ __forceinline__ uint32_t bound_of(Chooser<K> &c, int count, uint32_t 
 //
 // `count` threads have a key at least as large as the count-th largest of the threads' own largest ones, so nothing below that
 // is among the best: what is left is mostly little more than `count` keys, which are ranked by counting.  The bound is sought in
-// the uppermost BITS of a key: 16 for logits (the sign, the exponent and 7 bits more: the last bits would spare few keys), 24 for values, which
-// share their first bits where a score is low (32 x 8 beams of 128000, 16 choices, scores of -1000: 56 us with 16, 35 with 24).  Where
+// the uppermost BITS of a key: 16 for logits (the sign, the exponent and 7 bits more: the last bits would spare few keys), 20 for values, which
+// share their first bits where a score is low (32 x 8 beams of 128000, 16 choices, scores of -1000: 56 us with 16, 35 with 20).  Where
 // the best keys lie in a few threads (the frequent tokens of a vocabulary side by side) more are left; as long as they are more than
 // threads, they are dealt out to all of them and bounded again.
 template <int E, int BITS, typename K, typename From, typename Key, typename Out>
@@ -338,7 +338,7 @@ __global__ __launch_bounds__(kThreads) void beam_join_kernel(SelectArgs a, int p
         key[E] = t < kMaxChoices ? list[t] : uint128_t(0);
         top = max(top, upper(key[E]));
         __syncthreads();
-        choose<E + 1, 24>(
+        choose<E + 1, 20>(
             chooser, a.count, top, [&](uint32_t bound) { return [&key, bound](int e) { return upper(key[e]) >= bound; }; },
             [&](int e) { return key[e]; }, [&](int i, uint128_t k) { list[i] = k; });
         __syncthreads();
