@@ -433,7 +433,8 @@ int quamba_fp8_quantize(int64_t rows, int64_t cols, int32_t block_rows, const vo
  *   w device e4m3 [n, k], rows w_stride >= k bytes apart;  w_scales device fp32 [ceil(n / 128), ceil(k / 128)]
  *   y device y_type (quamba_dtype) [m, n], rows y_stride >= n values apart; must not overlap the operands
  *   workspace  device scratch of workspace_bytes, 16-byte aligned
- * Products and sums are fp32, rounded once to y_type; the sum over the blocks is made in parts where few outputs would
+ * Products and sums are fp32, rounded once to y_type; the two scales of a block are multiplied first, so their product must lie in fp32's
+ * normal range where the output is to be right to rounding; the sum over the blocks is made in parts where few outputs would
  * leave the device idle, always in the same order.  A NaN code or a non-finite scale reaches the outputs that it belongs to
  * and no others.  m = 0: nothing is launched.  Any alignment and any stride are taken; rows that start at multiples of 16
  * bytes are read fastest.

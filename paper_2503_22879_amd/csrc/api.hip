@@ -454,7 +454,7 @@ extern "C" const char *quamba_strerror(int status)
         case QUAMBA_OK: return "ok";
         case QUAMBA_ENULL: return "a required pointer is NULL";
         case QUAMBA_ESHAPE: return "a dimension is non-positive, inconsistent or unsupported";
-        case QUAMBA_EWORKSPACE: return "workspace too small";
+        case QUAMBA_EWORKSPACE: return "workspace missing, too small or not aligned";
         case QUAMBA_EHIP: return "the HIP runtime refused the launch";
         case QUAMBA_EINVAL: return "invalid argument value";
         default: return "unknown status";

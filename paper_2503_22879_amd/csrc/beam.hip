@@ -352,8 +352,9 @@ __global__ __launch_bounds__(kThreads) void beam_join_kernel(SelectArgs a, int p
     }
 }
 
-// Logits of a piece for each of its 256 threads: 16 where 32 leave most of the device without a piece (1 x 4 beams of 50021: 9.1 us with 16,
-// 10.0 with 32; 8 x 8 of 50021: 12.2 and 11.9; 32 x 8 of 128000: 39.2 and 38.0; pieces of 8 gain nothing on small ones).
+// Logits of a piece for each of its 256 threads: 16 where 32 leave most of the device without a piece (1 x 4 beams of 50021: 9.8 us with 16,
+// 10.8 with 32; 8 x 8 of 50021: 13.7 and 13.2; 1 x 16 of 200000, 32 choices: 19.2 and 16.5; 32 x 8 of 128000: 33.7 and 35.3; pieces of 8 gain nothing
+// on small ones).
 int piece_values(int64_t rows, int32_t vocab)
 {
     return rows * ((vocab + kThreads * 32 - 1) / (kThreads * 32)) < compute_units() / 2 ? 16 : 32;
@@ -382,7 +383,8 @@ struct ReorderArgs {
     quamba_beam_cache_t cache[kCaches];
 };
 
-// Bytes that a thread moves of every beam: 16, fewer for many beams, so that they fit 64 registers.
+// Bytes that a thread moves of every beam: 16, fewer for many beams, so that they fit 64 registers.  With twice as many for more than 16 beams:
+// 32 beams of 80 MiB in all 18.96 -> 19.28 us, 640 MiB 206 -> 204; 64 beams of 160 MiB 41.0 -> 40.1, 1280 MiB 459 -> 421.
 constexpr int move_bytes(int beams) { return beams <= 16 ? 16 : 256 / beams; }
 
 // The parents of a sequence's beams, a byte each in scalar registers.
@@ -502,8 +504,9 @@ hipError_t launch_beam_reorder(int32_t batch, int32_t beams, const int32_t *pare
                       : beams <= 16 ? launch_slices<16> : beams <= 32 ? launch_slices<32> : launch_slices<64>;
     const int64_t slice = kMovers * (beams <= 16 ? move_bytes(16) : beams <= 32 ? move_bytes(32) : move_bytes(64));
     const int64_t most = kMaxCacheBytes / slice;
-    // What fits the last cache (256 MiB) is left there for the step that reads the states next: 24 layers of 4 beams, 75 MB, take 15.0 us,
-    // past the caches 17.0.
+    // What fits the last cache (256 MiB) is left there for the step that reads the states next.  Layers of 4 beams in fp32, through the caches
+    // and past them: 72 MiB 16.5 and 19.5 us, 216 MiB 36 and 52, 288 MiB 64 and 68, 432 MiB 120 and 113, 1152 MiB 319 and 299; 8 beams in 8
+    // bits: 256 MiB 50 and 75, 384 MiB 104 both, 1024 MiB 310 and 293.
     double bytes = 0.0;
     for (int32_t i = 0; i < n; ++i) bytes += (double)caches[i].bytes * beams * batch;
     const bool past = bytes > 256.0 * 1024 * 1024;
