@@ -493,6 +493,88 @@ typedef struct quamba_beam_cache_t {
 int quamba_beam_reorder(int32_t batch, int32_t beams, const int32_t *parents, int32_t n_caches,
                         const quamba_beam_cache_t *caches, void *hip_stream);
 
+/* ---- what a model answers: log probabilities of tokens, distance from a teacher ----
+ * Rows of logits x [rows, vocab] of `type` (quamba_dtype), logits_stride >= vocab values apart, at any address that is a multiple of the type's
+ * size.  z = x / temperature, p = softmax(z), everything in fp32.  A logit of -infinity is a token that cannot come (p = 0).  A row has no
+ * distribution where a logit is NaN or +infinity or none is above -infinity: its outputs are NaN.  No rows: nothing is launched. */
+
+/*
+ * Log probabilities of given tokens, with the entropy and the most likely alternatives.
+ *   targets    device int32 [rows] or NULL (then logprobs is NULL too).  A target that is no token (outside 0 .. vocab - 1) marks a row of
+ *              padding: it is not read, its outputs are 0, its alternatives -infinity and -1.
+ *   logprobs   device fp32 [rows]  ln p[target]
+ *   log_sums   device fp32 [rows] or NULL   ln sum_v exp(z_v), what the gradient takes
+ *   entropies  device fp32 [rows] or NULL   -sum_v p_v ln p_v
+ *   count      0 .. 128 alternatives;  top_logprobs device fp32 [rows, count], top_tokens device int32 [rows, count]: the tokens of the largest
+ *              logits with ln p, falling, equal logits by rising token; -infinity and -1 where fewer tokens may come, and in rows without a
+ *              distribution
+ *   workspace  device scratch of workspace_bytes, 16-byte aligned
+ * quamba_token_logprobs_workspace_size is the scratch memory with which a call of this size takes its fastest launch on the current device (may
+ * be 0; 0 for invalid sizes).  With a workspace that is NULL, smaller or not aligned a row is one workgroup's: the same tokens, values to
+ * rounding, slower for few rows.  Calls that share a workspace must not overlap.
+ * Errors: ENULL, ESHAPE (negative rows, more than 2^31, vocab not positive or above 2^26, count, stride below vocab or above 2^40), EINVAL (type,
+ * temperature outside 2^-100 .. 2^100, logits at an address between the type's), EHIP.
+ */
+size_t quamba_token_logprobs_workspace_size(int64_t rows, int64_t vocab, int32_t count);
+int quamba_token_logprobs(int64_t rows, int64_t vocab, const void *logits, int32_t type, int64_t logits_stride,
+                          float temperature, const int32_t *targets, float *logprobs, float *log_sums, float *entropies,
+                          int32_t count, float *top_logprobs, int32_t *top_tokens, void *workspace,
+                          size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Its gradient: grad_logits = d / dx of sum over the rows of grad_logprobs logprobs + grad_entropies entropies,
+ *   grad_logits[v] = (grad_logprobs ([v = target] - p_v) - grad_entropies p_v (ln p_v + entropy)) / temperature
+ *   targets, grad_logprobs  device [rows], both or neither      log_sums  device fp32 [rows], as that call left them
+ *   entropies, grad_entropies  device fp32 [rows], both or neither
+ *   grad_logits  device `type` [rows, vocab], rows grad_stride >= vocab values apart; it may take the logits' place (the same address and
+ *                stride) and must not overlap them otherwise
+ * Rows of padding, and rows whose gradients are 0, are not read: their gradient is 0.  p is made from log_sums, so its relative error is theirs
+ * (2^-24 of |log_sum|).
+ * Errors: as above, and EINVAL for a gradient that overlaps the logits.
+ */
+int quamba_token_logprobs_backward(int64_t rows, int64_t vocab, const void *logits, int32_t type, int64_t logits_stride,
+                                   float temperature, const int32_t *targets, const float *log_sums,
+                                   const float *entropies, const float *grad_logprobs, const float *grad_entropies,
+                                   void *grad_logits, int64_t grad_stride, void *hip_stream);
+
+/*
+ * Distance of each row from a teacher that is known by its most likely tokens (distillation; how far a quantized model is from the one it was made
+ * from), and its gradient.
+ *   teacher, teacher_tokens  device fp32 and int32 [rows, places], 1 .. 128 places.  A place whose token is outside 0 .. vocab - 1, or whose
+ *              value is -infinity, is empty.  A token may stand in several places; its probabilities add up.
+ *   rest = 0:  teacher holds logits (or log probabilities): q = softmax over the row's places of teacher / temperature,
+ *                loss = sum_k q_k (ln q_k - ln p[token_k])
+ *   rest = 1:  teacher holds log probabilities at this temperature, as quamba_token_logprobs gives them: q = exp(teacher), and what they
+ *              leave, q_R = max(0, 1 - sum_k q_k), is one more outcome,
+ *                loss += q_R (ln q_R - ln p_R),  p_R = sum of p over the tokens without a place
+ *              (left out, with q_R = 0, where p_R = 0).
+ *   weights    device fp32 [rows] or NULL (1).  A row whose weight is 0, or whose places are all empty, is not read: its loss and its
+ *              gradient are 0.
+ *   losses     device fp32 [rows], without the weights
+ *   log_sums, log_rests  device fp32 [rows] or NULL: ln sum exp(z) over all tokens, and over those without a place (rest = 1; else 0)
+ *   grad_logits  NULL, or device `type` [rows, vocab], rows grad_stride >= vocab values apart: d / dx of sum over the rows of weights losses,
+ *                grad_logits[v] = weight / temperature (p_v (sum q + q_R) - sum of the q_k with token_k = v - [no place] q_R p_v / p_R);
+ *              it may take the logits' place (the same address and stride) and must not overlap them otherwise
+ *   workspace  as for quamba_token_logprobs
+ * A place of 1 is the cross-entropy of its token.  A teacher's NaN makes its row NaN.
+ * Errors: as above, ESHAPE also for places outside 1 .. 128, EINVAL also for rest other than 0 and 1 and a gradient that overlaps the logits.
+ */
+size_t quamba_distill_loss_workspace_size(int64_t rows, int64_t vocab, int32_t places);
+int quamba_distill_loss(int64_t rows, int64_t vocab, const void *logits, int32_t type, int64_t logits_stride,
+                        float temperature, int32_t places, const float *teacher, const int32_t *teacher_tokens,
+                        int32_t rest, const float *weights, float *losses, float *log_sums, float *log_rests,
+                        void *grad_logits, int64_t grad_stride, void *workspace, size_t workspace_bytes,
+                        void *hip_stream);
+
+/*
+ * The gradient alone, from the log sums of such a call (log_rests with rest = 1): grad_logits as above with grad_losses [rows] for the
+ * weights.  p and p / p_R are made from the log sums, so their relative error is theirs.  Errors: as above.
+ */
+int quamba_distill_backward(int64_t rows, int64_t vocab, const void *logits, int32_t type, int64_t logits_stride,
+                            float temperature, int32_t places, const float *teacher, const int32_t *teacher_tokens,
+                            int32_t rest, const float *log_sums, const float *log_rests, const float *grad_losses,
+                            void *grad_logits, int64_t grad_stride, void *hip_stream);
+
 /* Static description of a quamba_status value. */
 const char *quamba_strerror(int status);
 

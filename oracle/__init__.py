@@ -11,6 +11,7 @@ from .conv1d import conv1d_silu_f64, ref_conv1d_q8, output_scales
 from .mamba1 import ref_mamba1_scan, channel_scales
 from .fp8 import e4m3_values, e4m3_codes, quantize_fp8, dequantize_fp8, ref_fp8_matmul
 from .beam import beam_values, ref_beam_select, ref_beam_reorder
+from .logits import ref_token_logprobs, ref_token_logprobs_backward, ref_distill
 from .state_q8 import (exp_f32, cell_index_table, state_scales_from_absmax, quantize_state, ref_decode_step_q8)
 
 __all__ = ["Scales", "ref_prefill", "ref_decode_step", "build_oracle", "x_scale_table",
@@ -19,4 +20,5 @@ __all__ = ["Scales", "ref_prefill", "ref_decode_step", "build_oracle", "x_scale_
            "conv1d_silu_f64", "ref_conv1d_q8", "output_scales", "ref_mamba1_scan", "channel_scales",
            "e4m3_values", "e4m3_codes", "quantize_fp8", "dequantize_fp8", "ref_fp8_matmul",
            "beam_values", "ref_beam_select", "ref_beam_reorder",
+           "ref_token_logprobs", "ref_token_logprobs_backward", "ref_distill",
            "exp_f32", "cell_index_table", "state_scales_from_absmax", "quantize_state", "ref_decode_step_q8"]

@@ -14,6 +14,8 @@ from .binding import (QuambaError, Shape, HostScales, DeviceScales, Gate, load_l
                       quamba_hadamard_quantize, quamba_conv1d_q8, quamba_mamba1_scan, quamba_mamba1_decode_step,
                       quamba_fp8_quantize, quamba_fp8_matmul, quamba_fp8_matmul_workspace_size,
                       quamba_beam_select, quamba_beam_select_workspace_size, quamba_beam_reorder,
+                      quamba_token_logprobs, quamba_token_logprobs_workspace_size, quamba_token_logprobs_backward,
+                      quamba_distill_loss, quamba_distill_loss_workspace_size, quamba_distill_backward,
                       quamba_reorder_params, quamba_gather_rows, quamba_quantize_x, quamba_quantize_groups,
                       quamba_strerror, FLAG_GENERIC_KERNEL, FLAG_PRECISE_STATE, FLAG_NO_CHANNEL_SPLIT, FLAG_NO_DECAY_SKIP,
                       FLAG_NO_SEQ_SPLIT,
@@ -27,6 +29,8 @@ __all__ = ["QuambaError", "Shape", "HostScales", "DeviceScales", "Gate", "load_l
            "quamba_hadamard_quantize", "quamba_conv1d_q8", "quamba_mamba1_scan", "quamba_mamba1_decode_step",
            "quamba_fp8_quantize", "quamba_fp8_matmul", "quamba_fp8_matmul_workspace_size",
            "quamba_beam_select", "quamba_beam_select_workspace_size", "quamba_beam_reorder",
+           "quamba_token_logprobs", "quamba_token_logprobs_workspace_size", "quamba_token_logprobs_backward",
+           "quamba_distill_loss", "quamba_distill_loss_workspace_size", "quamba_distill_backward",
            "quamba_reorder_params", "quamba_gather_rows", "quamba_quantize_x", "quamba_quantize_groups",
            "quamba_strerror", "FLAG_GENERIC_KERNEL", "FLAG_PRECISE_STATE", "FLAG_NO_CHANNEL_SPLIT", "FLAG_NO_DECAY_SKIP",
            "FLAG_NO_SEQ_SPLIT",

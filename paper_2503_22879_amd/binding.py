@@ -31,6 +31,8 @@ EXPORTED_SYMBOLS = ("quamba_ssd_prefill_workspace_size", "quamba_ssd_prefill", "
                     "quamba_quantize_groups", "quamba_strerror",
                     "quamba_fp8_quantize", "quamba_fp8_matmul_workspace_size", "quamba_fp8_matmul",
                     "quamba_beam_select_workspace_size", "quamba_beam_select", "quamba_beam_reorder",
+                    "quamba_token_logprobs_workspace_size", "quamba_token_logprobs", "quamba_token_logprobs_backward",
+                    "quamba_distill_loss_workspace_size", "quamba_distill_loss", "quamba_distill_backward",
                     # measurement helpers of the benchmark harness (include/quamba_probe.h)
                     "quamba_probe_mfma", "quamba_probe_stream_rmw", "quamba_probe_stream_read", "quamba_probe_clock",
                     "quamba_probe_clock_xcd")
@@ -168,6 +170,20 @@ def load_library():
             [C.c_void_p] * 4 + [C.c_size_t, C.c_void_p]
         lib.quamba_beam_reorder.restype = C.c_int
         lib.quamba_beam_reorder.argtypes = [C.c_int32, C.c_int32, C.c_void_p, C.c_int32, C.POINTER(_BeamCacheStruct), C.c_void_p]
+        lib.quamba_token_logprobs_workspace_size.restype = C.c_size_t
+        lib.quamba_token_logprobs_workspace_size.argtypes = [C.c_int64, C.c_int64, C.c_int32]
+        rows = [C.c_int64, C.c_int64, C.c_void_p, C.c_int32, C.c_int64, C.c_float]  # rows, vocab, logits, type, stride, temperature
+        lib.quamba_token_logprobs.restype = C.c_int
+        lib.quamba_token_logprobs.argtypes = rows + [C.c_void_p] * 4 + [C.c_int32] + [C.c_void_p] * 3 + [C.c_size_t, C.c_void_p]
+        lib.quamba_token_logprobs_backward.restype = C.c_int
+        lib.quamba_token_logprobs_backward.argtypes = rows + [C.c_void_p] * 6 + [C.c_int64, C.c_void_p]
+        lib.quamba_distill_loss_workspace_size.restype = C.c_size_t
+        lib.quamba_distill_loss_workspace_size.argtypes = [C.c_int64, C.c_int64, C.c_int32]
+        teacher = [C.c_int32, C.c_void_p, C.c_void_p, C.c_int32]  # places, teacher, tokens, rest
+        lib.quamba_distill_loss.restype = C.c_int
+        lib.quamba_distill_loss.argtypes = rows + teacher + [C.c_void_p] * 5 + [C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p]
+        lib.quamba_distill_backward.restype = C.c_int
+        lib.quamba_distill_backward.argtypes = rows + teacher + [C.c_void_p] * 4 + [C.c_int64, C.c_void_p]
         lib.quamba_strerror.restype = C.c_char_p
         lib.quamba_strerror.argtypes = [C.c_int]
         _lib = lib
@@ -188,7 +204,8 @@ def _load_bind():
         lib.quamba_ssd_prefill_gated, lib.quamba_ssd_prefill_noalloc, lib.quamba_ssd_decode_step_gated,
         lib.quamba_ssd_decode_step_q8_gated, lib.quamba_ssd_quantize_state, lib.quamba_hadamard_quantize,
         lib.quamba_mamba1_scan_gated, lib.quamba_mamba1_decode_step_gated, lib.quamba_conv1d_q8, lib.quamba_fp8_quantize,
-        lib.quamba_fp8_matmul, lib.quamba_beam_select, lib.quamba_beam_reorder)), Shape, _ScalesStruct, _GateStruct,
+        lib.quamba_fp8_matmul, lib.quamba_beam_select, lib.quamba_beam_reorder, lib.quamba_token_logprobs,
+        lib.quamba_token_logprobs_backward, lib.quamba_distill_loss, lib.quamba_distill_backward)), Shape, _ScalesStruct, _GateStruct,
         DeviceScales, Gate, lambda p: C.cast(p, C.c_void_p).value)
     _bind = mod
     return mod
@@ -383,6 +400,59 @@ def quamba_beam_reorder(parents, caches, stream=None) -> None:
     rc = (_bind or _load_bind()).beam_reorder(parents, caches, stream)
     if rc != 0:
         raise QuambaError(rc, "quamba_beam_reorder")
+
+
+def quamba_token_logprobs_workspace_size(rows: int, vocab: int, count: int) -> int:
+    return int(load_library().quamba_token_logprobs_workspace_size(rows, vocab, count))
+
+
+def quamba_token_logprobs(logits, targets, logprobs, log_sums=None, entropies=None, top_logprobs=None, top_tokens=None,
+                          temperature: float = 1.0, workspace=None, stream=None) -> None:
+    """Enqueue logprobs = log softmax(logits / temperature) at the targets, and what else is given a tensor: the log sums of
+    exponentials and the entropies [rows], and the top_tokens.shape[1] most likely tokens [rows, count] with their log
+    probabilities.  logits [rows, vocab] in fp32, fp16 or bf16 (rows any distance apart), targets and tokens int32, all other fp32;
+    a target that is no token marks a row of padding.  targets and logprobs may both be None."""
+    rc = (_bind or _load_bind()).token_logprobs(logits, targets, logprobs, log_sums, entropies, top_logprobs, top_tokens, temperature,
+                                                workspace, stream)
+    if rc != 0:
+        raise QuambaError(rc, "quamba_token_logprobs")
+
+
+def quamba_token_logprobs_backward(logits, targets, log_sums, grad_logprobs, grad_logits, entropies=None, grad_entropies=None,
+                                   temperature: float = 1.0, stream=None) -> None:
+    """Enqueue the gradient of sum(grad_logprobs * logprobs + grad_entropies * entropies) by the logits, in their type;
+    grad_logits may be the logits.  log_sums and entropies are those of quamba_token_logprobs."""
+    rc = (_bind or _load_bind()).token_logprobs_backward(logits, targets, log_sums, grad_logprobs, grad_logits, entropies,
+                                                         grad_entropies, temperature, stream)
+    if rc != 0:
+        raise QuambaError(rc, "quamba_token_logprobs_backward")
+
+
+def quamba_distill_loss_workspace_size(rows: int, vocab: int, places: int) -> int:
+    return int(load_library().quamba_distill_loss_workspace_size(rows, vocab, places))
+
+
+def quamba_distill_loss(logits, teacher, teacher_tokens, losses, log_sums=None, log_rests=None, weights=None, grad_logits=None,
+                        rest: bool = False, temperature: float = 1.0, workspace=None, stream=None) -> None:
+    """Enqueue the distance of every row of logits [rows, vocab] (fp32, fp16 or bf16) from a teacher's most likely tokens, and with
+    grad_logits (the logits' type; it may be the logits) the gradient of sum(weights * losses).  teacher fp32 and
+    teacher_tokens int32 [rows, places]: logits, whose probabilities are made to sum to 1 over the places, or with `rest` log
+    probabilities at the temperature, all other tokens being one more outcome.  A token out of range marks an empty place, a
+    weight of 0 a row that is left out."""
+    rc = (_bind or _load_bind()).distill_loss(logits, teacher, teacher_tokens, losses, log_sums, log_rests, weights, grad_logits, rest,
+                                              temperature, workspace, stream)
+    if rc != 0:
+        raise QuambaError(rc, "quamba_distill_loss")
+
+
+def quamba_distill_backward(logits, teacher, teacher_tokens, log_sums, grad_losses, grad_logits, log_rests=None, rest: bool = False,
+                            temperature: float = 1.0, stream=None) -> None:
+    """Enqueue the gradient of sum(grad_losses * losses) by the logits from the log sums (and log rests) of quamba_distill_loss;
+    grad_logits may be the logits."""
+    rc = (_bind or _load_bind()).distill_backward(logits, teacher, teacher_tokens, log_sums, grad_losses, grad_logits, log_rests, rest,
+                                                  temperature, stream)
+    if rc != 0:
+        raise QuambaError(rc, "quamba_distill_backward")
 
 
 def quamba_reorder_params(nheads, headdim, ngroups, m, n, d_state, x_calib_absmax, B_calib_absmax,

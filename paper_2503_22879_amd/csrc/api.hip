@@ -448,6 +448,139 @@ extern "C" int quamba_beam_reorder(int32_t batch, int32_t beams, const int32_t *
     return e == hipSuccess ? QUAMBA_OK : QUAMBA_EHIP;
 }
 
+namespace {
+
+bool logits_size(int64_t rows, int64_t vocab, int32_t count, int32_t most)
+{
+    return rows >= 0 && rows <= quamba::kMaxLogitRows && vocab > 0 && vocab <= quamba::kMaxVocab && count >= 0 && count <= most;
+}
+bool rows_apart(int64_t vocab, int64_t stride) { return stride >= vocab && stride <= (int64_t)1 << 40; }
+int type_bytes(int32_t type) { return type == QUAMBA_F32 ? 4 : 2; }
+bool at_its_type(const void *p, int32_t type) { return reinterpret_cast<uintptr_t>(p) % type_bytes(type) == 0; }
+bool is_temperature(float t) { return t >= 0x1p-100f && t <= 0x1p100f; }
+
+// Whether a gradient shares memory with the logits other than by taking their place.
+bool overlaps(int64_t rows, int64_t vocab, const void *logits, int64_t stride, const void *gradient, int64_t gradient_stride, int32_t type)
+{
+    const int64_t size = type_bytes(type);
+    const uintptr_t x = reinterpret_cast<uintptr_t>(logits), g = reinterpret_cast<uintptr_t>(gradient);
+    if (g == x && (stride == gradient_stride || rows == 1)) return false;
+    if (g >= x + (uintptr_t)(((rows - 1) * stride + vocab) * size) || x >= g + (uintptr_t)(((rows - 1) * gradient_stride + vocab) * size)) return false;
+    if (stride != gradient_stride) return true;
+    const int64_t between = (int64_t)((g > x ? g - x : x - g) / size) % stride;  // columns of one matrix, side by side
+    return between < vocab || between > stride - vocab;
+}
+
+}  // namespace
+
+extern "C" size_t quamba_token_logprobs_workspace_size(int64_t rows, int64_t vocab, int32_t count)
+{
+    return logits_size(rows, vocab, count, quamba::kMaxChoices) ? quamba::token_logprobs_workspace_bytes(rows, (int32_t)vocab, count) : 0;
+}
+
+extern "C" int quamba_token_logprobs(int64_t rows, int64_t vocab, const void *logits, int32_t type, int64_t logits_stride,
+                                     float temperature, const int32_t *targets, float *logprobs, float *log_sums,
+                                     float *entropies, int32_t count, float *top_logprobs, int32_t *top_tokens,
+                                     void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    if (!logits_size(rows, vocab, count, quamba::kMaxChoices) || !rows_apart(vocab, logits_stride)) return QUAMBA_ESHAPE;
+    if (!known_type(type) || !is_temperature(temperature) || !at_its_type(logits, type)) return QUAMBA_EINVAL;
+    if (rows == 0) return QUAMBA_OK;
+    if (!logits || !targets != !logprobs || (count > 0 && (!top_logprobs || !top_tokens))) return QUAMBA_ENULL;
+    if (!logprobs && !log_sums && !entropies && count == 0) return QUAMBA_OK;
+    quamba::LogprobArgs a = {};
+    a.logits = logits; a.rows = rows; a.stride = logits_stride; a.vocab = (int32_t)vocab; a.type = type;
+    a.targets = targets; a.logprobs = logprobs; a.log_sums = log_sums; a.entropies = entropies;
+    a.count = count; a.top_logprobs = top_logprobs; a.top_tokens = top_tokens;
+    a.per_temperature = (float)(1.0 / temperature); a.c = (float)(1.44269504088896341 / temperature);
+    if (!workspace || !aligned16(workspace) || workspace_bytes < quamba_token_logprobs_workspace_size(rows, vocab, count)) workspace = nullptr;
+    const hipError_t e = quamba::launch_token_logprobs(a, workspace, static_cast<hipStream_t>(hip_stream));
+    return e == hipSuccess ? QUAMBA_OK : QUAMBA_EHIP;
+}
+
+extern "C" int quamba_token_logprobs_backward(int64_t rows, int64_t vocab, const void *logits, int32_t type,
+                                              int64_t logits_stride, float temperature, const int32_t *targets,
+                                              const float *log_sums, const float *entropies, const float *grad_logprobs,
+                                              const float *grad_entropies, void *grad_logits, int64_t grad_stride,
+                                              void *hip_stream)
+{
+    if (!logits_size(rows, vocab, 0, 0) || !rows_apart(vocab, logits_stride) || !rows_apart(vocab, grad_stride)) return QUAMBA_ESHAPE;
+    if (!known_type(type) || !is_temperature(temperature) || !at_its_type(logits, type) || !at_its_type(grad_logits, type)) return QUAMBA_EINVAL;
+    if (rows == 0) return QUAMBA_OK;
+    if (!logits || !grad_logits || !log_sums || !targets != !grad_logprobs || !entropies != !grad_entropies) return QUAMBA_ENULL;
+    if (overlaps(rows, vocab, logits, logits_stride, grad_logits, grad_stride, type)) return QUAMBA_EINVAL;
+    quamba::LogprobGradientArgs a = {};
+    a.logits = logits; a.rows = rows; a.stride = logits_stride; a.vocab = (int32_t)vocab; a.type = type;
+    a.gradient = grad_logits; a.gradient_stride = grad_stride; a.targets = targets;
+    a.log_sums = log_sums; a.entropies = entropies; a.grad_logprobs = grad_logprobs; a.grad_entropies = grad_entropies;
+    a.temperature = temperature; a.per_temperature = (float)(1.0 / temperature); a.c = (float)(1.44269504088896341 / temperature);
+    const hipError_t e = quamba::launch_token_logprobs_backward(a, static_cast<hipStream_t>(hip_stream));
+    return e == hipSuccess ? QUAMBA_OK : QUAMBA_EHIP;
+}
+
+namespace {
+
+// What the two entry points of the distillation share: their arguments, checked.
+int distill_args(quamba::DistillArgs &a, int64_t rows, int64_t vocab, const void *logits, int32_t type, int64_t logits_stride,
+                 float temperature, int32_t places, const float *teacher, const int32_t *teacher_tokens, int32_t rest,
+                 const float *weights, void *gradient, int64_t grad_stride)
+{
+    if (!logits_size(rows, vocab, places, quamba::kMaxPlaces) || places == 0 || !rows_apart(vocab, logits_stride) ||
+        (gradient && !rows_apart(vocab, grad_stride)))
+        return QUAMBA_ESHAPE;
+    if (!known_type(type) || !is_temperature(temperature) || !at_its_type(logits, type) || !at_its_type(gradient, type) || rest < 0 || rest > 1)
+        return QUAMBA_EINVAL;
+    if (rows == 0) return QUAMBA_OK;
+    if (!logits || !teacher || !teacher_tokens) return QUAMBA_ENULL;
+    if (gradient && overlaps(rows, vocab, logits, logits_stride, gradient, grad_stride, type)) return QUAMBA_EINVAL;
+    a.logits = logits; a.rows = rows; a.stride = logits_stride; a.vocab = (int32_t)vocab; a.type = type;
+    a.places = places; a.teacher = teacher; a.tokens = teacher_tokens; a.rest = rest != 0; a.weights = weights;
+    a.gradient = gradient; a.gradient_stride = grad_stride;
+    a.temperature = temperature; a.per_temperature = (float)(1.0 / temperature); a.c = (float)(1.44269504088896341 / temperature);
+    return QUAMBA_OK;
+}
+
+}  // namespace
+
+extern "C" size_t quamba_distill_loss_workspace_size(int64_t rows, int64_t vocab, int32_t places)
+{
+    return logits_size(rows, vocab, places, quamba::kMaxPlaces) && places ? quamba::distill_workspace_bytes(rows, (int32_t)vocab) : 0;
+}
+
+extern "C" int quamba_distill_loss(int64_t rows, int64_t vocab, const void *logits, int32_t type, int64_t logits_stride,
+                                   float temperature, int32_t places, const float *teacher, const int32_t *teacher_tokens,
+                                   int32_t rest, const float *weights, float *losses, float *log_sums, float *log_rests,
+                                   void *grad_logits, int64_t grad_stride, void *workspace, size_t workspace_bytes,
+                                   void *hip_stream)
+{
+    quamba::DistillArgs a = {};
+    const int rc = distill_args(a, rows, vocab, logits, type, logits_stride, temperature, places, teacher, teacher_tokens, rest, weights,
+                                grad_logits, grad_stride);
+    if (rc != QUAMBA_OK || rows == 0) return rc;
+    if (!losses) return QUAMBA_ENULL;
+    a.losses = losses; a.log_sums = log_sums; a.log_rests = log_rests;
+    if (!workspace || !aligned16(workspace) || workspace_bytes < quamba_distill_loss_workspace_size(rows, vocab, places)) workspace = nullptr;
+    const hipError_t e = quamba::launch_distill(a, workspace, static_cast<hipStream_t>(hip_stream));
+    return e == hipSuccess ? QUAMBA_OK : QUAMBA_EHIP;
+}
+
+extern "C" int quamba_distill_backward(int64_t rows, int64_t vocab, const void *logits, int32_t type, int64_t logits_stride,
+                                       float temperature, int32_t places, const float *teacher,
+                                       const int32_t *teacher_tokens, int32_t rest, const float *log_sums,
+                                       const float *log_rests, const float *grad_losses, void *grad_logits,
+                                       int64_t grad_stride, void *hip_stream)
+{
+    if (!grad_logits) grad_stride = vocab;  // the missing pointer is what is wrong
+    quamba::DistillArgs a = {};
+    const int rc = distill_args(a, rows, vocab, logits, type, logits_stride, temperature, places, teacher, teacher_tokens, rest,
+                                grad_losses, grad_logits, grad_stride);
+    if (rc != QUAMBA_OK || rows == 0) return rc;
+    if (!grad_logits || !grad_losses || !log_sums || (rest && !log_rests)) return QUAMBA_ENULL;
+    a.saved_sums = log_sums; a.saved_rests = log_rests;
+    const hipError_t e = quamba::launch_distill_backward(a, static_cast<hipStream_t>(hip_stream));
+    return e == hipSuccess ? QUAMBA_OK : QUAMBA_EHIP;
+}
+
 extern "C" const char *quamba_strerror(int status)
 {
     switch (status) {

@@ -12,7 +12,7 @@
 // small ones.
 #include <algorithm>
 
-#include "quamba_internal.h"
+#include "logits.h"
 
 namespace quamba {
 namespace {
@@ -20,24 +20,6 @@ namespace {
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kGathered = 1024;  // candidates that are ranked against each other
 constexpr int kJoined = 1024;    // candidates of a round of the second launch
-
-// Floats as whole numbers of the same order; 0 is below all (the place of what is no candidate).
-__device__ __forceinline__ uint32_t ordered(float v)
-{
-    const uint32_t b = __builtin_bit_cast(uint32_t, v);
-    return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
-}
-__device__ __forceinline__ float of_ordered(uint32_t o)
-{
-    return from_bits(o & 0x80000000u ? o ^ 0x80000000u : ~o);
-}
-
-__device__ __forceinline__ float wave_max(float v)
-{
-#pragma unroll
-    for (int d = 32; d; d >>= 1) v = fmaxf(v, __shfl_xor(v, d, 64));
-    return v;
-}
 
 // A key's uppermost 32 bits, an ordered float, decide first; 0 is no candidate.
 typedef unsigned __int128 uint128_t;
@@ -166,40 +148,6 @@ __device__ __forceinline__ bool offers(const SelectArgs &a, int row)
     const float s = a.scores[row];
     return __builtin_fabsf(s) < __builtin_inff();
 }
-
-// Sixteen bytes of logits.
-template <int TYPE>
-struct Logits {
-    static constexpr int kBytes = TYPE == QUAMBA_F32 ? 4 : 2, kCount = 16 / kBytes;
-    uint32_t w[4];
-    __device__ __forceinline__ float operator[](int i) const
-    {
-        if (TYPE == QUAMBA_F32) return from_bits(w[i]);
-        const uint32_t h = i & 1 ? w[i / 2] >> 16 : w[i / 2] & 0xffffu;
-        return TYPE == QUAMBA_BF16 ? from_bits(h << 16) : (float)__builtin_bit_cast(_Float16, (uint16_t)h);
-    }
-    __device__ __forceinline__ void load(const char *p) { __builtin_memcpy(w, p, 16); }
-    __device__ __forceinline__ void load(const char *p, int left)  // the first `left`, -infinity behind them
-    {
-        if (left >= kCount) {
-            load(p);
-            return;
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = TYPE == QUAMBA_F32 ? 0xff800000u : TYPE == QUAMBA_BF16 ? 0xff80ff80u : 0xfc00fc00u;
-#pragma unroll
-        for (int i = 0; i < kCount; ++i)
-            if (i < left) {
-                if (kBytes == 4) {
-                    __builtin_memcpy(&w[i], p + 4 * i, 4);
-                } else {
-                    uint16_t h;
-                    __builtin_memcpy(&h, p + 2 * i, 2);
-                    w[i / 2] = i & 1 ? (w[i / 2] & 0xffffu) | (uint32_t)h << 16 : (w[i / 2] & 0xffff0000u) | h;
-                }
-            }
-    }
-};
 
 // A piece of 256 E logits of a row to a workgroup.
 template <int TYPE, int E>

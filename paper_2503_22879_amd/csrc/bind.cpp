@@ -34,6 +34,10 @@ struct Entry {
     decltype(&quamba_fp8_matmul) fp8_matmul;
     decltype(&quamba_beam_select) beam_select;
     decltype(&quamba_beam_reorder) beam_reorder;
+    decltype(&quamba_token_logprobs) token_logprobs;
+    decltype(&quamba_token_logprobs_backward) token_logprobs_backward;
+    decltype(&quamba_distill_loss) distill_loss;
+    decltype(&quamba_distill_backward) distill_backward;
 } entry;
 
 // The ctypes structures that carry the shape, the scale tables and the side inputs, and the classes that are read directly:
@@ -560,6 +564,143 @@ PyObject *beam_reorder(PyObject *const *a)
     return call([&] { return entry.beam_reorder((int32_t)b, (int32_t)K, parents, (int32_t)n, caches.data(), stream); });
 }
 
+// The tensors among these arguments lie on the current device, where the call is enqueued.
+void on_current_device(std::initializer_list<PyObject *> tensors)
+{
+    const int device = c10::hip::current_device();
+    for (PyObject *o : tensors)
+        if (THPVariable_Check(o) && THPVariable_Unpack(o).get_device() != device)
+            fail(PyExc_ValueError, "every tensor must be on the current device%s", "");
+}
+
+// A workspace argument: contiguous device memory of any type, or None.
+struct Space {
+    void *p;
+    size_t bytes;
+    explicit Space(PyObject *o)
+    {
+        const at::Tensor *t = tensor_or_null(o, "workspace");
+        p = device_pointer(t, "workspace");
+        bytes = t ? (size_t)t->numel() * t->element_size() : 0;
+    }
+};
+
+// A gradient of logits x: like them, or (with `optional`) None.
+struct Gradient {
+    void *p = nullptr;
+    int64_t stride = 0;
+    Gradient(PyObject *o, const Matrix &x, bool optional)
+    {
+        if (o == Py_None && optional) return;
+        const Matrix g(o, "grad_logits");
+        g.expect(x.rows, x.cols, "grad_logits");
+        if (g.type != x.type) fail(PyExc_ValueError, "%s must have the logits' dtype", "grad_logits");
+        p = g.p;
+        stride = g.stride;
+    }
+};
+
+// [rows, count] of the tensor, which is not None.
+int32_t columns(PyObject *o, const char *name)
+{
+    const at::Tensor *t = tensor_or_null(o, name);
+    if (!t || t->dim() != 2) fail(PyExc_ValueError, "%s must be a tensor of rows and columns", name);
+    return t->size(1) > INT32_MAX ? INT32_MAX : (int32_t)t->size(1);
+}
+
+// logits, targets, logprobs, log_sums, entropies, top_logprobs, top_tokens, temperature, workspace, stream
+PyObject *token_logprobs(PyObject *const *a)
+{
+    const Matrix x(a[0], "logits");
+    const int32_t type = dtype_of(x.type, "logits");
+    on_current_device({a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[8]});
+    const int32_t *targets = pointer<int32_t>(a[1], at::kInt, {x.rows}, "targets");
+    float *logprobs = pointer<float>(a[2], at::kFloat, {x.rows}, "logprobs");
+    float *log_sums = pointer<float>(a[3], at::kFloat, {x.rows}, "log_sums");
+    float *entropies = pointer<float>(a[4], at::kFloat, {x.rows}, "entropies");
+    const int32_t count = a[6] != Py_None ? columns(a[6], "top_tokens") : a[5] != Py_None ? columns(a[5], "top_logprobs") : 0;
+    float *top_logprobs = pointer<float>(a[5], at::kFloat, {x.rows, count}, "top_logprobs");
+    int32_t *top_tokens = pointer<int32_t>(a[6], at::kInt, {x.rows, count}, "top_tokens");
+    const float temperature = number(a[7]);
+    const Space space(a[8]);
+    void *stream = stream_of(a[9]);
+    return call([&] {
+        return entry.token_logprobs(x.rows, x.cols, x.p, type, x.stride, temperature, targets, logprobs, log_sums, entropies, count,
+                                    top_logprobs, top_tokens, space.p, space.bytes, stream);
+    });
+}
+
+// logits, targets, log_sums, grad_logprobs, grad_logits, entropies, grad_entropies, temperature, stream
+PyObject *token_logprobs_backward(PyObject *const *a)
+{
+    const Matrix x(a[0], "logits");
+    const int32_t type = dtype_of(x.type, "logits");
+    on_current_device({a[0], a[1], a[2], a[3], a[4], a[5], a[6]});
+    const Gradient g(a[4], x, false);
+    const int32_t *targets = pointer<int32_t>(a[1], at::kInt, {x.rows}, "targets");
+    const float *log_sums = pointer<float>(a[2], at::kFloat, {x.rows}, "log_sums");
+    const float *grad_logprobs = pointer<float>(a[3], at::kFloat, {x.rows}, "grad_logprobs");
+    const float *entropies = pointer<float>(a[5], at::kFloat, {x.rows}, "entropies");
+    const float *grad_entropies = pointer<float>(a[6], at::kFloat, {x.rows}, "grad_entropies");
+    const float temperature = number(a[7]);
+    void *stream = stream_of(a[8]);
+    return call([&] {
+        return entry.token_logprobs_backward(x.rows, x.cols, x.p, type, x.stride, temperature, targets, log_sums, entropies, grad_logprobs,
+                                             grad_entropies, g.p, g.stride, stream);
+    });
+}
+
+int32_t truth(PyObject *o)
+{
+    const int v = PyObject_IsTrue(o);
+    if (v < 0) throw Fail();
+    return v;
+}
+
+// logits, teacher, teacher_tokens, losses, log_sums, log_rests, weights, grad_logits, rest, temperature, workspace, stream
+PyObject *distill_loss(PyObject *const *a)
+{
+    const Matrix x(a[0], "logits");
+    const int32_t type = dtype_of(x.type, "logits"), places = columns(a[1], "teacher");
+    on_current_device({a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7], a[10]});
+    const float *teacher = pointer<float>(a[1], at::kFloat, {x.rows, places}, "teacher");
+    const int32_t *tokens = pointer<int32_t>(a[2], at::kInt, {x.rows, places}, "teacher_tokens");
+    float *losses = pointer<float>(a[3], at::kFloat, {x.rows}, "losses");
+    float *log_sums = pointer<float>(a[4], at::kFloat, {x.rows}, "log_sums");
+    float *log_rests = pointer<float>(a[5], at::kFloat, {x.rows}, "log_rests");
+    const float *weights = pointer<float>(a[6], at::kFloat, {x.rows}, "weights");
+    const Gradient g(a[7], x, true);
+    const int32_t rest = truth(a[8]);
+    const float temperature = number(a[9]);
+    const Space space(a[10]);
+    void *stream = stream_of(a[11]);
+    return call([&] {
+        return entry.distill_loss(x.rows, x.cols, x.p, type, x.stride, temperature, places, teacher, tokens, rest, weights, losses, log_sums,
+                                  log_rests, g.p, g.stride, space.p, space.bytes, stream);
+    });
+}
+
+// logits, teacher, teacher_tokens, log_sums, grad_losses, grad_logits, log_rests, rest, temperature, stream
+PyObject *distill_backward(PyObject *const *a)
+{
+    const Matrix x(a[0], "logits");
+    const int32_t type = dtype_of(x.type, "logits"), places = columns(a[1], "teacher");
+    on_current_device({a[0], a[1], a[2], a[3], a[4], a[5], a[6]});
+    const float *teacher = pointer<float>(a[1], at::kFloat, {x.rows, places}, "teacher");
+    const int32_t *tokens = pointer<int32_t>(a[2], at::kInt, {x.rows, places}, "teacher_tokens");
+    const float *log_sums = pointer<float>(a[3], at::kFloat, {x.rows}, "log_sums");
+    const float *grad_losses = pointer<float>(a[4], at::kFloat, {x.rows}, "grad_losses");
+    const Gradient g(a[5], x, false);
+    const float *log_rests = pointer<float>(a[6], at::kFloat, {x.rows}, "log_rests");
+    const int32_t rest = truth(a[7]);
+    const float temperature = number(a[8]);
+    void *stream = stream_of(a[9]);
+    return call([&] {
+        return entry.distill_backward(x.rows, x.cols, x.p, type, x.stride, temperature, places, teacher, tokens, rest, log_sums, log_rests,
+                                      grad_losses, g.p, g.stride, stream);
+    });
+}
+
 template <PyObject *(*F)(PyObject *const *), int N>
 PyObject *method(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
@@ -577,7 +718,7 @@ PyObject *method(PyObject *, PyObject *const *a, Py_ssize_t n)
 // The addresses of the library's functions, in the order of Entry, and what binding.py has for the objects above.
 PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
-    constexpr int kEntries = 13;
+    constexpr int kEntries = 17;
     PyObject **const objects[] = {&shape_type, &scales_type, &gate_struct_type, &device_scales_type, &gate_type, &address_of};
     constexpr int kObjects = sizeof(objects) / sizeof(objects[0]);
     void *p[kEntries];
@@ -621,6 +762,10 @@ PyMethodDef methods[] = {
     QUAMBA_METHOD(fp8_matmul, 7),
     QUAMBA_METHOD(beam_select, 9),
     QUAMBA_METHOD(beam_reorder, 3),
+    QUAMBA_METHOD(token_logprobs, 10),
+    QUAMBA_METHOD(token_logprobs_backward, 9),
+    QUAMBA_METHOD(distill_loss, 12),
+    QUAMBA_METHOD(distill_backward, 10),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_bind", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

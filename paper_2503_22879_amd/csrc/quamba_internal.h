@@ -451,4 +451,69 @@ hipError_t launch_beam_select(const SelectArgs &a, void *workspace, hipStream_t 
 hipError_t launch_beam_reorder(int32_t batch, int32_t beams, const int32_t *parents, int32_t n, const quamba_beam_cache_t *caches,
                                hipStream_t stream);
 
+// ---- rows of logits: log probabilities of tokens, distillation ----
+constexpr int32_t kMaxVocab = 1 << 26;
+constexpr int64_t kMaxLogitRows = (int64_t)1 << 31;
+constexpr int kMaxPlaces = 128;  // of a teacher
+// A row's segments, each of so many vectors of 16 bytes.
+struct LogitsCut {
+    int segments, vectors;
+};
+LogitsCut logits_cut(int64_t rows, int32_t vocab, int32_t type);
+// What a segment leaves: its sums of exponentials against a reference logit.
+struct LogitsPart {
+    float reference, sum, second, unused;
+};
+struct LogprobArgs {
+    const void *logits;
+    int64_t rows, stride;
+    const int32_t *targets;                      // or null
+    float *logprobs, *log_sums, *entropies;      // or null
+    float *top_logprobs;
+    int32_t *top_tokens;
+    int32_t vocab, type, count;
+    float per_temperature, c;                    // 1 / T, log2(e) / T
+    // set by the launcher
+    int64_t first_row;                           // of the launch
+    LogitsPart *parts;
+    uint64_t *best;
+    Divisor by_segments;
+    int32_t segments, segment_vectors;
+};
+size_t token_logprobs_workspace_bytes(int64_t rows, int32_t vocab, int32_t count);
+hipError_t launch_token_logprobs(LogprobArgs a, void *workspace, hipStream_t stream);
+struct LogprobGradientArgs {
+    const void *logits;
+    void *gradient;
+    int64_t rows, stride, gradient_stride;
+    const int32_t *targets;                      // or null
+    const float *log_sums, *entropies, *grad_logprobs, *grad_entropies;
+    int32_t vocab, type;
+    float temperature, per_temperature, c;
+    int64_t first_row;
+    Divisor by_segments;
+    int32_t segments, segment_vectors;
+};
+hipError_t launch_token_logprobs_backward(LogprobGradientArgs a, hipStream_t stream);
+struct DistillArgs {
+    const void *logits;
+    int64_t rows, stride, gradient_stride;
+    const float *teacher;                        // [rows, places]
+    const int32_t *tokens;
+    const float *weights;                        // or null; the gradient's of each row's loss
+    float *losses, *log_sums, *log_rests;        // or null
+    const float *saved_sums, *saved_rests;       // of an earlier call, for the gradient alone
+    void *gradient;                              // or null
+    int32_t vocab, type, places;
+    bool rest;
+    float temperature, per_temperature, c;
+    int64_t first_row;
+    LogitsPart *parts;
+    Divisor by_segments;
+    int32_t segments, segment_vectors;
+};
+size_t distill_workspace_bytes(int64_t rows, int32_t vocab);
+hipError_t launch_distill(DistillArgs a, void *workspace, hipStream_t stream);
+hipError_t launch_distill_backward(DistillArgs a, hipStream_t stream);
+
 }  // namespace quamba
