@@ -577,7 +577,7 @@ extern "C" int quamba_distill_backward(int64_t rows, int64_t vocab, const void *
     if (rc != QUAMBA_OK || rows == 0) return rc;
     if (!grad_logits || !grad_losses || !log_sums || (rest && !log_rests)) return QUAMBA_ENULL;
     a.saved_sums = log_sums; a.saved_rests = log_rests;
-    const hipError_t e = quamba::launch_distill_backward(a, static_cast<hipStream_t>(hip_stream));
+    const hipError_t e = quamba::launch_distill(a, nullptr, static_cast<hipStream_t>(hip_stream));
     return e == hipSuccess ? QUAMBA_OK : QUAMBA_EHIP;
 }
 

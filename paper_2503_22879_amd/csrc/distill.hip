@@ -4,8 +4,8 @@
 //   dx_v = w / T (p_v Q - sum of the q_k with token_k = v),  Q = sum_k q_k + q_R;    of other tokens w / T (p_v / p_R) (Q p_R - q_R)
 //
 // One pass over a row makes its sum of exponentials and the other tokens' (whose own sum is exact where it is a small part of the row's: a
-// difference would not be); a second one writes the gradient as if no token were the teacher's, and then the teacher's tokens are
-// put right one by one from their logits, which were read before.  Bound: HBM.
+// difference would not be); the gradient is written as if no token were the teacher's, but for those, which come from their logits and
+// places.  Bound: HBM.
 #include <algorithm>
 
 #include "logits.h"
@@ -13,119 +13,161 @@
 namespace quamba {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256;  // but where a row is held in registers
 constexpr int64_t kRowsOfALaunch = (int64_t)1 << 22;
+constexpr int kGradientVectors = 3;  // of a thread, of the gradient alone
 constexpr float kLog2e = 1.44269504088896341f;
 
-// The teacher's places of a row, in LDS.
+// The teacher's places of a row, two to a lane; every wave reads them for itself, so none waits for another.
 struct Places {
-    float q[kMaxPlaces], log_q[kMaxPlaces], logit[kMaxPlaces];
-    int32_t token[kMaxPlaces];  // -1: an empty place
-    float wave[4][2];
-};
+    float q[2], log_q[2];
+    int token[2];  // -1: an empty place
+    float sum;     // of q
+    bool any;      // whether there is a place that is not empty
 
-// Fills them in; every thread gets the sum of q.  any: whether there is a place that is not empty.
-template <int TYPE>
-__device__ __forceinline__ float read_places(Places &s, const DistillArgs &a, int64_t row, const Row<TYPE> &x, bool &any)
-{
-    const int t = threadIdx.x, w = t / 64;
-    float value = -__builtin_inff(), logit = 0.0f, q = 0.0f;
-    int token = -1;
-    if (t < a.places) {
-        value = a.teacher[row * a.places + t];
-        token = a.tokens[row * a.places + t];
-        if ((uint32_t)token >= (uint32_t)a.vocab || value == -__builtin_inff()) {
-            token = -1;
-            value = -__builtin_inff();
-        } else {
-            logit = x.logit(token);
+    __device__ __forceinline__ Places(const DistillArgs &a, int64_t row) : Places(a, Raw(a, row)) {}
+
+    // As they lie in memory.  Loads return in order: what a wave asks for before its logits does not wait for them.
+    struct Raw {
+        float value[2];
+        int token[2];
+        __device__ __forceinline__ Raw(const DistillArgs &a, int64_t row)
+        {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int k = (threadIdx.x & 63) + 64 * h;
+                value[h] = -__builtin_inff();
+                token[h] = -1;
+                if (k < a.places) {
+                    value[h] = a.teacher[row * a.places + k];
+                    token[h] = a.tokens[row * a.places + k];
+                }
+            }
+        }
+    };
+    __device__ __forceinline__ Places(const DistillArgs &a, const Raw &raw)
+    {
+        float value[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            value[h] = raw.value[h];
+            token[h] = raw.token[h];
+            if ((uint32_t)token[h] >= (uint32_t)a.vocab || value[h] == -__builtin_inff()) {
+                token[h] = -1;
+                value[h] = -__builtin_inff();
+            }
+        }
+        any = __builtin_amdgcn_ballot_w64(token[0] >= 0 || token[1] >= 0) != 0;
+        const float top = a.rest ? 0.0f : group_max(fmaxf(value[0], value[1])), scale = a.rest ? 1.0f : a.per_temperature;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            log_q[h] = (value[h] - top) * scale;
+            q[h] = token[h] >= 0 ? expf(log_q[h]) : 0.0f;
+        }
+        sum = group_sum<64>(q[0] + q[1]);
+        if (!a.rest) {  // to sum to 1
+            const float log = logf(sum);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                log_q[h] -= log;
+                q[h] /= sum;
+            }
+            sum = group_sum<64>(q[0] + q[1]);
         }
     }
-    any = __syncthreads_or(token >= 0);
-    float log_q = value;
-    if (!a.rest) {  // to sum to 1
-        const float top = wave_max(value);
-        if (t % 64 == 0 && w < 2) s.wave[w][0] = top;
-        __syncthreads();
-        log_q = (value - fmaxf(s.wave[0][0], s.wave[1][0])) * a.per_temperature;
+    // The sum of q over all places with the token of place h of the lane: a token may have several.  By the whole wave.
+    __device__ __forceinline__ void of_tokens(int places, float (&all)[2]) const
+    {
+        all[0] = all[1] = 0.0f;
+        for (int i = 0; i < places; ++i) {
+            const int t = __builtin_amdgcn_readlane(i < 64 ? token[0] : token[1], i & 63);
+            const float p = from_bits(__builtin_amdgcn_readlane(__builtin_bit_cast(int, i < 64 ? q[0] : q[1]), i & 63));
+            all[0] += token[0] == t ? p : 0.0f;
+            all[1] += token[1] == t ? p : 0.0f;
+        }
     }
-    if (token >= 0) q = expf(log_q);
-    float sum = group_sum<64>(q);
-    if (t % 64 == 0 && w < 2) s.wave[w][1] = sum;
-    __syncthreads();
-    sum = s.wave[0][1] + s.wave[1][1];
-    if (!a.rest) {
-        log_q -= logf(sum);
-        q /= sum;
-        sum = group_sum<64>(q);
-        if (t % 64 == 0 && w < 2) s.wave[w + 2][1] = sum;
-        __syncthreads();
-        sum = s.wave[2][1] + s.wave[3][1];
-    }
-    if (t < a.places) {
-        s.q[t] = q;
-        s.log_q[t] = log_q;
-        s.logit[t] = logit;
-        s.token[t] = token;
-    }
-    __syncthreads();
-    return sum;
-}
+};
 
 // What the gradient of a row is made from: that of other tokens is flat 2^((x - reference) c - log), that of the teacher's comes from p and q.
 struct Slope {
     float reference, log, flat;
     float own_reference, own_log, whole, scale;
-    __device__ __forceinline__ float of_place(const Places &s, int places, int k, float c) const
+    template <int TYPE>
+    __device__ __forceinline__ void of_others(const Logits<TYPE> &x, float c, float (&g)[Logits<TYPE>::kCount]) const
     {
-        float q = 0.0f;  // a token may have several places
-        for (int i = 0; i < places; ++i) q += s.token[i] == s.token[k] ? s.q[i] : 0.0f;
-        return (exp2_of(fmaf(s.logit[k] - own_reference, c, -own_log)) * whole - q) * scale;
+#pragma unroll
+        for (int i = 0; i < Logits<TYPE>::kCount; ++i) g[i] = exp2_of(fmaf(x[i] - reference, c, -log)) * flat;
+    }
+    __device__ __forceinline__ float of_token(float x, float q, float c) const
+    {
+        return (exp2_of(fmaf(x - own_reference, c, -own_log)) * whole - q) * scale;
     }
 };
 
-__device__ __forceinline__ Slope slope_of(float reference, float log_sum, float rest_reference, float log_rest, float share, bool rest, float sum_q,
-                                          float scale)
+__device__ __forceinline__ Slope slope_of(const DistillArgs &a, float weight, float reference, float log_sum, float rest_reference, float log_rest,
+                                          float share, bool rest, float sum_q)
 {
     Slope s;
     const float left = rest ? fmaxf(1.0f - sum_q, 0.0f) : 0.0f;
     s.own_reference = reference;
     s.own_log = log_sum;
     s.whole = sum_q + left;
-    s.scale = scale;
+    s.scale = weight * a.per_temperature;
     s.reference = rest ? rest_reference : reference;
     s.log = rest ? log_rest : log_sum;
-    s.flat = (rest ? fmaf(s.whole, share, -left) : s.whole) * scale;
+    s.flat = (rest ? fmaf(s.whole, share, -left) : s.whole) * s.scale;
     return s;
 }
 
 // Whether the rest counts: there is a token outside the teacher's that may come (or no number).
 __device__ __forceinline__ bool has_rest(const DistillArgs &a, const ExpSum &s) { return a.rest && s.second != 0.0f; }
 
-__device__ __forceinline__ Slope slope_of(const DistillArgs &a, int64_t row, const ExpSum &s, float sum_q)
+// From a row's sums, ...
+__device__ __forceinline__ Slope slope_of(const DistillArgs &a, float weight, const ExpSum &s, float sum_q)
 {
     const float sum = s.sum > 0.0f ? s.sum : __builtin_nanf("");
-    return slope_of(s.reference, log2f(sum), s.reference, log2f(s.second), s.second / sum, has_rest(a, s), sum_q,
-                    (a.weights ? a.weights[row] : 1.0f) * a.per_temperature);
+    return slope_of(a, weight, s.reference, log2f(sum), s.reference, log2f(s.second), s.second / sum, has_rest(a, s), sum_q);
+}
+// ... and from the log sums that a call before has left.
+__device__ __forceinline__ Slope slope_of(const DistillArgs &a, float weight, int64_t row, float sum_q)
+{
+    const float sum = a.saved_sums[row], rest = a.rest ? a.saved_rests[row] : 0.0f;
+    const bool other = a.rest && rest != -__builtin_inff();
+    const Saved whole(sum, a.temperature, a.c), part(other ? rest : 0.0f, a.temperature, a.c);
+    return slope_of(a, weight, whole.reference, whole.log, part.reference, part.log, exp2_of((rest - sum) * kLog2e), other, sum_q);
 }
 
-// The losses of a row and its log sums.
-__device__ __forceinline__ void write_loss(const DistillArgs &a, int64_t row, Places &p, const ExpSum &s, float sum_q)
+__device__ __forceinline__ float weight_of(const DistillArgs &a, int64_t row) { return a.weights ? a.weights[row] : 1.0f; }
+
+// The logits at the teacher's tokens: asked for early, values late.
+template <int TYPE>
+struct TokenLogits {
+    uint32_t bits[2];
+    template <bool PAST>
+    __device__ __forceinline__ void load(const Places &p, const Row<TYPE, PAST> &x)
+    {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) bits[h] = x.bits(0, max(p.token[h], 0) + x.skip);
+    }
+    __device__ __forceinline__ float operator[](int h) const { return Row<TYPE>::value(bits[h]); }
+    // ... that are here, behind this.
+    __device__ __forceinline__ void wait() { asm volatile("" : "+v"(bits[0]), "+v"(bits[1])); }
+};
+
+// The loss of a row and its log sums, by one wave.
+template <int TYPE>
+__device__ __forceinline__ void write_loss(const DistillArgs &a, int64_t row, const Places &p, const TokenLogits<TYPE> &logit, const ExpSum &s)
 {
-    const int t = threadIdx.x, w = t / 64;
     const float log_sum = s.sum > 0.0f ? logf(s.sum) : __builtin_nanf("");
-    float term = 0.0f;
-    if (t < a.places && p.token[t] >= 0 && p.q[t] != 0.0f)
-        term = p.q[t] * (p.log_q[t] - ((p.logit[t] - s.reference) * a.per_temperature - log_sum));
-    term = group_sum<64>(term);
-    if (t % 64 == 0 && w < 2) p.wave[w][0] = term;
-    __syncthreads();
-    if (t != 0) return;
-    float loss = p.wave[0][0] + p.wave[1][0];
-    const float left = fmaxf(1.0f - sum_q, 0.0f), log_rest = logf(s.second);
+    float loss = 0.0f;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+        if (p.token[h] >= 0 && p.q[h] != 0.0f) loss += p.q[h] * (p.log_q[h] - ((logit[h] - s.reference) * a.per_temperature - log_sum));
+    loss = group_sum<64>(loss);
+    if ((threadIdx.x & 63) != 0) return;
+    const float left = fmaxf(1.0f - p.sum, 0.0f), log_rest = logf(s.second);
     if (has_rest(a, s) && left > 0.0f) loss += left * (logf(left) - (log_rest - log_sum));
-    // a sum of no number may have met no place that shows it
-    a.losses[row] = log_sum == log_sum ? loss : log_sum;
+    a.losses[row] = log_sum == log_sum ? loss : log_sum;  // a row without a distribution may have no place that shows it
     if (a.log_sums) a.log_sums[row] = fmaf(s.reference, a.per_temperature, log_sum);
     if (a.log_rests) a.log_rests[row] = a.rest ? fmaf(s.reference, a.per_temperature, log_rest) : 0.0f;
 }
@@ -137,158 +179,347 @@ __device__ __forceinline__ void write_no_loss(const DistillArgs &a, int64_t row)
     if (a.log_rests) a.log_rests[row] = 0.0f;
 }
 
-// The gradient of vectors first .. last - 1 of a row.
-template <int TYPE>
-__device__ __forceinline__ void write_slope(const DistillArgs &a, const Row<TYPE> &x, const GradientRow<TYPE> &to, const Places &p, const Slope &s,
-                                            int first, int last)
+// The gradients of the teacher's tokens in the place of what the workgroup has written there.
+template <int TYPE, bool PAST>
+__device__ __forceinline__ void put_tokens(const DistillArgs &a, const Places &p, const TokenLogits<TYPE> &logit, const Slope &slope,
+                                           const GradientRow<TYPE, PAST> &to)
 {
-    write_gradient<TYPE, kThreads, 4, false>(x, to, first, last, s.reference, a.c, s.log, s.flat, 0.0f);
     __syncthreads();
-    const int t = threadIdx.x;
-    if (t < a.places && p.token[t] >= 0) {
-        const int at = p.token[t] + x.skip;
-        if (at >= first * Logits<TYPE>::kCount && at < last * Logits<TYPE>::kCount) to.store_one(s.of_place(p, a.places, t, a.c), p.token[t]);
-    }
+    if (threadIdx.x >= 64) return;
+    float q[2];
+    p.of_tokens(a.places, q);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+        if (p.token[h] >= 0) to.store_one(slope.of_token(logit[h], q[h], a.c), p.token[h]);
 }
 
-// A segment of a row to a workgroup; where a row has one only, that is all, with the gradient.
-template <int TYPE, bool REST>
+// A bit for each logit of some vectors: whether it is the teacher's.
+template <int N>
+struct Marks {
+    uint32_t *bits;  // in LDS
+    int first;       // vector
+    __device__ __forceinline__ void clear(int vectors, int threads) const
+    {
+        for (int i = threadIdx.x; i < (vectors * N + 31) / 32; i += threads) bits[i] = 0;
+    }
+    __device__ __forceinline__ void set(const Places &p, int skip, int vectors) const  // by one wave
+    {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int at = p.token[h] + skip - first * N;
+            if (p.token[h] >= 0 && at >= 0 && at < vectors * N) atomicOr(&bits[at / 32], 1u << at % 32);
+        }
+    }
+    __device__ __forceinline__ uint32_t of(int j) const
+    {
+        const uint32_t at = (uint32_t)(j - first) * N;
+        return bits[at / 32] >> at % 32 & ((1u << N) - 1);
+    }
+};
+
+// A segment of a row to a workgroup; where a row has one only, that is all.  GRADIENT: with the gradient in a second pass, where there is no
+// workspace for what a launch behind this one would need.
+template <int TYPE, bool REST, bool PAST, bool GRADIENT>
 __global__ __launch_bounds__(kThreads) void distill_kernel(DistillArgs a)
 {
     constexpr int N = Logits<TYPE>::kCount, kRange = (1 << 17) / N;  // vectors that are marked at once
-    __shared__ Places places;
-    __shared__ uint32_t marks[REST ? (1 << 17) / 32 : 1];           // a bit for a logit: whether it is the teacher's
+    __shared__ uint32_t bits[REST ? (1 << 17) / 32 : 1];
     const int t = threadIdx.x;
     const int local = quotient((int)blockIdx.x, a.by_segments), segment = (int)blockIdx.x - local * a.segments;
     const int64_t row = a.first_row + local;
-    const Row<TYPE> x(a.logits, row * a.stride, a.vocab);
+    const Row<TYPE, PAST> x(a.logits, row * a.stride, a.vocab);
+    const GradientRow<TYPE, PAST> to(a.gradient, GRADIENT ? row * a.gradient_stride : 0, x);
     const bool alone = a.segments == 1;
-    bool live = !a.weights || a.weights[row] != 0.0f;
-    float sum_q = 0.0f;
-    if (live) sum_q = read_places(places, a, row, x, live);
-    if (!live) {
-        if (alone) {
-            write_no_loss(a, row);
-            if (a.gradient) write_zeros<TYPE, kThreads>(GradientRow<TYPE>(a.gradient, row * a.gradient_stride, x), 0, x.vectors);
-        }
+    const float weight = weight_of(a, row);
+    if (weight == 0.0f) {
+        if (alone) write_no_loss(a, row);
+        if (GRADIENT) write_zeros<kThreads>(x, to, 0, x.vectors);
         return;
     }
-    ExpSum s;
+    const Places places(a, row);
+    if (!places.any) {
+        if (alone) write_no_loss(a, row);
+        if (GRADIENT) write_zeros<kThreads>(x, to, 0, x.vectors);
+        return;
+    }
+    TokenLogits<TYPE> logit = {};
+    if (alone && t < 64) logit.load(places, x);
+    Adder<REST ? 2 : 0> adder(a.c);
     const int first = segment * a.segment_vectors, last = alone ? x.vectors : min(first + a.segment_vectors, x.vectors);
     if (REST) {
         for (int from = first; from < last; from += kRange) {
             const int to = min(from + kRange, last);
-            for (int i = t; i < ((to - from) * N + 31) / 32; i += kThreads) marks[i] = 0;
+            const Marks<N> marks{bits, from};
+            marks.clear(to - from, kThreads);
             __syncthreads();
-            if (t < a.places && places.token[t] >= 0) {
-                const int at = places.token[t] + x.skip - from * N;
-                if (at >= 0 && at < (to - from) * N) atomicOr(&marks[at / 32], 1u << at % 32);
-            }
+            if (t < 64) marks.set(places, x.skip, to - from);
             __syncthreads();
-            walk<TYPE, kThreads, 4>(x, from, to, [&](const Logits<TYPE> &v, int j) {
-                const int at = (min(j, to - 1) - from) * N;
-                add<2>(s, v, largest(v), a.c, marks[at / 32] >> at % 32 & ((1u << N) - 1));
-            });
+            const auto add = [&](const Logits<TYPE> &v, int j) { adder.add(v, marks.of(min(j, to - 1))); };
+            walk<kThreads, 4>(x, from, to, [&](const Logits<TYPE> &v, int j, int) { add(v, j); }, add);
             __syncthreads();
         }
     } else {
-        walk<TYPE, kThreads, 4>(x, first, last, [&](const Logits<TYPE> &v, int) { add<0>(s, v, largest(v), a.c); });
+        walk<kThreads, 4>(
+            x, first, last, [&](const Logits<TYPE> &v, int, int) { adder.add(v); }, [&](const Logits<TYPE> &v, int) { adder.add(v); });
     }
-    s = join<false, kThreads>(s, a.c);
-    if (!alone) {
-        if (t == 0) a.parts[blockIdx.x] = {s.reference, s.sum, s.second, 0.0f};
-        return;
+    logit.wait();  // before the barriers in join: the gradient may take the logits' place
+    const ExpSum s = join<false, kThreads>(adder.result(), a.c);
+    if (alone && t < 64) write_loss(a, row, places, logit, s);
+    if (a.parts && t == 0) a.parts[blockIdx.x] = {s.reference, s.sum, s.second, 0.0f};
+    if (GRADIENT) {
+        const Slope slope = slope_of(a, weight, s, places.sum);
+        const Span span(x, 0, x.vectors);
+        walk<kThreads, 4>(
+            x, 0, x.vectors,
+            [&](const Logits<TYPE> &v, int j, int) {
+                float g[N];
+                slope.of_others(v, a.c, g);
+                if (j < span.end) to.store(g, j);
+            },
+            [&](const Logits<TYPE> &v, int j) {
+                float g[N];
+                slope.of_others(v, a.c, g);
+                if (span.takes_end()) to.store_within(g, j);
+            });
+        put_tokens(a, places, logit, slope, to);
     }
-    write_loss(a, row, places, s, sum_q);
-    if (a.gradient) write_slope(a, x, GradientRow<TYPE>(a.gradient, row * a.gradient_stride, x), places, slope_of(a, row, s, sum_q), 0, x.vectors);
 }
 
-// A row to a workgroup: its segments' sums as one, which take the first one's place for the gradient.
+// A row to a wave: its segments' sums as one, which take the first one's place for the gradient.
 template <int TYPE>
-__global__ __launch_bounds__(kThreads) void distill_join_kernel(DistillArgs a)
+__global__ __launch_bounds__(64) void distill_join_kernel(DistillArgs a)
 {
-    __shared__ Places places;
     const int64_t row = a.first_row + blockIdx.x;
-    const Row<TYPE> x(a.logits, row * a.stride, a.vocab);
-    bool live = !a.weights || a.weights[row] != 0.0f;
-    float sum_q = 0.0f;
-    if (live) sum_q = read_places(places, a, row, x, live);
-    if (!live) {
+    const float weight = weight_of(a, row);
+    if (weight == 0.0f) {
         write_no_loss(a, row);
         return;
     }
     LogitsPart *parts = a.parts + (int64_t)blockIdx.x * a.segments;
-    const ExpSum s = join<false, kThreads>(parts, a.segments, a.c);
-    write_loss(a, row, places, s, sum_q);
+    const ExpSum s = join<false, 64>(parts, a.segments, a.c);
+    const Places places(a, row);
+    if (!places.any) {
+        write_no_loss(a, row);
+        return;
+    }
+    TokenLogits<TYPE> logit;
+    logit.load(places, Row<TYPE>(a.logits, row * a.stride, a.vocab));
+    write_loss(a, row, places, logit, s);
     if (threadIdx.x == 0) parts[0] = {s.reference, s.sum, s.second, 0.0f};
 }
 
-// A segment of a row's gradient to a workgroup: from the sums that the launches in front left, or from those of an earlier call.
-template <int TYPE>
+// A segment of a row's gradient to a workgroup: from the sums that the launches in front left, or from those of an earlier call.  One wave makes
+// what the others need, while their logits are on the way.  The teacher's tokens of the segment, mostly none to some, are put right where
+// their vector is, so that nothing is written twice.
+template <int TYPE, bool PAST>
 __global__ __launch_bounds__(kThreads) void distill_gradient_kernel(DistillArgs a)
 {
-    __shared__ Places places;
+    constexpr int N = Logits<TYPE>::kCount;
+    __shared__ int token[kMaxPlaces], shared_found;
+    __shared__ float token_q[kMaxPlaces];
+    __shared__ Slope shared_slope;
+    const int t = threadIdx.x;
     const int local = quotient((int)blockIdx.x, a.by_segments), segment = (int)blockIdx.x - local * a.segments;
     const int64_t row = a.first_row + local;
-    const Row<TYPE> x(a.logits, row * a.stride, a.vocab);
-    const GradientRow<TYPE> to(a.gradient, row * a.gradient_stride, x);
+    const Row<TYPE, PAST> x(a.logits, row * a.stride, a.vocab);
+    const GradientRow<TYPE, PAST> to(a.gradient, row * a.gradient_stride, x);
     const int first = segment * a.segment_vectors, last = min(first + a.segment_vectors, x.vectors);
-    bool live = !a.weights || a.weights[row] != 0.0f;
-    float sum_q = 0.0f;
-    if (live) sum_q = read_places(places, a, row, x, live);
-    if (!live) {
-        write_zeros<TYPE, kThreads>(to, first, last);
+    const float weight = weight_of(a, row);
+    if (weight == 0.0f) {
+        write_zeros<kThreads>(x, to, first, last);
         return;
     }
-    Slope slope;
-    if (a.saved_sums) {
-        const float sum = a.saved_sums[row], rest = a.rest ? a.saved_rests[row] : 0.0f;
-        const bool other = a.rest && rest != -__builtin_inff();
-        const Saved whole(sum, a.temperature, a.c), part(other ? rest : 0.0f, a.temperature, a.c);
-        slope = slope_of(whole.reference, whole.log, part.reference, part.log, exp2_of((rest - sum) * kLog2e), other, sum_q,
-                         (a.weights ? a.weights[row] : 1.0f) * a.per_temperature);
+    GradientSegment<kThreads, kGradientVectors, TYPE, PAST> segment_of(x, to, first, last);
+    if (t < 64) {
+        const Places places(a, row);
+        segment_of.load();
+        Slope slope;
+        if (a.saved_sums) {
+            slope = slope_of(a, weight, row, places.sum);
+        } else {
+            const LogitsPart part = a.parts[(int64_t)local * a.row_parts];
+            ExpSum s;
+            s.reference = part.reference;
+            s.sum = part.sum;
+            s.second = part.second;
+            slope = slope_of(a, weight, s, places.sum);
+        }
+        bool here[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int at = places.token[h] + x.skip;
+            here[h] = places.token[h] >= 0 && at >= first * N && at < last * N;
+        }
+        const uint64_t low = __builtin_amdgcn_ballot_w64(here[0]), high = __builtin_amdgcn_ballot_w64(here[1]);
+        const int n = __builtin_popcountll(low) + __builtin_popcountll(high);
+        if (n) {
+            float q[2];
+            places.of_tokens(a.places, q);
+            const uint64_t before = ((uint64_t)1 << t) - 1;
+            if (here[0]) {
+                const int i = __builtin_popcountll(low & before);
+                token[i] = places.token[0];
+                token_q[i] = q[0];
+            }
+            if (here[1]) {
+                const int i = __builtin_popcountll(low) + __builtin_popcountll(high & before);
+                token[i] = places.token[1];
+                token_q[i] = q[1];
+            }
+        }
+        if (t == 0) {
+            shared_found = places.any ? n : -1;
+            shared_slope = slope;
+        }
     } else {
-        const LogitsPart part = a.parts[(int64_t)local * a.segments];
-        ExpSum s;
-        s.reference = part.reference;
-        s.sum = part.sum;
-        s.second = part.second;
-        slope = slope_of(a, row, s, sum_q);
+        segment_of.load();
     }
-    write_slope(a, x, to, places, slope, first, last);
+    __syncthreads();
+    const int n = shared_found;
+    if (n < 0) {
+        write_zeros<kThreads>(x, to, first, last);
+        return;
+    }
+    const Slope slope = shared_slope;
+    segment_of.write([&](const Logits<TYPE> &v, int j, float(&g)[N]) {
+        slope.of_others(v, a.c, g);
+        for (int k = 0; k < n; ++k) {
+            const int at = token[k] - x.token(j);
+            if (at < 0 || at >= N) continue;
+            const float of_token = slope.of_token(v.at(at), token_q[k], a.c);
+#pragma unroll
+            for (int i = 0; i < N; ++i) g[i] = i == at ? of_token : g[i];
+        }
+    });
 }
 
-template <int TYPE>
-void launch_rows(const DistillArgs &a, int64_t rows, hipStream_t stream)
+// A row to a workgroup that holds it in its registers, so that it is read once for the loss and the gradient.  The row has a vector that lies inside it.
+template <int TYPE, int THREADS, int VECTORS, bool REST>
+__global__ __launch_bounds__(THREADS) void distill_resident_kernel(DistillArgs a)
+{
+    constexpr int N = Logits<TYPE>::kCount;
+    __shared__ uint32_t bits[REST ? THREADS * VECTORS * N / 32 : 1];
+    const int t = threadIdx.x;
+    const int64_t row = a.first_row + blockIdx.x;
+    const Row<TYPE, true> x(a.logits, row * a.stride, a.vocab);
+    const GradientRow<TYPE, true> to(a.gradient, row * a.gradient_stride, x);
+    const Span span(x, 0, x.vectors);
+    const float weight = weight_of(a, row);
+    if (weight == 0.0f) {
+        write_no_loss(a, row);
+        write_zeros<THREADS>(x, to, 0, x.vectors);
+        return;
+    }
+    const Places::Raw raw(a, row);
+    Held<THREADS, VECTORS, TYPE> held;
+    held.load(x, span);
+    const Marks<N> marks{bits, 0};
+    if (REST) marks.clear(x.vectors, THREADS);
+    const Places places(a, raw);
+    if (!places.any) {
+        write_no_loss(a, row);
+        write_zeros<THREADS>(x, to, 0, x.vectors);
+        return;
+    }
+    TokenLogits<TYPE> logit = {};
+    if (t < 64) logit.load(places, x);
+    if (REST) {
+        __syncthreads();
+        if (t < 64) marks.set(places, x.skip, x.vectors);
+        __syncthreads();
+    }
+    Adder<REST ? 2 : 0> adder(a.c);
+    held.go_through(span, [&](Logits<TYPE> &v, int j) {
+        if (j >= span.end) v.fill();
+        adder.add(v, REST ? marks.of(min(j, span.end - 1)) : 0u);
+    });
+    Logits<TYPE> ends = {};
+    int end = 0;
+    if (t < 64 && span.has_ends()) {
+        Ends<TYPE> loads;
+        loads.load(x, span);
+        ends = loads.vector();
+        end = loads.j;
+        adder.add(ends, REST ? marks.of(end) : 0u);
+    }
+    logit.wait();  // before the barriers in join: the gradient may take the logits' place
+    const ExpSum s = join<false, THREADS>(adder.result(), a.c);
+    if (t < 64) write_loss(a, row, places, logit, s);
+    const Slope slope = slope_of(a, weight, s, places.sum);
+    held.go_through(span, [&](const Logits<TYPE> &v, int j) {
+        float g[N];
+        slope.of_others(v, a.c, g);
+        if (j < span.end) to.store(g, j);
+    });
+    if (span.takes_end()) {
+        float g[N];
+        slope.of_others(ends, a.c, g);
+        to.store_within(g, end);
+    }
+    put_tokens(a, places, logit, slope, to);
+}
+
+template <int TYPE, bool REST>
+void launch_resident(const DistillArgs &a, int vectors, int64_t rows, hipStream_t stream)
+{
+    const int grid = (int)rows;
+    if (vectors <= 4 * 256)
+        distill_resident_kernel<TYPE, 256, 4, REST><<<grid, 256, 0, stream>>>(a);
+    else if (vectors <= 4 * 1024)
+        distill_resident_kernel<TYPE, 1024, 4, REST><<<grid, 1024, 0, stream>>>(a);
+    else if (vectors <= 8 * 1024)
+        distill_resident_kernel<TYPE, 1024, 8, REST><<<grid, 1024, 0, stream>>>(a);
+    else
+        distill_resident_kernel<TYPE, 1024, 16, REST><<<grid, 1024, 0, stream>>>(a);
+}
+
+template <int TYPE, bool PAST>
+void launch_sums(const DistillArgs &a, int64_t rows, hipStream_t stream)
 {
     const int grid = (int)(rows * a.segments);
-    if (a.rest)
-        distill_kernel<TYPE, true><<<grid, kThreads, 0, stream>>>(a);
+    if (a.gradient && !a.parts)
+        (a.rest ? distill_kernel<TYPE, true, PAST, true> : distill_kernel<TYPE, false, PAST, true>)<<<grid, kThreads, 0, stream>>>(a);
     else
-        distill_kernel<TYPE, false><<<grid, kThreads, 0, stream>>>(a);
-    if (a.segments == 1) return;
-    distill_join_kernel<TYPE><<<(int)rows, kThreads, 0, stream>>>(a);
-    if (a.gradient) distill_gradient_kernel<TYPE><<<grid, kThreads, 0, stream>>>(a);
+        (a.rest ? distill_kernel<TYPE, true, PAST, false> : distill_kernel<TYPE, false, PAST, false>)<<<grid, kThreads, 0, stream>>>(a);
+    if (a.segments > 1) distill_join_kernel<TYPE><<<(int)rows, 64, 0, stream>>>(a);
 }
 
-template <int TYPE>
-void launch_gradient(const DistillArgs &a, int64_t rows, hipStream_t stream)
-{
-    distill_gradient_kernel<TYPE><<<(int)(rows * a.segments), kThreads, 0, stream>>>(a);
-}
-
-template <typename F>
-hipError_t by_launches(DistillArgs &a, const LogitsCut &cut, const F &launch)
+void cut_into(DistillArgs &a, const LogitsCut &cut)
 {
     a.segments = cut.segments;
     a.segment_vectors = cut.vectors;
     a.by_segments = divisor((uint32_t)cut.segments);
-    for (a.first_row = 0; a.first_row < a.rows; a.first_row += kRowsOfALaunch) {
-        launch(std::min(a.rows - a.first_row, kRowsOfALaunch));
+}
+
+template <int TYPE, bool PAST>
+hipError_t launch(DistillArgs a, void *workspace, hipStream_t stream)
+{
+    const int vectors = (a.vocab + 2 * Logits<TYPE>::kCount - 2) / Logits<TYPE>::kCount;  // the most that a row's address may make of it
+    const bool sums = !a.saved_sums, resident = sums && a.gradient && vectors <= 16 * 1024 && a.vocab >= 2 * Logits<TYPE>::kCount;
+    const LogitsCut cut = workspace ? logits_cut(a.rows, a.vocab, TYPE) : LogitsCut{1, 0}, gradient = gradient_cut(a.vocab, TYPE, kThreads * kGradientVectors);
+    a.parts = static_cast<LogitsPart *>(workspace);
+    a.row_parts = cut.segments;
+    const int64_t most = a.gradient && !resident ? kRowsOfALaunch / gradient.segments : kRowsOfALaunch;
+    for (a.first_row = 0; a.first_row < a.rows; a.first_row += most) {
+        const int64_t rows = std::min(a.rows - a.first_row, most);
+        if (resident) {
+            a.rest ? launch_resident<TYPE, true>(a, vectors, rows, stream) : launch_resident<TYPE, false>(a, vectors, rows, stream);
+        } else {
+            cut_into(a, cut);
+            if (sums) launch_sums<TYPE, PAST>(a, rows, stream);
+            cut_into(a, gradient);
+            if (a.gradient && (a.parts || !sums)) distill_gradient_kernel<TYPE, PAST><<<(int)(rows * a.segments), kThreads, 0, stream>>>(a);
+        }
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
+}
+
+template <int TYPE>
+hipError_t launch(const DistillArgs &a, void *workspace, hipStream_t stream)
+{
+    return logits_past_caches(a.rows, a.vocab, TYPE) ? launch<TYPE, true>(a, workspace, stream) : launch<TYPE, false>(a, workspace, stream);
 }
 
 }  // namespace
@@ -297,33 +528,18 @@ size_t distill_workspace_bytes(int64_t rows, int32_t vocab)
 {
     size_t most = 0;  // over the types
     for (const int type : {QUAMBA_F32, QUAMBA_BF16}) {
-        const int segments = logits_cut(rows, vocab, type).segments;
-        if (segments > 1) most = std::max(most, (size_t)rows * segments * sizeof(LogitsPart));
+        most = std::max(most, (size_t)rows * logits_cut(rows, vocab, type).segments * sizeof(LogitsPart));
     }
     return most;
 }
 
-hipError_t launch_distill(DistillArgs a, void *workspace, hipStream_t stream)
+hipError_t launch_distill(const DistillArgs &a, void *workspace, hipStream_t stream)
 {
-    a.parts = static_cast<LogitsPart *>(workspace);
-    return by_launches(a, workspace ? logits_cut(a.rows, a.vocab, a.type) : LogitsCut{1, 0}, [&](int64_t rows) {
-        switch (a.type) {
-            case QUAMBA_F32: launch_rows<QUAMBA_F32>(a, rows, stream); break;
-            case QUAMBA_F16: launch_rows<QUAMBA_F16>(a, rows, stream); break;
-            default: launch_rows<QUAMBA_BF16>(a, rows, stream); break;
-        }
-    });
-}
-
-hipError_t launch_distill_backward(DistillArgs a, hipStream_t stream)
-{
-    return by_launches(a, logits_cut(a.rows, a.vocab, a.type), [&](int64_t rows) {
-        switch (a.type) {
-            case QUAMBA_F32: launch_gradient<QUAMBA_F32>(a, rows, stream); break;
-            case QUAMBA_F16: launch_gradient<QUAMBA_F16>(a, rows, stream); break;
-            default: launch_gradient<QUAMBA_BF16>(a, rows, stream); break;
-        }
-    });
+    switch (a.type) {
+        case QUAMBA_F32: return launch<QUAMBA_F32>(a, workspace, stream);
+        case QUAMBA_F16: return launch<QUAMBA_F16>(a, workspace, stream);
+        default: return launch<QUAMBA_BF16>(a, workspace, stream);
+    }
 }
 
 }  // namespace quamba

@@ -24,6 +24,19 @@ __device__ __forceinline__ float wave_max(float v)
     return v;
 }
 
+// The same, mostly by moves between lanes that are part of an operation.
+__device__ __forceinline__ float group_max(float v)
+{
+    v = fmaxf(v, dpp_move<0xB1>(v));   // the steps of group_sum
+    v = fmaxf(v, dpp_move<0x4E>(v));
+    v = fmaxf(v, dpp_move<0x141>(v));
+    v = fmaxf(v, dpp_move<0x140>(v));
+    v = fmaxf(v, __builtin_bit_cast(float, __builtin_amdgcn_ds_swizzle(__builtin_bit_cast(int, v), 0x401F)));
+    return fmaxf(v, __shfl_xor(v, 32, 64));
+}
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
 // Sixteen bytes of logits.
 template <int TYPE>
 struct Logits {
@@ -35,22 +48,31 @@ struct Logits {
         const uint32_t h = i & 1 ? w[i / 2] >> 16 : w[i / 2] & 0xffffu;
         return TYPE == QUAMBA_BF16 ? from_bits(h << 16) : (float)__builtin_bit_cast(_Float16, (uint16_t)h);
     }
+    __device__ __forceinline__ float at(int i) const  // of an i that is known at run time only: by selections, not from memory
+    {
+        const int word = i * kBytes / 4;
+        uint32_t a = w[0], b = w[1], c = w[2], d = w[3];
+        asm("" : "+v"(a), "+v"(b), "+v"(c), "+v"(d));  // a choice between them, and not between their addresses
+        Logits one;
+        one.w[0] = word < 2 ? (word < 1 ? a : b) : (word < 3 ? c : d);
+        return kBytes == 2 && i & 1 ? one[1] : one[0];
+    }
     __device__ __forceinline__ void load(const char *p) { __builtin_memcpy(w, p, 16); }
+    __device__ __forceinline__ void fill()  // with -infinity
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = TYPE == QUAMBA_F32 ? 0xff800000u : TYPE == QUAMBA_BF16 ? 0xff80ff80u : 0xfc00fc00u;
+    }
     __device__ __forceinline__ void load(const char *p, int left)  // the first `left`, -infinity behind them
     {
         if (left >= kCount) {
             load(p);
             return;
         }
-        load(p, 0, left);
-    }
-    __device__ __forceinline__ void load(const char *p, int from, int to)  // those from `from` to `to`, -infinity around them
-    {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = TYPE == QUAMBA_F32 ? 0xff800000u : TYPE == QUAMBA_BF16 ? 0xff80ff80u : 0xfc00fc00u;
+        fill();
 #pragma unroll
         for (int i = 0; i < kCount; ++i)
-            if (i >= from && i < to) {
+            if (i < left) {
                 if (kBytes == 4) {
                     __builtin_memcpy(&w[i], p + 4 * i, 4);
                 } else {
@@ -63,8 +85,9 @@ struct Logits {
 };
 
 // A row of logits as vectors of 16 bytes that lie at multiples of 16 bytes, whatever the row's address: vector j holds the logits from
-// j * kCount - skip on; what the first and the last hold around the row reads as -infinity.
-template <int TYPE>
+// j * kCount - skip on; what the first and the last hold around the row reads as -infinity.  PAST: the row is not to stay in the
+// caches.
+template <int TYPE, bool PAST = false>
 struct Row {
     static constexpr int kCount = Logits<TYPE>::kCount, kBytes = Logits<TYPE>::kBytes;
     const char *base;  // of vector 0
@@ -77,57 +100,121 @@ struct Row {
         vectors = (vocab + skip + kCount - 1) / kCount;
     }
     __device__ __forceinline__ int token(int j) const { return j * kCount - skip; }  // of vector j's first logit
-    // vectors first .. last - 1 lie inside the row
-    __device__ __forceinline__ bool whole(int first, int last) const { return (first > 0 || skip == 0) && last * kCount - skip <= vocab; }
-    __device__ __forceinline__ void load(Logits<TYPE> &v, int j) const { v.load(base + (int64_t)j * 16); }
-    __device__ __forceinline__ void load(Logits<TYPE> &v, int j, int last) const  // vector j of those before `last`
+    __device__ __forceinline__ void load(Logits<TYPE> &v, int j) const  // inside the row
     {
-        const int from = j == 0 ? skip : 0, to = j < last ? min(kCount, vocab - token(j)) : 0;
-        if (from == 0 && to == kCount)
-            load(v, j);
-        else
-            v.load(base + (int64_t)j * 16, from, to);
+        const u32x4 *p = reinterpret_cast<const u32x4 *>(base + (uint32_t)j * 16u);
+        const u32x4 w = PAST ? __builtin_nontemporal_load(p) : *p;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v.w[i] = w[i];
     }
-    __device__ __forceinline__ float logit(int t) const
+    // The bits of logit k of vector j.
+    __device__ __forceinline__ uint32_t bits(int j, int k) const
     {
-        const char *p = base + ((int64_t)t + skip) * kBytes;
-        if (TYPE == QUAMBA_F32) return *reinterpret_cast<const float *>(p);
-        const uint16_t h = *reinterpret_cast<const uint16_t *>(p);
-        return TYPE == QUAMBA_BF16 ? from_bits((uint32_t)h << 16) : (float)__builtin_bit_cast(_Float16, h);
+        const char *p = base + (uint32_t)j * 16u;
+        return kBytes == 4 ? reinterpret_cast<const uint32_t *>(p)[k] : reinterpret_cast<const uint16_t *>(p)[k];
+    }
+    static __device__ __forceinline__ float value(uint32_t bits)
+    {
+        return TYPE == QUAMBA_F32 ? from_bits(bits) : TYPE == QUAMBA_BF16 ? from_bits(bits << 16) : (float)__builtin_bit_cast(_Float16, (uint16_t)bits);
+    }
+    __device__ __forceinline__ float logit(int t) const { return value(bits(0, t + skip)); }
+};
+
+// What of vectors first .. last - 1 lies inside the row, and whether its first or last vector, across the row's ends, are among them.
+struct Span {
+    int begin, end;  // inside
+    int whole;       // the row's last vector, or the one behind it
+    bool head, tail;
+    Span() = default;
+    template <typename Row>
+    __device__ __forceinline__ Span(const Row &row, int first, int last)
+    {
+        head = first == 0 && row.skip > 0;
+        whole = (row.vocab + row.skip) / Row::kCount;
+        begin = head ? 1 : first;
+        end = min(last, whole);
+        tail = first < last && last > whole && (whole > 0 || !head);
+    }
+    __device__ __forceinline__ bool has_ends() const { return head || tail; }
+    __device__ __forceinline__ bool takes_end() const { return (head && threadIdx.x == 0) || (tail && threadIdx.x == 1); }
+};
+
+// The ends of a span, in a wave: the head in lane 0, the tail in lane 1, -infinity in the others.  All loads go together.
+template <int TYPE>
+struct Ends {
+    uint32_t bits[Logits<TYPE>::kCount];
+    int j, lo, hi;  // the vector, and which of its logits are the row's
+    template <bool PAST>
+    __device__ __forceinline__ void load(const Row<TYPE, PAST> &row, const Span &span)
+    {
+        constexpr int N = Logits<TYPE>::kCount;
+        const int t = threadIdx.x;
+        const bool at_tail = span.tail && (t == 1 || !span.head);
+        j = at_tail ? span.whole : 0;
+        lo = j == 0 ? row.skip : 0;
+        hi = min(N, row.vocab + row.skip - j * N);
+#pragma unroll
+        for (int i = 0; i < N; ++i) bits[i] = row.bits(j, min(max(i, lo), hi - 1));
+        if (t != (at_tail ? 1 : 0)) hi = lo;  // not this lane's
+    }
+    __device__ __forceinline__ Logits<TYPE> vector() const
+    {
+        Logits<TYPE> v;
+        v.fill();
+#pragma unroll
+        for (int i = 0; i < Logits<TYPE>::kCount; ++i)
+            if (i >= lo && i < hi) {
+                if (Logits<TYPE>::kBytes == 4)
+                    v.w[i] = bits[i];
+                else
+                    v.w[i / 2] = i & 1 ? (v.w[i / 2] & 0xffffu) | bits[i] << 16 : (v.w[i / 2] & 0xffff0000u) | bits[i];
+            }
+        return v;
     }
 };
 
-// Vectors first .. last - 1 of a row by a workgroup of THREADS: each(v, j) for vector j, in every thread as often, with -infinity where
-// there is none.  U vectors of a thread are on their way while the U before them are worked on.
-template <int TYPE, int THREADS, int U, typename Each>
-__device__ __forceinline__ void walk(const Row<TYPE> &row, int first, int last, const Each &each)
+// Vectors first .. last - 1 of a row by a workgroup of THREADS: each(v, j, u) for those that lie inside the row, the vectors of a thread in
+// rising order, u = 0 .. U - 1 in turn; in every thread of a wave as often, with -infinity where there is none.  At last end(v, j) for the row's first and last vector, where
+// they lie across its ends, in the first wave (Span::takes_end).
+//
+// U loads of a thread are on their way together, and what follows them waits for one after the other; there is no branch between a load
+// and its use, since behind one the compiler waits for all loads.  The next U are not asked for ahead: with 8 waves to a SIMD the other
+// waves' work is as long as the memory takes.
+template <int THREADS, int U, int TYPE, bool PAST, typename Each, typename End>
+__device__ __forceinline__ void walk(const Row<TYPE, PAST> &row, int first, int last, const Each &each, const End &end)
 {
     constexpr int kStep = THREADS * U;
     const int t = threadIdx.x;
-    auto fetch = [&](Logits<TYPE>(&v)[U], int from) {
-        if (from + kStep <= last && row.whole(from, from + kStep)) {
+    const Span span(row, first, last);
+    int from = span.begin;
+    for (; from + kStep <= span.end; from += kStep) {
+        Logits<TYPE> v[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) row.load(v[u], from + u * THREADS + t);
-        } else {
+        for (int u = 0; u < U; ++u) row.load(v[u], from + u * THREADS + t);
 #pragma unroll
-            for (int u = 0; u < U; ++u) row.load(v[u], from + u * THREADS + t, last);
-        }
-    };
-    Logits<TYPE> v[U], next[U];
-    if (first < last) fetch(v, first);
-    for (int from = first; from < last; from += kStep) {
-        if (from + kStep < last) fetch(next, from + kStep);
+        for (int u = 0; u < U; ++u) each(v[u], from + u * THREADS + t, u);
+    }
+    if (from < span.end) {
+        Logits<TYPE> v[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) each(v[u], from + u * THREADS + t);
+        for (int u = 0; u < U; ++u) row.load(v[u], min(from + u * THREADS + t, span.end - 1));
 #pragma unroll
-        for (int u = 0; u < U; ++u) v[u] = next[u];
+        for (int u = 0; u < U; ++u)
+            if (from + u * THREADS < span.end) {
+                if (from + u * THREADS + t >= span.end) v[u].fill();
+                each(v[u], from + u * THREADS + t, u);
+            }
+    }
+    if (t < 64 && span.has_ends()) {
+        Ends<TYPE> ends;
+        ends.load(row, span);
+        end(ends.vector(), ends.j);
     }
 }
 
-// A sum of exponentials, of e = (x - reference) c and to the base 2, for c = log2(e) / temperature.  The reference is a logit that was among
-// the largest when it was met: it is replaced only by one whose exponential would be above 2^8, so the sum is hardly ever rescaled, e
-// stays as small as its rounding asks for, and what is lost beside the sum is below 2^-126.  (A difference first and then the factor: x c alone may leave fp32's range,
-// and its rounding grows with x.)
+// A sum of exponentials 2^e, e = (x - reference) c with c = log2(e) / temperature.  The reference is a logit that was among the largest when
+// it was met: it is replaced only where an exponential would be above some 2^8, so the sum is hardly ever rescaled, e stays as small
+// as its rounding asks for, and what is lost beside the sum is below 2^-126.
 struct ExpSum {
     float reference = -__FLT_MAX__;
     float sum = 0.0f;     // NaN where the logits hold a NaN or +infinity
@@ -156,31 +243,68 @@ __device__ __forceinline__ float largest(const Logits<TYPE> &v)
     return m;
 }
 
-// Takes a vector of logits whose largest is `top` into the sum.  SECOND: 0 none, 1 times e, 2 without the logits whose bit in
-// `without` is set.
-template <int SECOND, int TYPE>
-__device__ __forceinline__ void add(ExpSum &s, const Logits<TYPE> &v, float top, float c, uint32_t without = 0)
-{
-    constexpr int N = Logits<TYPE>::kCount;
-    if ((top - s.reference) * c > 8.0f) rebase<SECOND == 1>(s, top, c);
-    float part = 0.0f, kept = 0.0f;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const float e = (v[i] - s.reference) * c, p = exp2_of(e);
-        part += p;
-        if (SECOND == 1) s.second = fmaf(p, fmaxf(e, kFarBelow), s.second);
+// A thread's sum while it grows.  SECOND: 0 none, 1 times e, 2 without the logits that are marked.  Mostly e is made by one operation, x c -
+// offset with offset = reference c: the product is not rounded, and what the offset's rounding leaves is the same for all terms, so it
+// is taken out at the end.  A vector for which the reference is too low (its sum shows it, so no largest logit is sought), one without an
+// entropy's term (0 times infinity), and all where reference c leaves fp32's range are made from the difference.
+template <int SECOND>
+struct Adder {
+    ExpSum s;
+    float c, offset = -__builtin_inff();  // -infinity: there is none
+    __device__ __forceinline__ explicit Adder(float c_) : c(c_) {}
+
+    __device__ __forceinline__ float residue() const { return offset > -__builtin_inff() ? fmaf(s.reference, c, -offset) : 0.0f; }
+    // e without the offset's residue, or with it
+    __device__ __forceinline__ void shift(float by)
+    {
+        const float f = exp2_of(by);
+        s.second = f * (SECOND == 1 ? fmaf(by, s.sum, s.second) : s.second);
+        s.sum *= f;
     }
-    if (SECOND == 2) {
-        kept = part;
-        if (without) {
-            kept = 0.0f;
+    __device__ __forceinline__ ExpSum result()
+    {
+        shift(-residue());
+        offset = -__builtin_inff();
+        return s;
+    }
+    template <int TYPE>
+    __device__ __forceinline__ void add(const Logits<TYPE> &v, uint32_t marked = 0)
+    {
+        constexpr int N = Logits<TYPE>::kCount;
+        float part = 0.0f, weighted = s.second;
 #pragma unroll
-            for (int i = 0; i < N; ++i) kept += without >> i & 1 ? 0.0f : exp2_of((v[i] - s.reference) * c);
+        for (int i = 0; i < N; ++i) {
+            const float e = fmaf(v[i], c, -offset), p = exp2_of(e);
+            part += p;
+            if (SECOND == 1) weighted = fmaf(p, e, weighted);
         }
-        s.second += kept;
+        if (!(part <= 256.0f * N) || (SECOND == 1 && weighted != weighted) || (SECOND == 2 && marked)) {
+            const float top = largest(v);
+            if ((top - s.reference) * c > 8.0f) {
+                result();
+                rebase<SECOND == 1>(s, top, c);
+                if (__builtin_fabsf(top * c) < 0x1p100f) offset = top * c;
+                shift(residue());
+            }
+            const float r = residue();
+            float kept = 0.0f;
+            part = 0.0f;
+            weighted = s.second;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float e = fmaf(v[i] - s.reference, c, r), p = exp2_of(e);
+                part += p;
+                if (SECOND == 1) weighted = fmaf(p, fmaxf(e, kFarBelow), weighted);
+                if (SECOND == 2) kept += marked >> i & 1 ? 0.0f : p;
+            }
+            if (SECOND == 2) s.second += kept;
+        } else if (SECOND == 2) {
+            s.second += part;
+        }
+        s.sum += part;
+        if (SECOND == 1) s.second = weighted;
     }
-    s.sum += part;
-}
+};
 
 // The sums of a workgroup's threads as one, in every thread.
 template <bool ENTROPY, int THREADS>
@@ -189,7 +313,7 @@ __device__ __forceinline__ ExpSum join(ExpSum s, float c)
     constexpr int kWaves = THREADS / 64;
     __shared__ float wave[3][kWaves];
     const int w = threadIdx.x / 64;
-    rebase<ENTROPY>(s, wave_max(s.reference), c);
+    rebase<ENTROPY>(s, group_max(s.reference), c);
     s.sum = group_sum<64>(s.sum);
     s.second = group_sum<64>(s.second);
     if (kWaves == 1) return s;
@@ -237,15 +361,38 @@ __device__ __forceinline__ ExpSum join(const LogitsPart *parts, int segments, fl
     return join<ENTROPY, THREADS>(s, c);
 }
 
-// The best tokens that a wave has met, as keys: the ordered logit above, the complement of the token below, so that of equal logits the
-// lower token is the larger key; -0 counts as 0.  Keys are gathered in LDS, and when little room is left the `count` largest are kept; from
-// then on only logits above the least of them are looked at, so that few of a long row are.
-constexpr int kListed = 256;
+// The best tokens that a workgroup has met, as keys: the ordered logit above, the complement of the token below, so that of equal logits the
+// lower token is the larger key; -0 counts as 0.  Every wave gathers keys in LDS, and when little room is left it keeps its `count` largest.
+// Only logits above a bound are looked at, which at least `count` logits reach: first as many lanes' largest of one vector, then the least
+// that is kept; the waves know the highest of their bounds.  So few of a long row are gathered.
+constexpr int kListed = 256;  // keys of a wave
+constexpr int kTurns = 4;     // of a walk that the best tokens are sought after
+template <int WAVES>
+struct TopKeys {  // in LDS
+    uint64_t keys[WAVES][kListed];
+    uint64_t all[WAVES * kMaxChoices];
+    uint32_t bound;  // ordered; some keys of a wave that has set it are above, `count` of them
+    int n, groups;
+    uint32_t tops[256];
+    uint16_t group[WAVES * 64 * kTurns];
+};
+__device__ __forceinline__ float next_below(float v) { return of_ordered(ordered(v + 0.0f) - (v == 0.0f ? 2 : 1)); }  // below 0 is not -0
+
+template <int WAVES>
 struct TopList {
-    uint64_t *keys;  // of kListed, the wave's own
-    int count, n;
-    float bound;     // candidates are above
-    __device__ __forceinline__ TopList(uint64_t *keys_, int count_) : keys(keys_), count(count_), n(0), bound(-__builtin_inff()) {}
+    TopKeys<WAVES> &shared;
+    uint64_t *keys;  // the wave's own
+    int count, n = 0;
+    float bound = -__builtin_inff();  // candidates are above
+
+    // The workgroup waits before it offers.
+    __device__ __forceinline__ TopList(TopKeys<WAVES> &shared_, int count_) : shared(shared_), keys(shared_.keys[threadIdx.x / 64]), count(count_)
+    {
+        if (threadIdx.x == 0) {
+            shared.bound = 0;
+            shared.n = 0;
+        }
+    }
 
     // Keeps the `count` largest of more.
     __device__ __forceinline__ void shrink()
@@ -254,18 +401,25 @@ struct TopList {
         uint64_t mine[kListed / 64];
 #pragma unroll
         for (int i = 0; i < kListed / 64; ++i) mine[i] = i * 64 + lane < n ? keys[i * 64 + lane] : 0;
-        auto reach = [&](uint64_t least) {
+        uint64_t least = 0;  // a number that `count` keys reach: the largest, or one that exactly so many do
+        uint32_t high = 0;   // first among the upper halves
+        bool exact = false;
+        for (int bit = 31; bit >= 0 && !exact; --bit) {
+            const uint32_t higher = high | 1u << bit;
             int r = 0;
 #pragma unroll
-            for (int i = 0; i < kListed / 64; ++i) r += __builtin_popcountll(__builtin_amdgcn_ballot_w64(mine[i] >= least));
-            return r;
-        };
-        uint64_t least = 0;  // the largest number that `count` keys reach, or one that exactly so many do
-        for (int bit = 63; bit >= 0; --bit) {
+            for (int i = 0; i < kListed / 64; ++i) r += __builtin_popcountll(__builtin_amdgcn_ballot_w64((uint32_t)(mine[i] >> 32) >= higher));
+            if (r >= count) high = higher;
+            exact = r == count;
+        }
+        least = (uint64_t)high << 32;
+        for (int bit = 31; bit >= 0 && !exact; --bit) {
             const uint64_t higher = least | (uint64_t)1 << bit;
-            const int r = reach(higher);
+            int r = 0;
+#pragma unroll
+            for (int i = 0; i < kListed / 64; ++i) r += __builtin_popcountll(__builtin_amdgcn_ballot_w64(mine[i] >= higher));
             if (r >= count) least = higher;
-            if (r == count) break;
+            exact = r == count;
         }
         uint32_t low = 0xffffffffu;
         int at = 0;
@@ -285,33 +439,175 @@ struct TopList {
         for (int d = 32; d; d >>= 1) low = min(low, (uint32_t)__shfl_xor((int)low, d, 64));
         n = at;
         bound = of_ordered(low);
+        tell(next_below(bound));
     }
 
-    // Candidates value(e) with their keys key(e), e < E, of which `top` is the lane's largest; called by the whole wave.  RISING: every later call's
-    // tokens are above all of this one's, so equals of the least that is kept are no candidates there.
+    // `count` keys of this wave are above this.
+    __device__ __forceinline__ void tell(float b)
+    {
+        if (WAVES > 1 && (threadIdx.x & 63) == 0) atomicMax(&shared.bound, ordered(b));
+    }
+
+    // Candidates value(e) with their keys key(e), e < E, of which `top` is the lane's largest; called by the whole wave.  RISING: the tokens are above
+    // all that were offered before, so equals of the least that is kept are no candidates.
     template <int E, bool RISING, typename Value, typename Key>
     __device__ __forceinline__ void offer(float top, const Value &value, const Key &key)
     {
-        if (!__builtin_amdgcn_ballot_w64(top > bound)) return;
+        if (!RISING && bound > -__builtin_inff()) bound = next_below(bound);
+        if (__builtin_expect(!__builtin_amdgcn_ballot_w64(top > bound), 1)) return;
         const int lane = threadIdx.x & 63;
-        float above = bound;
+        if (WAVES > 1) {
+            const uint32_t b = __builtin_amdgcn_readfirstlane(*(volatile uint32_t *)&shared.bound);
+            if (b) bound = fmaxf(bound, of_ordered(b));
+        }
+        if (n < count && count <= 64) {
+            const uint32_t mine = top > -__builtin_inff() ? ordered(top + 0.0f) : 0u;
+            uint32_t reached = 0;  // by `count` lanes
 #pragma unroll
+            for (int bit = 31; bit >= 16; --bit) {
+                const uint32_t higher = reached | 1u << bit;
+                if (__builtin_popcountll(__builtin_amdgcn_ballot_w64(mine >= higher)) >= count) reached = higher;
+            }
+            if (reached > ordered(-__FLT_MAX__)) {
+                const float b = next_below(of_ordered(reached));
+                if (b > bound) {
+                    bound = b;
+                    tell(b);
+                }
+            }
+        }
+        float above = bound;
+#pragma unroll 1
         for (int e = 0; e < E; ++e) {
             const float v = value(e);
             uint64_t those = __builtin_amdgcn_ballot_w64(v > above);
             if (!those) continue;
             if (n > kListed - 64) {
                 shrink();
-                above = of_ordered(ordered(bound) - (bound == 0.0f ? 2 : 1));  // the next below, which is not -0
+                above = next_below(bound);
                 those = __builtin_amdgcn_ballot_w64(v > above);
             }
             if (v > above) keys[n + __builtin_popcountll(those & (((uint64_t)1 << lane) - 1))] = key(e);
             n += __builtin_popcountll(those);
         }
-        if (!RISING && bound > -__builtin_inff()) bound = above;
+    }
+
+    // The workgroup's best: out(i, key) for the i-th largest, i < count, 0 where there are no more.
+    template <typename Out>
+    __device__ __forceinline__ void ranked(const Out &out)
+    {
+        const int lane = threadIdx.x & 63;
+        if (n > (count < 64 ? 64 : count)) shrink();
+        __syncthreads();
+        const uint32_t least = shared.bound;
+        for (int i = 0; i < n; i += 64) {  // what may be among the best of all waves, one behind the other
+            const uint64_t key = i + lane < n ? keys[i + lane] : 0;
+            const bool is = (uint32_t)(key >> 32) > least;
+            const uint64_t those = __builtin_amdgcn_ballot_w64(is);
+            int at = 0;
+            if (lane == 0 && those) at = atomicAdd(&shared.n, __builtin_popcountll(those));
+            at = __builtin_amdgcn_readfirstlane(at);
+            if (is) shared.all[at + __builtin_popcountll(those & (((uint64_t)1 << lane) - 1))] = key;
+        }
+        __syncthreads();
+        const int all = shared.n;
+        for (int i = threadIdx.x; i < all; i += WAVES * 64) {
+            const uint64_t key = shared.all[i];
+            int rank = 0;
+#pragma unroll 4
+            for (int k = 0; k < all; ++k) rank += shared.all[k] > key;
+            if (rank < count) out(rank, key);
+        }
+        for (int i = all + threadIdx.x; i < count; i += WAVES * 64) out(i, (uint64_t)0);
     }
 };
 __device__ __forceinline__ uint64_t key_of(float logit, int token) { return (uint64_t)ordered(logit + 0.0f) << 32 | (uint32_t)~token; }
+
+// The best tokens of vectors first .. last - 1 of a row that have been walked through: out(i, key) for the i-th largest, i < count, 0 where there
+// are no more.  tops[u] is the thread's largest logit among the vectors of its turns u.
+//
+// `count` threads have a logit at least as large as the count-th largest of their own largest ones, so nothing
+// below that is among the best, and little more than `count` logits are above: the turns that hold one are read again, from the caches,
+// and what reaches the bound is ranked by counting.  A list that is kept up to date while the row goes by was slower: of some 250 vectors of a
+// wave a tenth to a half brought a better token, for ten times the work of one that did not.  Where so many logits are equal that those at
+// the bound do not fit, such lists are made after all.
+template <int U, int TYPE, bool PAST, typename Out>
+__device__ __forceinline__ void best_tokens(TopKeys<4> &shared, const Row<TYPE, PAST> &row, int first, int last, const float (&tops)[U], int count,
+                                            const Out &out)
+{
+    constexpr int THREADS = 256, N = Logits<TYPE>::kCount, kStep = THREADS * U, kRoom = 4 * kListed;
+    const int t = threadIdx.x, lane = t & 63;
+    const Span span(row, first, last);
+    float top = tops[0];
+#pragma unroll
+    for (int u = 1; u < U; ++u) top = fmaxf(top, tops[u]);
+    shared.tops[t] = top > -__builtin_inff() ? ordered(top + 0.0f) : 0u;
+    if (t == 0) shared.n = shared.groups = 0;
+    __syncthreads();
+    uint32_t mine[4], bound = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) mine[w] = shared.tops[w * 64 + lane];
+#pragma unroll
+    for (int bit = 31; bit >= 16; --bit) {
+        const uint32_t higher = bound | 1u << bit;
+        int n = 0;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) n += __builtin_popcountll(__builtin_amdgcn_ballot_w64(mine[w] >= higher));
+        bound = n >= count ? higher : bound;
+    }
+    const float least = fmaxf(of_ordered(max(bound, 1u)), -__FLT_MAX__);
+    auto take = [&](const Logits<TYPE> &v, int j) {
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            if (v[e] >= least) {
+                const int at = atomicAdd(&shared.n, 1);
+                if (at < kRoom) shared.keys[at / kListed][at % kListed] = key_of(v[e], row.token(j) + e);
+            }
+    };
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        if (tops[u] >= least) shared.group[atomicAdd(&shared.groups, 1)] = (uint16_t)(u * THREADS + t);
+    __syncthreads();
+    const int steps = (span.end - span.begin + kStep - 1) / kStep, items = shared.groups * steps;
+    for (int i = t; i < items; i += THREADS) {
+        const int g = i / steps, j = span.begin + (i - g * steps) * kStep + shared.group[g];
+        if (j < span.end) {
+            Logits<TYPE> v;
+            row.load(v, j);
+            take(v, j);
+        }
+    }
+    if (t < 64 && span.has_ends()) {
+        Ends<TYPE> ends;
+        ends.load(row, span);
+        if (span.takes_end()) take(ends.vector(), ends.j);
+    }
+    __syncthreads();
+    const int n = shared.n;
+    __syncthreads();  // all know it
+    if (n > kRoom) {
+        TopList<4> list(shared, count);
+        __syncthreads();
+        walk<THREADS, 1>(
+            row, first, last,
+            [&](const Logits<TYPE> &v, int j, int) {
+                list.template offer<N, true>(largest(v), [&](int e) { return v.at(e); }, [&](int e) { return key_of(v.at(e), row.token(j) + e); });
+            },
+            [&](const Logits<TYPE> &v, int j) {
+                list.template offer<N, false>(largest(v), [&](int e) { return v.at(e); }, [&](int e) { return key_of(v.at(e), row.token(j) + e); });
+            });
+        list.ranked(out);
+        return;
+    }
+    for (int i = t; i < n; i += THREADS) {
+        const uint64_t key = shared.keys[i / kListed][i % kListed];
+        int rank = 0;
+#pragma unroll 4
+        for (int k = 0; k < n; ++k) rank += shared.keys[k / kListed][k % kListed] > key;
+        if (rank < count) out(rank, key);
+    }
+    for (int i = n + t; i < count; i += THREADS) out(i, (uint64_t)0);
+}
 
 // ---- gradients ----
 
@@ -322,12 +618,12 @@ __device__ __forceinline__ uint32_t bits_of(float v)
 }
 
 // A row of the gradient, cut into the vectors of its row of logits: it may lie elsewhere in 16 bytes.
-template <int TYPE>
+template <int TYPE, bool PAST = false>
 struct GradientRow {
     static constexpr int kCount = Logits<TYPE>::kCount, kBytes = Logits<TYPE>::kBytes;
     char *base;
     int skip, vocab;
-    __device__ __forceinline__ GradientRow(void *gradient, int64_t at, const Row<TYPE> &x) : skip(x.skip), vocab(x.vocab)
+    __device__ __forceinline__ GradientRow(void *gradient, int64_t at, const Row<TYPE, PAST> &x) : skip(x.skip), vocab(x.vocab)
     {
         base = static_cast<char *>(gradient) + (at - skip) * kBytes;
     }
@@ -336,7 +632,13 @@ struct GradientRow {
         uint32_t w[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[i] = kBytes == 4 ? bits_of<TYPE>(v[i]) : bits_of<TYPE>(v[2 * i % kCount]) | bits_of<TYPE>(v[(2 * i + 1) % kCount]) << 16;
-        __builtin_memcpy(base + (int64_t)j * 16, w, 16);
+        typedef uint32_t Vec __attribute__((ext_vector_type(4), aligned(2)));  // at the type's alignment
+        const Vec q = {w[0], w[1], w[2], w[3]};
+        Vec *p = reinterpret_cast<Vec *>(base + (uint32_t)j * 16u);
+        if (PAST)
+            __builtin_nontemporal_store(q, p);
+        else
+            *p = q;
     }
     __device__ __forceinline__ void store_one(float v, int token) const
     {
@@ -347,37 +649,69 @@ struct GradientRow {
         else
             *reinterpret_cast<uint16_t *>(p) = (uint16_t)b;
     }
-    __device__ __forceinline__ void store(const float (&v)[kCount], int j, int last) const  // what of vector j, one of those before `last`, is the row's
+    __device__ __forceinline__ void store_within(const float (&v)[kCount], int j) const  // what of it is the row's
     {
         const int token = j * kCount - skip;
-        if (j >= last) return;
-        if (token >= 0 && token + kCount <= vocab) {
-            store(v, j);
-            return;
-        }
 #pragma unroll
         for (int i = 0; i < kCount; ++i)
             if (token + i >= 0 && token + i < vocab) store_one(v[i], token + i);
     }
 };
 
-// gradient = p (flat + tilted log2 p) with p = 2^e, e = (x - reference) c - log, over vectors first .. last - 1 of a row.  The gradient may
-// take the logits' place: a vector's values are read before they are written, by the same thread, and by no other.
-template <int TYPE, int THREADS, int U, bool TILTED>
-__device__ __forceinline__ void write_gradient(const Row<TYPE> &x, const GradientRow<TYPE> &to, int first, int last, float reference, float c,
-                                               float log, float flat, float tilted)
-{
-    constexpr int N = Logits<TYPE>::kCount;
-    walk<TYPE, THREADS, U>(x, first, last, [&](const Logits<TYPE> &v, int j) {
-        float g[N];
+// Up to THREADS * VECTORS vectors of a row in a workgroup's registers.  All are asked for together and without a branch between them (behind one
+// the compiler waits for all): where there are fewer, the last again; there is one.
+template <int THREADS, int VECTORS, int TYPE>
+struct Held {
+    Logits<TYPE> v[VECTORS];
+    template <bool PAST>
+    __device__ __forceinline__ void load(const Row<TYPE, PAST> &x, const Span &span)
+    {
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const float e = fmaf(v[i] - reference, c, -log), p = exp2_of(e);
-            g[i] = p * (TILTED ? fmaf(tilted, fmaxf(e, kFarBelow), flat) : flat);
+        for (int u = 0; u < VECTORS; ++u) x.load(v[u], min(span.begin + u * THREADS + (int)threadIdx.x, span.end - 1));
+    }
+    // each(v, j) in turn; j may be span.end and above in some lanes
+    template <typename Each>
+    __device__ __forceinline__ void go_through(const Span &span, const Each &each)
+    {
+#pragma unroll
+        for (int u = 0; u < VECTORS; ++u)
+            if (span.begin + u * THREADS < span.end) each(v[u], span.begin + u * THREADS + (int)threadIdx.x);
+    }
+};
+
+// A segment of a row's gradient: make(v, j, g) is that of vector j.  It may take the logits' place: a vector's values are read before they are
+// written, by the same thread, and by no other.
+template <int THREADS, int VECTORS, int TYPE, bool PAST>
+struct GradientSegment {
+    const Row<TYPE, PAST> &x;
+    const GradientRow<TYPE, PAST> &to;
+    const Span span;
+    Held<THREADS, VECTORS, TYPE> held;
+    Ends<TYPE> ends;
+    __device__ __forceinline__ GradientSegment(const Row<TYPE, PAST> &x_, const GradientRow<TYPE, PAST> &to_, int first, int last)
+        : x(x_), to(to_), span(x_, first, last)
+    {
+    }
+    __device__ __forceinline__ void load()
+    {
+        if (threadIdx.x < 64 && span.has_ends()) ends.load(x, span);
+        if (span.begin < span.end) held.load(x, span);
+    }
+    template <typename Make>
+    __device__ __forceinline__ void write(const Make &make)
+    {
+        held.go_through(span, [&](const Logits<TYPE> &v, int j) {
+            float g[Logits<TYPE>::kCount];
+            make(v, j, g);
+            if (j < span.end) to.store(g, j);
+        });
+        if (span.takes_end()) {
+            float g[Logits<TYPE>::kCount];
+            make(ends.vector(), ends.j, g);
+            to.store_within(g, ends.j);
         }
-        to.store(g, j, last);
-    });
-}
+    }
+};
 
 // The log sum of a row as the caller has it, in fp32, turned into a reference logit and what is left of it: (x - reference) c - log is
 // log2 p up to the rounding of the difference.
@@ -390,11 +724,13 @@ struct Saved {
     }
 };
 
-template <int TYPE, int THREADS>
-__device__ __forceinline__ void write_zeros(const GradientRow<TYPE> &to, int first, int last)
+template <int THREADS, int TYPE, bool PAST>
+__device__ __forceinline__ void write_zeros(const Row<TYPE, PAST> &x, const GradientRow<TYPE, PAST> &to, int first, int last)
 {
     const float zero[Logits<TYPE>::kCount] = {};
-    for (int j = first + threadIdx.x; j < last; j += THREADS) to.store(zero, j, last);
+    const Span span(x, first, last);
+    for (int j = span.begin + threadIdx.x; j < span.end; j += THREADS) to.store(zero, j);
+    if (span.takes_end()) to.store_within(zero, span.tail && (threadIdx.x == 1 || !span.head) ? span.whole : 0);
 }
 
 }  // namespace

@@ -459,7 +459,9 @@ constexpr int kMaxPlaces = 128;  // of a teacher
 struct LogitsCut {
     int segments, vectors;
 };
-LogitsCut logits_cut(int64_t rows, int32_t vocab, int32_t type);
+LogitsCut logits_cut(int64_t rows, int32_t vocab, int32_t type);      // of a pass that sums
+LogitsCut gradient_cut(int32_t vocab, int32_t type, int vectors);    // into segments of so many
+bool logits_past_caches(int64_t rows, int32_t vocab, int32_t type);  // whether the logits are not to stay in the caches
 // What a segment leaves: its sums of exponentials against a reference logit.
 struct LogitsPart {
     float reference, sum, second, unused;
@@ -481,7 +483,7 @@ struct LogprobArgs {
     int32_t segments, segment_vectors;
 };
 size_t token_logprobs_workspace_bytes(int64_t rows, int32_t vocab, int32_t count);
-hipError_t launch_token_logprobs(LogprobArgs a, void *workspace, hipStream_t stream);
+hipError_t launch_token_logprobs(const LogprobArgs &a, void *workspace, hipStream_t stream);
 struct LogprobGradientArgs {
     const void *logits;
     void *gradient;
@@ -494,7 +496,7 @@ struct LogprobGradientArgs {
     Divisor by_segments;
     int32_t segments, segment_vectors;
 };
-hipError_t launch_token_logprobs_backward(LogprobGradientArgs a, hipStream_t stream);
+hipError_t launch_token_logprobs_backward(const LogprobGradientArgs &a, hipStream_t stream);
 struct DistillArgs {
     const void *logits;
     int64_t rows, stride, gradient_stride;
@@ -502,7 +504,7 @@ struct DistillArgs {
     const int32_t *tokens;
     const float *weights;                        // or null; the gradient's of each row's loss
     float *losses, *log_sums, *log_rests;        // or null
-    const float *saved_sums, *saved_rests;       // of an earlier call, for the gradient alone
+    const float *saved_sums, *saved_rests;       // of an earlier call, for the gradient alone; else null
     void *gradient;                              // or null
     int32_t vocab, type, places;
     bool rest;
@@ -511,9 +513,9 @@ struct DistillArgs {
     LogitsPart *parts;
     Divisor by_segments;
     int32_t segments, segment_vectors;
+    int32_t row_parts;                           // parts of a row
 };
 size_t distill_workspace_bytes(int64_t rows, int32_t vocab);
-hipError_t launch_distill(DistillArgs a, void *workspace, hipStream_t stream);
-hipError_t launch_distill_backward(DistillArgs a, hipStream_t stream);
+hipError_t launch_distill(const DistillArgs &a, void *workspace, hipStream_t stream);
 
 }  // namespace quamba

@@ -13,32 +13,9 @@
 namespace quamba {
 namespace {
 
-constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int64_t kRowsOfALaunch = (int64_t)1 << 22;
-
-// The lists of a workgroup's waves as one: out(i, key) for the i-th largest, i < count, 0 where there are no more.
-template <int WAVES, typename Out>
-__device__ __forceinline__ void ranked(const uint64_t (&keys)[WAVES][kListed], TopList &list, int count, const Out &out)
-{
-    __shared__ int lengths[WAVES];
-    if (list.n > count) list.shrink();
-    if (threadIdx.x % 64 == 0) lengths[threadIdx.x / 64] = list.n;
-    __syncthreads();
-    int n[WAVES], all = 0;
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) all += n[w] = lengths[w];
-    for (int i = threadIdx.x; i < WAVES * kMaxChoices; i += WAVES * 64) {
-        const int w = i / kMaxChoices, j = i % kMaxChoices;
-        if (j >= lengths[w]) continue;
-        const uint64_t key = keys[w][j];
-        int rank = 0;
-#pragma unroll
-        for (int o = 0; o < WAVES; ++o)
-            for (int k = 0; k < n[o]; ++k) rank += keys[o][k] > key;
-        if (rank < count) out(rank, key);
-    }
-    for (int i = all + threadIdx.x; i < count; i += WAVES * 64) out(i, (uint64_t)0);
-}
+constexpr int kThreads = 256;
+constexpr int kGradientVectors = 1;  // of a thread
 
 // A row's results from its sums; every thread has them.
 struct Finish {
@@ -83,46 +60,60 @@ __device__ __forceinline__ void write_padding(const LogprobArgs &a, int64_t row)
 }
 
 // A segment of a row to a workgroup; where a row has one only, that is all.
-template <int TYPE, bool ENTROPY, bool TOP>
+template <int TYPE, bool ENTROPY, bool TOP, bool PAST>
 __global__ __launch_bounds__(kThreads) void token_logprobs_kernel(LogprobArgs a)
 {
-    __shared__ uint64_t keys[TOP ? kWaves : 1][kListed];
+    __shared__ TopKeys<TOP ? 4 : 1> keys;
     const int t = threadIdx.x;
     const int local = quotient((int)blockIdx.x, a.by_segments), segment = (int)blockIdx.x - local * a.segments;
     const int64_t row = a.first_row + local;
+    const bool alone = a.segments == 1;
     if (is_padding(a, row)) {
-        if (a.segments == 1) write_padding<kThreads>(a, row);
+        if (alone) write_padding<kThreads>(a, row);
         return;
     }
-    const Row<TYPE> x(a.logits, row * a.stride, a.vocab);
-    const bool alone = a.segments == 1;
+    const Row<TYPE, PAST> x(a.logits, row * a.stride, a.vocab);
     float chosen = 0.0f;
     if (alone && t == 0 && a.targets) chosen = x.logit(a.targets[row]);
+    Adder<ENTROPY ? 1 : 0> adder(a.c);
+    const int first = segment * a.segment_vectors, last = alone ? x.vectors : min(first + a.segment_vectors, x.vectors);
     ExpSum s;
-    TopList list(keys[TOP ? t / 64 : 0], a.count);
-    const int first = segment * a.segment_vectors;
-    walk<TYPE, kThreads, 4>(x, first, alone ? x.vectors : min(first + a.segment_vectors, x.vectors), [&](const Logits<TYPE> &v, int j) {
-        const float top = largest(v);
-        add<ENTROPY ? 1 : 0>(s, v, top, a.c);
-        if (TOP)
-            list.offer<Logits<TYPE>::kCount, true>(top, [&](int e) { return v[e]; }, [&](int e) { return key_of(v[e], x.token(j) + e); });
-    });
-    s = join<ENTROPY, kThreads>(s, a.c);
-    if (alone) {
+    const auto at_end = [&](const Logits<TYPE> &v, int) { adder.add(v); };
+    if constexpr (TOP) {
+        float tops[kTurns];
+#pragma unroll
+        for (int u = 0; u < kTurns; ++u) tops[u] = -__builtin_inff();
+        walk<kThreads, kTurns>(
+            x, first, last,
+            [&](const Logits<TYPE> &v, int, int u) {
+                adder.add(v);
+                tops[u] = fmaxf(tops[u], largest(v));
+            },
+            at_end);
+        s = join<ENTROPY, kThreads>(adder.result(), a.c);
         const Finish finish(a, row, s);
-        if (t == 0) finish.write(s, chosen);
-        if (TOP) ranked(keys, list, a.count, [&](int i, uint64_t key) { finish.alternative(i, key); });
+        best_tokens(keys, x, first, last, tops, a.count, [&](int i, uint64_t key) {
+            if (alone)
+                finish.alternative(i, key);
+            else
+                a.best[(int64_t)blockIdx.x * a.count + i] = key;
+        });
     } else {
-        if (t == 0) a.parts[blockIdx.x] = {s.reference, s.sum, s.second, 0.0f};
-        if (TOP) ranked(keys, list, a.count, [&](int i, uint64_t key) { a.best[(int64_t)blockIdx.x * a.count + i] = key; });
+        walk<kThreads, kTurns>(x, first, last, [&](const Logits<TYPE> &v, int, int) { adder.add(v); }, at_end);
+        s = join<ENTROPY, kThreads>(adder.result(), a.c);
     }
+    if (t != 0) return;
+    if (alone)
+        Finish(a, row, s).write(s, chosen);
+    else
+        a.parts[blockIdx.x] = {s.reference, s.sum, s.second, 0.0f};
 }
 
 // A row to a workgroup: its segments' sums and best tokens as one.
 template <int TYPE, bool TOP>
 __global__ __launch_bounds__(kThreads) void token_logprobs_join_kernel(LogprobArgs a)
 {
-    __shared__ uint64_t keys[TOP ? kWaves : 1][kListed];
+    __shared__ TopKeys<TOP ? kThreads / 64 : 1> keys;
     const int t = threadIdx.x;
     const int64_t row = a.first_row + blockIdx.x;
     if (is_padding(a, row)) {
@@ -135,53 +126,55 @@ __global__ __launch_bounds__(kThreads) void token_logprobs_join_kernel(LogprobAr
     const ExpSum s = join<true, kThreads>(parts, a.segments, a.c);
     const Finish finish(a, row, s);
     if (t == 0) finish.write(s, chosen);
-    if (TOP) {
-        TopList list(keys[t / 64], a.count);
+    if constexpr (TOP) {
+        TopList<kThreads / 64> list(keys, a.count);
+        __syncthreads();
         const uint64_t *best = a.best + (int64_t)blockIdx.x * a.segments * a.count;
         const int all = a.segments * a.count;
         for (int i = 0; i < all; i += kThreads) {  // place by place, the best of all segments first
-            const int k = i + t, place = k / a.segments;
+            const int k = i + t, place = quotient(k, a.by_segments);
             const uint64_t key = k < all ? best[(int64_t)(k - place * a.segments) * a.count + place] : 0;
             const float v = key ? of_ordered((uint32_t)(key >> 32)) : -__builtin_inff();
-            list.offer<1, false>(v, [&](int) { return v; }, [&](int) { return key; });
+            list.template offer<1, false>(v, [&](int) { return v; }, [&](int) { return key; });
         }
-        ranked(keys, list, a.count, [&](int i, uint64_t key) { finish.alternative(i, key); });
+        list.ranked([&](int i, uint64_t key) { finish.alternative(i, key); });
     }
 }
 
 // A segment of a row's gradient to a workgroup.
-template <int TYPE, bool ENTROPY>
+template <int TYPE, bool ENTROPY, bool PAST>
 __global__ __launch_bounds__(kThreads) void token_logprobs_backward_kernel(LogprobGradientArgs a)
 {
-    const int t = threadIdx.x;
+    constexpr int N = Logits<TYPE>::kCount;
     const int local = quotient((int)blockIdx.x, a.by_segments), segment = (int)blockIdx.x - local * a.segments;
     const int64_t row = a.first_row + local;
-    const Row<TYPE> x(a.logits, row * a.stride, a.vocab);
-    const GradientRow<TYPE> to(a.gradient, row * a.gradient_stride, x);
+    const Row<TYPE, PAST> x(a.logits, row * a.stride, a.vocab);
+    const GradientRow<TYPE, PAST> to(a.gradient, row * a.gradient_stride, x);
     const int first = segment * a.segment_vectors, last = min(first + a.segment_vectors, x.vectors);
-    const int target = a.targets ? a.targets[row] : -1;
+    GradientSegment<kThreads, kGradientVectors, TYPE, PAST> segment_of(x, to, first, last);
+    const int target = a.targets ? a.targets[row] : -(1 << 30);
     const float g = a.targets ? a.grad_logprobs[row] : 0.0f, h = ENTROPY ? a.grad_entropies[row] : 0.0f;
     if ((a.targets && (uint32_t)target >= (uint32_t)a.vocab) || (g == 0.0f && h == 0.0f)) {
-        write_zeros<TYPE, kThreads>(to, first, last);
+        write_zeros<kThreads>(x, to, first, last);
         return;
     }
-    const float log_sum = a.log_sums[row], entropy = ENTROPY ? a.entropies[row] : 0.0f;
-    const Saved saved(log_sum, a.temperature, a.c);
-    // -g p - h p (ln p + entropy), over T
+    segment_of.load();
+    const float entropy = ENTROPY ? a.entropies[row] : 0.0f;
+    const Saved saved(a.log_sums[row], a.temperature, a.c);
+    // -g p - h p (ln p + entropy), over T: p (flat + tilted log2 p)
     const float flat = -(ENTROPY ? fmaf(h, entropy, g) : g) * a.per_temperature, tilted = -h * 0.693147180559945309f * a.per_temperature;
-    const int at = target + x.skip;
-    const bool here = t == 0 && target >= 0 && at >= first * Logits<TYPE>::kCount && at < last * Logits<TYPE>::kCount;
-    float of_target = 0.0f;
-    if (here) {
-        const float e = fmaf(x.logit(target) - saved.reference, a.c, -saved.log), p = exp2_of(e);
-        of_target = fmaf(g, a.per_temperature, p * (ENTROPY ? fmaf(tilted, fmaxf(e, kFarBelow), flat) : flat));
-    }
-    __shared__ float kept;  // the target's logit is read before its place is written: the value passes through here
-    if (t == 0) kept = of_target;
-    __syncthreads();
-    write_gradient<TYPE, kThreads, 4, ENTROPY>(x, to, first, last, saved.reference, a.c, saved.log, flat, tilted);
-    __syncthreads();
-    if (here) to.store_one(kept, target);
+    segment_of.write([&](const Logits<TYPE> &v, int j, float(&d)[N]) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float e = fmaf(v[i] - saved.reference, a.c, -saved.log), p = exp2_of(e);
+            d[i] = p * (ENTROPY ? fmaf(tilted, fmaxf(e, kFarBelow), flat) : flat);
+        }
+        const int at = target - x.token(j);
+        if (at >= 0 && at < N) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) d[i] = i == at ? fmaf(g, a.per_temperature, d[i]) : d[i];
+        }
+    });
 }
 
 }  // namespace
@@ -192,31 +185,78 @@ LogitsCut logits_cut(int64_t rows, int32_t vocab, int32_t type)
     const int per_vector = type == QUAMBA_F32 ? 4 : 8;
     const int vectors = (vocab + 2 * per_vector - 2) / per_vector;  // the most that a row's address may make of it
     const int64_t want = (4 * compute_units() + rows - 1) / std::max<int64_t>(rows, 1);
-    const int segments = (int)std::max<int64_t>(1, std::min<int64_t>({want, (vectors + 511) / 512, 256}));
+    const int least = 512;
+    const int segments = (int)std::max<int64_t>(1, std::min<int64_t>({want, (vectors + least - 1) / least, 256}));
     const int each = (vectors + segments - 1) / segments;
     return {(vectors + each - 1) / each, each};
 }
 
+LogitsCut gradient_cut(int32_t vocab, int32_t type, int vectors)
+{
+    const int per_vector = type == QUAMBA_F32 ? 4 : 8;
+    const int all = (vocab + 2 * per_vector - 2) / per_vector;
+    const int segments = (all + vectors - 1) / vectors, each = std::min(vectors, ((all + segments - 1) / segments + 63) / 64 * 64);
+    return {(all + each - 1) / each, each};
+}
+
+bool logits_past_caches(int64_t rows, int32_t vocab, int32_t type)
+{
+    return (double)rows * vocab * (type == QUAMBA_F32 ? 4 : 2) > 64 * 1048576.0;
+}
+
 namespace {
 
-template <int TYPE>
+template <int TYPE, bool PAST>
 void launch_rows(const LogprobArgs &a, int64_t rows, hipStream_t stream)
 {
-    const int grid = (int)(rows * a.segments);
-    const auto kernel = a.count ? (a.entropies ? token_logprobs_kernel<TYPE, true, true> : token_logprobs_kernel<TYPE, false, true>)
-                                : (a.entropies ? token_logprobs_kernel<TYPE, true, false> : token_logprobs_kernel<TYPE, false, false>);
-    kernel<<<grid, kThreads, 0, stream>>>(a);
+    const auto kernel = a.count ? (a.entropies ? token_logprobs_kernel<TYPE, true, true, PAST> : token_logprobs_kernel<TYPE, false, true, PAST>)
+                                : (a.entropies ? token_logprobs_kernel<TYPE, true, false, PAST> : token_logprobs_kernel<TYPE, false, false, PAST>);
+    kernel<<<(int)(rows * a.segments), kThreads, 0, stream>>>(a);
     if (a.segments == 1) return;
     const auto join_kernel = a.count ? token_logprobs_join_kernel<TYPE, true> : token_logprobs_join_kernel<TYPE, false>;
     join_kernel<<<(int)rows, kThreads, 0, stream>>>(a);
 }
 
 template <int TYPE>
-void launch_gradient(const LogprobGradientArgs &a, int64_t rows, hipStream_t stream)
+hipError_t launch(LogprobArgs a, void *workspace, hipStream_t stream)
 {
-    const int grid = (int)(rows * a.segments);
-    const auto kernel = a.grad_entropies ? token_logprobs_backward_kernel<TYPE, true> : token_logprobs_backward_kernel<TYPE, false>;
-    kernel<<<grid, kThreads, 0, stream>>>(a);
+    const LogitsCut cut = workspace ? logits_cut(a.rows, a.vocab, TYPE) : LogitsCut{1, 0};
+    a.segments = cut.segments;
+    a.segment_vectors = cut.vectors;
+    a.by_segments = divisor((uint32_t)cut.segments);
+    a.parts = static_cast<LogitsPart *>(workspace);
+    a.best = reinterpret_cast<uint64_t *>(a.parts + (cut.segments > 1 ? a.rows * cut.segments : 0));
+    const bool past = logits_past_caches(a.rows, a.vocab, TYPE);
+    for (a.first_row = 0; a.first_row < a.rows; a.first_row += kRowsOfALaunch) {
+        const int64_t rows = std::min(a.rows - a.first_row, kRowsOfALaunch);
+        past ? launch_rows<TYPE, true>(a, rows, stream) : launch_rows<TYPE, false>(a, rows, stream);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+template <int TYPE, bool PAST>
+hipError_t launch_gradient(LogprobGradientArgs a, hipStream_t stream)
+{
+    const LogitsCut cut = gradient_cut(a.vocab, TYPE, kThreads * kGradientVectors);
+    a.segments = cut.segments;
+    a.segment_vectors = cut.vectors;
+    a.by_segments = divisor((uint32_t)cut.segments);
+    const auto kernel = a.grad_entropies ? token_logprobs_backward_kernel<TYPE, true, PAST> : token_logprobs_backward_kernel<TYPE, false, PAST>;
+    const int64_t most = kRowsOfALaunch / cut.segments;
+    for (a.first_row = 0; a.first_row < a.rows; a.first_row += most) {
+        kernel<<<(int)(std::min(a.rows - a.first_row, most) * cut.segments), kThreads, 0, stream>>>(a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+template <int TYPE>
+hipError_t launch_gradient(const LogprobGradientArgs &a, hipStream_t stream)
+{
+    return logits_past_caches(a.rows, a.vocab, TYPE) ? launch_gradient<TYPE, true>(a, stream) : launch_gradient<TYPE, false>(a, stream);
 }
 
 }  // namespace
@@ -231,44 +271,22 @@ size_t token_logprobs_workspace_bytes(int64_t rows, int32_t vocab, int32_t count
     return most;
 }
 
-hipError_t launch_token_logprobs(LogprobArgs a, void *workspace, hipStream_t stream)
+hipError_t launch_token_logprobs(const LogprobArgs &a, void *workspace, hipStream_t stream)
 {
-    const LogitsCut cut = workspace ? logits_cut(a.rows, a.vocab, a.type) : LogitsCut{1, 0};
-    a.segments = cut.segments;
-    a.segment_vectors = cut.vectors;
-    a.by_segments = divisor((uint32_t)cut.segments);
-    a.parts = static_cast<LogitsPart *>(workspace);
-    a.best = reinterpret_cast<uint64_t *>(a.parts + (cut.segments > 1 ? a.rows * cut.segments : 0));
-    for (a.first_row = 0; a.first_row < a.rows; a.first_row += kRowsOfALaunch) {
-        const int64_t rows = std::min(a.rows - a.first_row, kRowsOfALaunch);
-        switch (a.type) {
-            case QUAMBA_F32: launch_rows<QUAMBA_F32>(a, rows, stream); break;
-            case QUAMBA_F16: launch_rows<QUAMBA_F16>(a, rows, stream); break;
-            default: launch_rows<QUAMBA_BF16>(a, rows, stream); break;
-        }
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
+    switch (a.type) {
+        case QUAMBA_F32: return launch<QUAMBA_F32>(a, workspace, stream);
+        case QUAMBA_F16: return launch<QUAMBA_F16>(a, workspace, stream);
+        default: return launch<QUAMBA_BF16>(a, workspace, stream);
     }
-    return hipSuccess;
 }
 
-hipError_t launch_token_logprobs_backward(LogprobGradientArgs a, hipStream_t stream)
+hipError_t launch_token_logprobs_backward(const LogprobGradientArgs &a, hipStream_t stream)
 {
-    const LogitsCut cut = logits_cut(a.rows, a.vocab, a.type);
-    a.segments = cut.segments;
-    a.segment_vectors = cut.vectors;
-    a.by_segments = divisor((uint32_t)cut.segments);
-    for (a.first_row = 0; a.first_row < a.rows; a.first_row += kRowsOfALaunch) {
-        const int64_t rows = std::min(a.rows - a.first_row, kRowsOfALaunch);
-        switch (a.type) {
-            case QUAMBA_F32: launch_gradient<QUAMBA_F32>(a, rows, stream); break;
-            case QUAMBA_F16: launch_gradient<QUAMBA_F16>(a, rows, stream); break;
-            default: launch_gradient<QUAMBA_BF16>(a, rows, stream); break;
-        }
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
+    switch (a.type) {
+        case QUAMBA_F32: return launch_gradient<QUAMBA_F32>(a, stream);
+        case QUAMBA_F16: return launch_gradient<QUAMBA_F16>(a, stream);
+        default: return launch_gradient<QUAMBA_BF16>(a, stream);
     }
-    return hipSuccess;
 }
 
 }  // namespace quamba
