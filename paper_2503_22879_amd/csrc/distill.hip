@@ -25,6 +25,7 @@ struct Places {
     float sum;     // of q
     bool any;      // whether there is a place that is not empty
 
+    Places() = default;
     __device__ __forceinline__ Places(const DistillArgs &a, int64_t row) : Places(a, Raw(a, row)) {}
 
     // As they lie in memory.  Loads return in order: what a wave asks for before its logits does not wait for them.
@@ -75,13 +76,26 @@ struct Places {
             sum = group_sum<64>(q[0] + q[1]);
         }
     }
+    // Whether place h of the lane has a token in these vectors.
+    template <int TYPE>
+    __device__ __forceinline__ bool is_in(int h, int skip, int first, int last) const
+    {
+        const int at = token[h] + skip;
+        return token[h] >= 0 && at >= first * Logits<TYPE>::kCount && at < last * Logits<TYPE>::kCount;
+    }
     // The sum of q over all places with the token of place h of the lane: a token may have several.  By the whole wave.
     __device__ __forceinline__ void of_tokens(int places, float (&all)[2]) const
     {
         all[0] = all[1] = 0.0f;
-        for (int i = 0; i < places; ++i) {
-            const int t = __builtin_amdgcn_readlane(i < 64 ? token[0] : token[1], i & 63);
-            const float p = from_bits(__builtin_amdgcn_readlane(__builtin_bit_cast(int, i < 64 ? q[0] : q[1]), i & 63));
+        for (int i = 0; i < min(places, 64); ++i) {
+            const int t = __builtin_amdgcn_readlane(token[0], i);
+            const float p = from_bits(__builtin_amdgcn_readlane(__builtin_bit_cast(int, q[0]), i));
+            all[0] += token[0] == t ? p : 0.0f;
+            if (places > 64) all[1] += token[1] == t ? p : 0.0f;
+        }
+        for (int i = 64; i < places; ++i) {
+            const int t = __builtin_amdgcn_readlane(token[1], i - 64);
+            const float p = from_bits(__builtin_amdgcn_readlane(__builtin_bit_cast(int, q[1]), i - 64));
             all[0] += token[0] == t ? p : 0.0f;
             all[1] += token[1] == t ? p : 0.0f;
         }
@@ -91,12 +105,18 @@ struct Places {
 // What the gradient of a row is made from: that of other tokens is flat 2^((x - reference) c - log), that of the teacher's comes from p and q.
 struct Slope {
     float reference, log, flat;
+    float offset, times;  // 16-bit logits: the same as times 2^(x c - offset), whose rounding is far below the result's; offset +infinity: it is not
     float own_reference, own_log, whole, scale;
     template <int TYPE>
     __device__ __forceinline__ void of_others(const Logits<TYPE> &x, float c, float (&g)[Logits<TYPE>::kCount]) const
     {
+        if (TYPE != QUAMBA_F32 && offset != __builtin_inff()) {
 #pragma unroll
-        for (int i = 0; i < Logits<TYPE>::kCount; ++i) g[i] = exp2_of(fmaf(x[i] - reference, c, -log)) * flat;
+            for (int i = 0; i < Logits<TYPE>::kCount; ++i) g[i] = exp2_of(fmaf(x[i], c, -offset)) * times;
+        } else {
+#pragma unroll
+            for (int i = 0; i < Logits<TYPE>::kCount; ++i) g[i] = exp2_of(fmaf(x[i] - reference, c, -log)) * flat;
+        }
     }
     __device__ __forceinline__ float of_token(float x, float q, float c) const
     {
@@ -116,6 +136,9 @@ __device__ __forceinline__ Slope slope_of(const DistillArgs &a, float weight, fl
     s.reference = rest ? rest_reference : reference;
     s.log = rest ? log_rest : log_sum;
     s.flat = (rest ? fmaf(s.whole, share, -left) : s.whole) * s.scale;
+    const float offset = fmaf(s.reference, a.c, s.log);
+    s.times = s.flat * exp2_of(-(fmaf(s.reference, a.c, -offset) + s.log));
+    s.offset = __builtin_fabsf(offset) < 0x1p100f || offset != offset ? offset : __builtin_inff();
     return s;
 }
 
@@ -179,18 +202,14 @@ __device__ __forceinline__ void write_no_loss(const DistillArgs &a, int64_t row)
     if (a.log_rests) a.log_rests[row] = 0.0f;
 }
 
-// The gradients of the teacher's tokens in the place of what the workgroup has written there.
+// The gradients of the teacher's tokens in vectors first .. last - 1, by one wave, in the place of what the workgroup has written there.
 template <int TYPE, bool PAST>
-__device__ __forceinline__ void put_tokens(const DistillArgs &a, const Places &p, const TokenLogits<TYPE> &logit, const Slope &slope,
-                                           const GradientRow<TYPE, PAST> &to)
+__device__ __forceinline__ void put_tokens(const DistillArgs &a, const Places &p, const float (&q)[2], const TokenLogits<TYPE> &logit,
+                                           const Slope &slope, const GradientRow<TYPE, PAST> &to, int first, int last)
 {
-    __syncthreads();
-    if (threadIdx.x >= 64) return;
-    float q[2];
-    p.of_tokens(a.places, q);
 #pragma unroll
     for (int h = 0; h < 2; ++h)
-        if (p.token[h] >= 0) to.store_one(slope.of_token(logit[h], q[h], a.c), p.token[h]);
+        if (p.is_in<TYPE>(h, to.skip, first, last)) to.store_one(slope.of_token(logit[h], q[h], a.c), p.token[h]);
 }
 
 // A bit for each logit of some vectors: whether it is the teacher's.
@@ -219,8 +238,8 @@ struct Marks {
 
 // A segment of a row to a workgroup; where a row has one only, that is all.  GRADIENT: with the gradient in a second pass, where there is no
 // workspace for what a launch behind this one would need.
-template <int TYPE, bool REST, bool PAST, bool GRADIENT>
-__global__ __launch_bounds__(kThreads) void distill_kernel(DistillArgs a)
+template <int TYPE, int THREADS, bool REST, bool PAST, bool GRADIENT>
+__global__ __launch_bounds__(THREADS) void distill_kernel(DistillArgs a)
 {
     constexpr int N = Logits<TYPE>::kCount, kRange = (1 << 17) / N;  // vectors that are marked at once
     __shared__ uint32_t bits[REST ? (1 << 17) / 32 : 1];
@@ -233,13 +252,13 @@ __global__ __launch_bounds__(kThreads) void distill_kernel(DistillArgs a)
     const float weight = weight_of(a, row);
     if (weight == 0.0f) {
         if (alone) write_no_loss(a, row);
-        if (GRADIENT) write_zeros<kThreads>(x, to, 0, x.vectors);
+        if (GRADIENT) write_zeros<THREADS>(x, to, 0, x.vectors);
         return;
     }
     const Places places(a, row);
     if (!places.any) {
         if (alone) write_no_loss(a, row);
-        if (GRADIENT) write_zeros<kThreads>(x, to, 0, x.vectors);
+        if (GRADIENT) write_zeros<THREADS>(x, to, 0, x.vectors);
         return;
     }
     TokenLogits<TYPE> logit = {};
@@ -250,26 +269,26 @@ __global__ __launch_bounds__(kThreads) void distill_kernel(DistillArgs a)
         for (int from = first; from < last; from += kRange) {
             const int to = min(from + kRange, last);
             const Marks<N> marks{bits, from};
-            marks.clear(to - from, kThreads);
+            marks.clear(to - from, THREADS);
             __syncthreads();
             if (t < 64) marks.set(places, x.skip, to - from);
             __syncthreads();
             const auto add = [&](const Logits<TYPE> &v, int j) { adder.add(v, marks.of(min(j, to - 1))); };
-            walk<kThreads, 4>(x, from, to, [&](const Logits<TYPE> &v, int j, int) { add(v, j); }, add);
+            walk<THREADS, 4>(x, from, to, [&](const Logits<TYPE> &v, int j, int) { add(v, j); }, add);
             __syncthreads();
         }
     } else {
-        walk<kThreads, 4>(
+        walk<THREADS, 4>(
             x, first, last, [&](const Logits<TYPE> &v, int, int) { adder.add(v); }, [&](const Logits<TYPE> &v, int) { adder.add(v); });
     }
     logit.wait();  // before the barriers in join: the gradient may take the logits' place
-    const ExpSum s = join<false, kThreads>(adder.result(), a.c);
+    const ExpSum s = join<false, THREADS>(adder.result(), a.c);
     if (alone && t < 64) write_loss(a, row, places, logit, s);
     if (a.parts && t == 0) a.parts[blockIdx.x] = {s.reference, s.sum, s.second, 0.0f};
     if (GRADIENT) {
         const Slope slope = slope_of(a, weight, s, places.sum);
         const Span span(x, 0, x.vectors);
-        walk<kThreads, 4>(
+        walk<THREADS, 4>(
             x, 0, x.vectors,
             [&](const Logits<TYPE> &v, int j, int) {
                 float g[N];
@@ -281,7 +300,12 @@ __global__ __launch_bounds__(kThreads) void distill_kernel(DistillArgs a)
                 slope.of_others(v, a.c, g);
                 if (span.takes_end()) to.store_within(g, j);
             });
-        put_tokens(a, places, logit, slope, to);
+        __syncthreads();
+        if (t < 64) {
+            float q[2];
+            places.of_tokens(a.places, q);
+            put_tokens(a, places, q, logit, slope, to, 0, x.vectors);
+        }
     }
 }
 
@@ -309,14 +333,12 @@ __global__ __launch_bounds__(64) void distill_join_kernel(DistillArgs a)
 }
 
 // A segment of a row's gradient to a workgroup: from the sums that the launches in front left, or from those of an earlier call.  One wave makes
-// what the others need, while their logits are on the way.  The teacher's tokens of the segment, mostly none to some, are put right where
-// their vector is, so that nothing is written twice.
+// what the others need, while their logits are on the way.
 template <int TYPE, bool PAST>
 __global__ __launch_bounds__(kThreads) void distill_gradient_kernel(DistillArgs a)
 {
     constexpr int N = Logits<TYPE>::kCount;
-    __shared__ int token[kMaxPlaces], shared_found;
-    __shared__ float token_q[kMaxPlaces];
+    __shared__ int shared_tokens;  // whether the segment holds some of the teacher's; -1: the teacher has none
     __shared__ Slope shared_slope;
     const int t = threadIdx.x;
     const int local = quotient((int)blockIdx.x, a.by_segments), segment = (int)blockIdx.x - local * a.segments;
@@ -330,8 +352,10 @@ __global__ __launch_bounds__(kThreads) void distill_gradient_kernel(DistillArgs 
         return;
     }
     GradientSegment<kThreads, kGradientVectors, TYPE, PAST> segment_of(x, to, first, last);
+    Places places;
+    TokenLogits<TYPE> logit;
     if (t < 64) {
-        const Places places(a, row);
+        places = Places(a, row);
         segment_of.load();
         Slope slope;
         if (a.saved_sums) {
@@ -344,53 +368,32 @@ __global__ __launch_bounds__(kThreads) void distill_gradient_kernel(DistillArgs 
             s.second = part.second;
             slope = slope_of(a, weight, s, places.sum);
         }
-        bool here[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int at = places.token[h] + x.skip;
-            here[h] = places.token[h] >= 0 && at >= first * N && at < last * N;
-        }
-        const uint64_t low = __builtin_amdgcn_ballot_w64(here[0]), high = __builtin_amdgcn_ballot_w64(here[1]);
-        const int n = __builtin_popcountll(low) + __builtin_popcountll(high);
-        if (n) {
-            float q[2];
-            places.of_tokens(a.places, q);
-            const uint64_t before = ((uint64_t)1 << t) - 1;
-            if (here[0]) {
-                const int i = __builtin_popcountll(low & before);
-                token[i] = places.token[0];
-                token_q[i] = q[0];
-            }
-            if (here[1]) {
-                const int i = __builtin_popcountll(low) + __builtin_popcountll(high & before);
-                token[i] = places.token[1];
-                token_q[i] = q[1];
-            }
+        const bool here = places.template is_in<TYPE>(0, x.skip, first, last) || places.template is_in<TYPE>(1, x.skip, first, last);
+        const bool tokens = __builtin_amdgcn_ballot_w64(here) != 0;
+        if (tokens) {
+            logit.load(places, x);  // also of other segments, of which nothing is used: the gradient may have taken their place
+            logit.wait();
         }
         if (t == 0) {
-            shared_found = places.any ? n : -1;
+            shared_tokens = places.any ? (tokens ? 1 : 0) : -1;
             shared_slope = slope;
         }
     } else {
         segment_of.load();
     }
     __syncthreads();
-    const int n = shared_found;
-    if (n < 0) {
+    const int tokens = shared_tokens;
+    if (tokens < 0) {
         write_zeros<kThreads>(x, to, first, last);
         return;
     }
     const Slope slope = shared_slope;
-    segment_of.write([&](const Logits<TYPE> &v, int j, float(&g)[N]) {
-        slope.of_others(v, a.c, g);
-        for (int k = 0; k < n; ++k) {
-            const int at = token[k] - x.token(j);
-            if (at < 0 || at >= N) continue;
-            const float of_token = slope.of_token(v.at(at), token_q[k], a.c);
-#pragma unroll
-            for (int i = 0; i < N; ++i) g[i] = i == at ? of_token : g[i];
-        }
-    });
+    segment_of.write([&](const Logits<TYPE> &v, int, float(&g)[N]) { slope.of_others(v, a.c, g); });
+    if (!tokens) return;
+    float q[2];
+    if (t < 64) places.of_tokens(a.places, q);
+    __syncthreads();
+    if (t < 64) put_tokens(a, places, q, logit, slope, to, first, last);
 }
 
 // A row to a workgroup that holds it in its registers, so that it is read once for the loss and the gradient.  The row has a vector that lies inside it.
@@ -422,12 +425,14 @@ __global__ __launch_bounds__(THREADS) void distill_resident_kernel(DistillArgs a
         return;
     }
     TokenLogits<TYPE> logit = {};
+    float q[2] = {};
     if (t < 64) logit.load(places, x);
     if (REST) {
         __syncthreads();
         if (t < 64) marks.set(places, x.skip, x.vectors);
         __syncthreads();
     }
+    if (t < 64) places.of_tokens(a.places, q);  // while the logits are on the way
     Adder<REST ? 2 : 0> adder(a.c);
     held.go_through(span, [&](Logits<TYPE> &v, int j) {
         if (j >= span.end) v.fill();
@@ -456,15 +461,20 @@ __global__ __launch_bounds__(THREADS) void distill_resident_kernel(DistillArgs a
         slope.of_others(ends, a.c, g);
         to.store_within(g, end);
     }
-    put_tokens(a, places, logit, slope, to);
+    __syncthreads();
+    if (t < 64) put_tokens(a, places, q, logit, slope, to, 0, x.vectors);
 }
 
 template <int TYPE, bool REST>
-void launch_resident(const DistillArgs &a, int vectors, int64_t rows, hipStream_t stream)
+void launch_resident(const DistillArgs &a, int64_t rows, hipStream_t stream)
 {
-    const int grid = (int)rows;
-    if (vectors <= 4 * 256)
+    const int grid = (int)rows, vectors = logit_vectors(a.vocab, TYPE);
+    if (vectors <= wave_vectors(a.rows, 256))
+        distill_resident_kernel<TYPE, 64, 4, REST><<<grid, 64, 0, stream>>>(a);
+    else if (vectors <= 4 * 256)
         distill_resident_kernel<TYPE, 256, 4, REST><<<grid, 256, 0, stream>>>(a);
+    else if (vectors <= 4 * 512)
+        distill_resident_kernel<TYPE, 512, 4, REST><<<grid, 512, 0, stream>>>(a);
     else if (vectors <= 4 * 1024)
         distill_resident_kernel<TYPE, 1024, 4, REST><<<grid, 1024, 0, stream>>>(a);
     else if (vectors <= 8 * 1024)
@@ -473,40 +483,59 @@ void launch_resident(const DistillArgs &a, int vectors, int64_t rows, hipStream_
         distill_resident_kernel<TYPE, 1024, 16, REST><<<grid, 1024, 0, stream>>>(a);
 }
 
+template <int TYPE, int THREADS, bool PAST, bool GRADIENT>
+void launch_first(const DistillArgs &a, int grid, hipStream_t stream)
+{
+    (a.rest ? distill_kernel<TYPE, THREADS, true, PAST, GRADIENT> : distill_kernel<TYPE, THREADS, false, PAST, GRADIENT>)<<<grid, THREADS, 0, stream>>>(a);
+}
+
 template <int TYPE, bool PAST>
-void launch_sums(const DistillArgs &a, int64_t rows, hipStream_t stream)
+void launch_sums(const DistillArgs &a, int threads, int64_t rows, hipStream_t stream)
 {
     const int grid = (int)(rows * a.segments);
     if (a.gradient && !a.parts)
-        (a.rest ? distill_kernel<TYPE, true, PAST, true> : distill_kernel<TYPE, false, PAST, true>)<<<grid, kThreads, 0, stream>>>(a);
+        launch_first<TYPE, 256, PAST, true>(a, grid, stream);
+    else if (threads == 1024)
+        launch_first<TYPE, 1024, false, false>(a, grid, stream);
+    else if (threads == 64)
+        launch_first<TYPE, 64, false, false>(a, grid, stream);
     else
-        (a.rest ? distill_kernel<TYPE, true, PAST, false> : distill_kernel<TYPE, false, PAST, false>)<<<grid, kThreads, 0, stream>>>(a);
+        launch_first<TYPE, 256, PAST, false>(a, grid, stream);
     if (a.segments > 1) distill_join_kernel<TYPE><<<(int)rows, 64, 0, stream>>>(a);
 }
 
-void cut_into(DistillArgs &a, const LogitsCut &cut)
+void cut_into(DistillArgs &a, const LogitsPlan &plan)
 {
-    a.segments = cut.segments;
-    a.segment_vectors = cut.vectors;
-    a.by_segments = divisor((uint32_t)cut.segments);
+    a.segments = plan.segments;
+    a.segment_vectors = plan.vectors;
+    a.by_segments = divisor((uint32_t)plan.segments);
+}
+
+// Whether a row is held in registers for its loss and its gradient.  Few long rows are cut into segments instead (1 row of 64000 bf16 logits 10.8 us
+// held and 11.6 in segments, of 128000 16.6 and 11.5; 32 rows of them 18.1 and 16.1, 64 18.5 and 19.7).
+bool is_resident(int64_t rows, int32_t vocab, int32_t type, bool workspace)
+{
+    const int vectors = logit_vectors(vocab, type);
+    if (vocab < (type == QUAMBA_F32 ? 8 : 16) || vectors > 16 * 1024) return false;  // it has no vector of its own, or too many
+    return !workspace || rows * 8 > compute_units() || vectors <= 10000;
 }
 
 template <int TYPE, bool PAST>
 hipError_t launch(DistillArgs a, void *workspace, hipStream_t stream)
 {
-    const int vectors = (a.vocab + 2 * Logits<TYPE>::kCount - 2) / Logits<TYPE>::kCount;  // the most that a row's address may make of it
-    const bool sums = !a.saved_sums, resident = sums && a.gradient && vectors <= 16 * 1024 && a.vocab >= 2 * Logits<TYPE>::kCount;
-    const LogitsCut cut = workspace ? logits_cut(a.rows, a.vocab, TYPE) : LogitsCut{1, 0}, gradient = gradient_cut(a.vocab, TYPE, kThreads * kGradientVectors);
+    const bool sums = !a.saved_sums, resident = sums && a.gradient && is_resident(a.rows, a.vocab, TYPE, workspace != nullptr);
+    const LogitsPlan plan = logits_plan(a.rows, a.vocab, TYPE, LogitsWork::distance, workspace != nullptr);
+    const LogitsPlan gradient = gradient_plan(a.vocab, TYPE, kThreads * kGradientVectors);
     a.parts = static_cast<LogitsPart *>(workspace);
-    a.row_parts = cut.segments;
+    a.row_parts = plan.segments;
     const int64_t most = a.gradient && !resident ? kRowsOfALaunch / gradient.segments : kRowsOfALaunch;
     for (a.first_row = 0; a.first_row < a.rows; a.first_row += most) {
         const int64_t rows = std::min(a.rows - a.first_row, most);
         if (resident) {
-            a.rest ? launch_resident<TYPE, true>(a, vectors, rows, stream) : launch_resident<TYPE, false>(a, vectors, rows, stream);
+            a.rest ? launch_resident<TYPE, true>(a, rows, stream) : launch_resident<TYPE, false>(a, rows, stream);
         } else {
-            cut_into(a, cut);
-            if (sums) launch_sums<TYPE, PAST>(a, rows, stream);
+            cut_into(a, plan);
+            if (sums) launch_sums<TYPE, PAST>(a, plan.threads, rows, stream);
             cut_into(a, gradient);
             if (a.gradient && (a.parts || !sums)) distill_gradient_kernel<TYPE, PAST><<<(int)(rows * a.segments), kThreads, 0, stream>>>(a);
         }
@@ -528,7 +557,7 @@ size_t distill_workspace_bytes(int64_t rows, int32_t vocab)
 {
     size_t most = 0;  // over the types
     for (const int type : {QUAMBA_F32, QUAMBA_BF16}) {
-        most = std::max(most, (size_t)rows * logits_cut(rows, vocab, type).segments * sizeof(LogitsPart));
+        most = std::max(most, (size_t)rows * logits_plan(rows, vocab, type, LogitsWork::distance, true).segments * sizeof(LogitsPart));
     }
     return most;
 }

@@ -245,8 +245,8 @@ __device__ __forceinline__ float largest(const Logits<TYPE> &v)
 
 // A thread's sum while it grows.  SECOND: 0 none, 1 times e, 2 without the logits that are marked.  Mostly e is made by one operation, x c -
 // offset with offset = reference c: the product is not rounded, and what the offset's rounding leaves is the same for all terms, so it
-// is taken out at the end.  A vector for which the reference is too low (its sum shows it, so no largest logit is sought), one without an
-// entropy's term (0 times infinity), and all where reference c leaves fp32's range are made from the difference.
+// is taken out at the end.  A vector for which the reference is too low (its sum shows it, so no largest logit is sought) and all where
+// reference c leaves fp32's range are made from the difference.
 template <int SECOND>
 struct Adder {
     ExpSum s;
@@ -271,14 +271,15 @@ struct Adder {
     __device__ __forceinline__ void add(const Logits<TYPE> &v, uint32_t marked = 0)
     {
         constexpr int N = Logits<TYPE>::kCount;
-        float part = 0.0f, weighted = s.second;
+        float p[N], part = 0.0f, weighted = s.second;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const float e = fmaf(v[i], c, -offset), p = exp2_of(e);
-            part += p;
-            if (SECOND == 1) weighted = fmaf(p, e, weighted);
+            const float e = fmaf(v[i], c, -offset);
+            p[i] = exp2_of(e);
+            part += p[i];
+            if (SECOND == 1) weighted = fmaf(p[i], fmaxf(e, kFarBelow), weighted);
         }
-        if (!(part <= 256.0f * N) || (SECOND == 1 && weighted != weighted) || (SECOND == 2 && marked)) {
+        if (!(part <= 256.0f * N)) {
             const float top = largest(v);
             if ((top - s.reference) * c > 8.0f) {
                 result();
@@ -287,22 +288,26 @@ struct Adder {
                 shift(residue());
             }
             const float r = residue();
-            float kept = 0.0f;
             part = 0.0f;
             weighted = s.second;
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const float e = fmaf(v[i] - s.reference, c, r), p = exp2_of(e);
-                part += p;
-                if (SECOND == 1) weighted = fmaf(p, fmaxf(e, kFarBelow), weighted);
-                if (SECOND == 2) kept += marked >> i & 1 ? 0.0f : p;
+                const float e = fmaf(v[i] - s.reference, c, r);
+                p[i] = exp2_of(e);
+                part += p[i];
+                if (SECOND == 1) weighted = fmaf(p[i], fmaxf(e, kFarBelow), weighted);
             }
-            if (SECOND == 2) s.second += kept;
-        } else if (SECOND == 2) {
-            s.second += part;
         }
         s.sum += part;
         if (SECOND == 1) s.second = weighted;
+        if (SECOND == 2) {
+            if (marked) {
+                part = 0.0f;
+#pragma unroll
+                for (int i = 0; i < N; ++i) part += marked >> i & 1 ? 0.0f : p[i];
+            }
+            s.second += part;
+        }
     }
 };
 
@@ -373,7 +378,7 @@ struct TopKeys {  // in LDS
     uint64_t all[WAVES * kMaxChoices];
     uint32_t bound;  // ordered; some keys of a wave that has set it are above, `count` of them
     int n, groups;
-    uint32_t tops[256];
+    uint32_t tops[WAVES > 1 ? 256 : 1];
     uint16_t group[WAVES * 64 * kTurns];
 };
 __device__ __forceinline__ float next_below(float v) { return of_ordered(ordered(v + 0.0f) - (v == 0.0f ? 2 : 1)); }  // below 0 is not -0
@@ -526,27 +531,39 @@ __device__ __forceinline__ uint64_t key_of(float logit, int token) { return (uin
 // The best tokens of vectors first .. last - 1 of a row that have been walked through: out(i, key) for the i-th largest, i < count, 0 where there
 // are no more.  tops[u] is the thread's largest logit among the vectors of its turns u.
 //
-// `count` threads have a logit at least as large as the count-th largest of their own largest ones, so nothing
+// `count` of 256 threads, fours of threads or turns of a lane have a logit at least as large as the count-th largest of their own largest ones, so nothing
 // below that is among the best, and little more than `count` logits are above: the turns that hold one are read again, from the caches,
 // and what reaches the bound is ranked by counting.  A list that is kept up to date while the row goes by was slower: of some 250 vectors of a
 // wave a tenth to a half brought a better token, for ten times the work of one that did not.  Where so many logits are equal that those at
 // the bound do not fit, such lists are made after all.
-template <int U, int TYPE, bool PAST, typename Out>
-__device__ __forceinline__ void best_tokens(TopKeys<4> &shared, const Row<TYPE, PAST> &row, int first, int last, const float (&tops)[U], int count,
-                                            const Out &out)
+template <int THREADS, int U, int TYPE, bool PAST, typename Out>
+__device__ __forceinline__ void best_tokens(TopKeys<THREADS / 64> &shared, const Row<TYPE, PAST> &row, int first, int last, const float (&tops)[U],
+                                            int count, const Out &out)
 {
-    constexpr int THREADS = 256, N = Logits<TYPE>::kCount, kStep = THREADS * U, kRoom = 4 * kListed;
+    constexpr int WAVES = THREADS / 64, N = Logits<TYPE>::kCount, kStep = THREADS * U, kRoom = WAVES * kListed, kShare = THREADS > 256 ? THREADS / 256 : 1;
     const int t = threadIdx.x, lane = t & 63;
     const Span span(row, first, last);
     float top = tops[0];
 #pragma unroll
     for (int u = 1; u < U; ++u) top = fmaxf(top, tops[u]);
-    shared.tops[t] = top > -__builtin_inff() ? ordered(top + 0.0f) : 0u;
-    if (t == 0) shared.n = shared.groups = 0;
-    __syncthreads();
+    static_assert(THREADS == 64 || THREADS == 256 || THREADS == 1024, "256 largest logits: of a lane's turns, of a thread, of a quad");
+    static_assert(U == 4, "turns of a lane");
     uint32_t mine[4], bound = 0;
+    if (t == 0) shared.n = shared.groups = 0;
+    if (THREADS == 64) {
 #pragma unroll
-    for (int w = 0; w < 4; ++w) mine[w] = shared.tops[w * 64 + lane];
+        for (int u = 0; u < U; ++u) mine[u] = tops[u] > -__builtin_inff() ? ordered(tops[u] + 0.0f) : 0u;
+        __syncthreads();
+    } else {
+        if (kShare == 4) {
+            top = fmaxf(top, dpp_move<0xB1>(top));
+            top = fmaxf(top, dpp_move<0x4E>(top));
+        }
+        if (t % kShare == 0) shared.tops[t / kShare] = top > -__builtin_inff() ? ordered(top + 0.0f) : 0u;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < 4; ++w) mine[w] = shared.tops[w * 64 + lane];
+    }
 #pragma unroll
     for (int bit = 31; bit >= 16; --bit) {
         const uint32_t higher = bound | 1u << bit;
@@ -586,7 +603,7 @@ __device__ __forceinline__ void best_tokens(TopKeys<4> &shared, const Row<TYPE, 
     const int n = shared.n;
     __syncthreads();  // all know it
     if (n > kRoom) {
-        TopList<4> list(shared, count);
+        TopList<WAVES> list(shared, count);
         __syncthreads();
         walk<THREADS, 1>(
             row, first, last,
@@ -617,6 +634,16 @@ __device__ __forceinline__ uint32_t bits_of(float v)
     return TYPE == QUAMBA_F32 ? __builtin_bit_cast(uint32_t, v) : TYPE == QUAMBA_F16 ? f32_to_f16_bits(v) : __builtin_bit_cast(uint16_t, (__bf16)v);
 }
 
+template <int TYPE>
+__device__ __forceinline__ uint32_t pair_of(float low, float high)
+{
+    typedef float Floats __attribute__((ext_vector_type(2)));
+    typedef __bf16 Brain __attribute__((ext_vector_type(2)));
+    typedef _Float16 Half __attribute__((ext_vector_type(2)));
+    const Floats v = {low, high};
+    return TYPE == QUAMBA_BF16 ? __builtin_bit_cast(uint32_t, __builtin_convertvector(v, Brain)) : __builtin_bit_cast(uint32_t, __builtin_convertvector(v, Half));
+}
+
 // A row of the gradient, cut into the vectors of its row of logits: it may lie elsewhere in 16 bytes.
 template <int TYPE, bool PAST = false>
 struct GradientRow {
@@ -631,7 +658,7 @@ struct GradientRow {
     {
         uint32_t w[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = kBytes == 4 ? bits_of<TYPE>(v[i]) : bits_of<TYPE>(v[2 * i % kCount]) | bits_of<TYPE>(v[(2 * i + 1) % kCount]) << 16;
+        for (int i = 0; i < 4; ++i) w[i] = kBytes == 4 ? bits_of<TYPE>(v[i]) : pair_of<TYPE>(v[2 * i % kCount], v[(2 * i + 1) % kCount]);
         typedef uint32_t Vec __attribute__((ext_vector_type(4), aligned(2)));  // at the type's alignment
         const Vec q = {w[0], w[1], w[2], w[3]};
         Vec *p = reinterpret_cast<Vec *>(base + (uint32_t)j * 16u);

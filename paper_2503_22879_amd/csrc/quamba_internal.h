@@ -455,12 +455,15 @@ hipError_t launch_beam_reorder(int32_t batch, int32_t beams, const int32_t *pare
 constexpr int32_t kMaxVocab = 1 << 26;
 constexpr int64_t kMaxLogitRows = (int64_t)1 << 31;
 constexpr int kMaxPlaces = 128;  // of a teacher
-// A row's segments, each of so many vectors of 16 bytes.
-struct LogitsCut {
-    int segments, vectors;
+// A row's segments, each of so many vectors of 16 bytes (of one segment: 0, all), and the threads of a workgroup that takes one.
+struct LogitsPlan {
+    int threads, segments, vectors;
 };
-LogitsCut logits_cut(int64_t rows, int32_t vocab, int32_t type);      // of a pass that sums
-LogitsCut gradient_cut(int32_t vocab, int32_t type, int vectors);    // into segments of so many
+enum class LogitsWork : int { sums, alternatives, distance };
+LogitsPlan logits_plan(int64_t rows, int32_t vocab, int32_t type, LogitsWork work, bool workspace);  // of a pass that sums
+LogitsPlan gradient_plan(int32_t vocab, int32_t type, int vectors);                                 // into segments of at most so many
+int logit_vectors(int32_t vocab, int32_t type);
+int wave_vectors(int64_t rows, int most);  // of rows that a wave takes
 bool logits_past_caches(int64_t rows, int32_t vocab, int32_t type);  // whether the logits are not to stay in the caches
 // What a segment leaves: its sums of exponentials against a reference logit.
 struct LogitsPart {

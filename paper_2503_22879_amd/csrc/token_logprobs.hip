@@ -60,16 +60,16 @@ __device__ __forceinline__ void write_padding(const LogprobArgs &a, int64_t row)
 }
 
 // A segment of a row to a workgroup; where a row has one only, that is all.
-template <int TYPE, bool ENTROPY, bool TOP, bool PAST>
-__global__ __launch_bounds__(kThreads) void token_logprobs_kernel(LogprobArgs a)
+template <int TYPE, int THREADS, bool ENTROPY, bool TOP, bool PAST>
+__global__ __launch_bounds__(THREADS) void token_logprobs_kernel(LogprobArgs a)
 {
-    __shared__ TopKeys<TOP ? 4 : 1> keys;
+    __shared__ TopKeys<TOP ? THREADS / 64 : 1> keys;
     const int t = threadIdx.x;
     const int local = quotient((int)blockIdx.x, a.by_segments), segment = (int)blockIdx.x - local * a.segments;
     const int64_t row = a.first_row + local;
     const bool alone = a.segments == 1;
     if (is_padding(a, row)) {
-        if (alone) write_padding<kThreads>(a, row);
+        if (alone) write_padding<THREADS>(a, row);
         return;
     }
     const Row<TYPE, PAST> x(a.logits, row * a.stride, a.vocab);
@@ -83,24 +83,24 @@ __global__ __launch_bounds__(kThreads) void token_logprobs_kernel(LogprobArgs a)
         float tops[kTurns];
 #pragma unroll
         for (int u = 0; u < kTurns; ++u) tops[u] = -__builtin_inff();
-        walk<kThreads, kTurns>(
+        walk<THREADS, kTurns>(
             x, first, last,
             [&](const Logits<TYPE> &v, int, int u) {
                 adder.add(v);
                 tops[u] = fmaxf(tops[u], largest(v));
             },
             at_end);
-        s = join<ENTROPY, kThreads>(adder.result(), a.c);
+        s = join<ENTROPY, THREADS>(adder.result(), a.c);
         const Finish finish(a, row, s);
-        best_tokens(keys, x, first, last, tops, a.count, [&](int i, uint64_t key) {
+        best_tokens<THREADS>(keys, x, first, last, tops, a.count, [&](int i, uint64_t key) {
             if (alone)
                 finish.alternative(i, key);
             else
                 a.best[(int64_t)blockIdx.x * a.count + i] = key;
         });
     } else {
-        walk<kThreads, kTurns>(x, first, last, [&](const Logits<TYPE> &v, int, int) { adder.add(v); }, at_end);
-        s = join<ENTROPY, kThreads>(adder.result(), a.c);
+        walk<THREADS, kTurns>(x, first, last, [&](const Logits<TYPE> &v, int, int) { adder.add(v); }, at_end);
+        s = join<ENTROPY, THREADS>(adder.result(), a.c);
     }
     if (t != 0) return;
     if (alone)
@@ -179,24 +179,40 @@ __global__ __launch_bounds__(kThreads) void token_logprobs_backward_kernel(Logpr
 
 }  // namespace
 
-// Segments of a row: none where the rows alone fill the device, else enough to give every compute unit 4 workgroups, of at least 512 vectors.
-LogitsCut logits_cut(int64_t rows, int32_t vocab, int32_t type)
+// How many vectors of 16 bytes a row is at most, whatever its address.
+int logit_vectors(int32_t vocab, int32_t type)
 {
     const int per_vector = type == QUAMBA_F32 ? 4 : 8;
-    const int vectors = (vocab + 2 * per_vector - 2) / per_vector;  // the most that a row's address may make of it
-    const int64_t want = (4 * compute_units() + rows - 1) / std::max<int64_t>(rows, 1);
-    const int least = 512;
-    const int segments = (int)std::max<int64_t>(1, std::min<int64_t>({want, (vectors + least - 1) / least, 256}));
-    const int each = (vectors + segments - 1) / segments;
-    return {(vectors + each - 1) / each, each};
+    return (vocab + 2 * per_vector - 2) / per_vector;
 }
 
-LogitsCut gradient_cut(int32_t vocab, int32_t type, int vectors)
+// Rows of few vectors take a wave each: there is nothing to wait for in it, and four times the rows are on a compute unit (10000 rows of bf16: 256
+// logits 11.8 -> 5.5 us, 2000 14.3 -> 10.4, 4000 18.4 -> 15.3, with 8 alternatives 29 -> 12.4, 31 -> 16.7, 36 -> 21.5; 100 rows of 2000 4.3 -> 4.3 and 5.6
+// -> 6.0).
+int wave_vectors(int64_t rows, int most) { return (int)std::min<int64_t>(most, std::max<int64_t>(128, rows / 4)); }
+
+// A workgroup of 256 threads takes a row, but where rows are few and long.  1024 threads then take one on a compute unit of its own (256 rows of
+// 200000 fp32 logits 44 -> 35 us, 128 of 128000 bf16 ones with 8 alternatives 17.8 -> 14.2; up to the borders below both take about as long).
+// Where a row still takes longer than a second launch that joins segments, it is cut into these (1 row of 128000 bf16 logits 15 us by 256
+// threads, 11 by 1024, 7.5 in segments; with alternatives 13.8, 12.7 and 10.4; 128 rows with alternatives 17.8, 14.2 and 16.0; 64 rows of 128000
+// fp32 ones with 20 of them and the entropy 21.6 and 17.5).
+LogitsPlan logits_plan(int64_t rows, int32_t vocab, int32_t type, LogitsWork work, bool workspace)
 {
-    const int per_vector = type == QUAMBA_F32 ? 4 : 8;
-    const int all = (vocab + 2 * per_vector - 2) / per_vector;
+    const int units = compute_units(), vectors = logit_vectors(vocab, type);
+    const bool best = work == LogitsWork::alternatives;
+    if (vectors <= wave_vectors(rows, 512)) return {64, 1, 0};
+    if (workspace && (best ? rows * 4 <= units && vocab > 100000 : rows * 8 <= units && vocab > 60000)) {
+        const int segments = (int)std::min<int64_t>({(4 * units + rows - 1) / rows, (vectors + 511) / 512, 256}), each = (vectors + segments - 1) / segments;
+        return {256, (vectors + each - 1) / each, each};
+    }
+    return {rows <= units && vectors > (best ? 8000 : 4000) ? 1024 : 256, 1, 0};
+}
+
+LogitsPlan gradient_plan(int32_t vocab, int32_t type, int vectors)
+{
+    const int all = logit_vectors(vocab, type);
     const int segments = (all + vectors - 1) / vectors, each = std::min(vectors, ((all + segments - 1) / segments + 63) / 64 * 64);
-    return {(all + each - 1) / each, each};
+    return {kThreads, (all + each - 1) / each, each};
 }
 
 bool logits_past_caches(int64_t rows, int32_t vocab, int32_t type)
@@ -206,30 +222,45 @@ bool logits_past_caches(int64_t rows, int32_t vocab, int32_t type)
 
 namespace {
 
-template <int TYPE, bool PAST>
-void launch_rows(const LogprobArgs &a, int64_t rows, hipStream_t stream)
+template <int TYPE, int THREADS, bool PAST>
+void launch_first(const LogprobArgs &a, int grid, hipStream_t stream)
 {
-    const auto kernel = a.count ? (a.entropies ? token_logprobs_kernel<TYPE, true, true, PAST> : token_logprobs_kernel<TYPE, false, true, PAST>)
-                                : (a.entropies ? token_logprobs_kernel<TYPE, true, false, PAST> : token_logprobs_kernel<TYPE, false, false, PAST>);
-    kernel<<<(int)(rows * a.segments), kThreads, 0, stream>>>(a);
+    const auto kernel = a.count ? (a.entropies ? token_logprobs_kernel<TYPE, THREADS, true, true, PAST> : token_logprobs_kernel<TYPE, THREADS, false, true, PAST>)
+                                : (a.entropies ? token_logprobs_kernel<TYPE, THREADS, true, false, PAST> : token_logprobs_kernel<TYPE, THREADS, false, false, PAST>);
+    kernel<<<grid, THREADS, 0, stream>>>(a);
+}
+
+template <int TYPE>
+void launch_rows(const LogprobArgs &a, int threads, int64_t rows, bool past, hipStream_t stream)
+{
+    const int grid = (int)(rows * a.segments);
+    if (threads == 1024)
+        launch_first<TYPE, 1024, false>(a, grid, stream);
+    else if (threads == 64)
+        launch_first<TYPE, 64, false>(a, grid, stream);
+    else if (past)
+        launch_first<TYPE, 256, true>(a, grid, stream);
+    else
+        launch_first<TYPE, 256, false>(a, grid, stream);
     if (a.segments == 1) return;
     const auto join_kernel = a.count ? token_logprobs_join_kernel<TYPE, true> : token_logprobs_join_kernel<TYPE, false>;
     join_kernel<<<(int)rows, kThreads, 0, stream>>>(a);
 }
 
+LogitsWork work_of(int count) { return count ? LogitsWork::alternatives : LogitsWork::sums; }
+
 template <int TYPE>
 hipError_t launch(LogprobArgs a, void *workspace, hipStream_t stream)
 {
-    const LogitsCut cut = workspace ? logits_cut(a.rows, a.vocab, TYPE) : LogitsCut{1, 0};
-    a.segments = cut.segments;
-    a.segment_vectors = cut.vectors;
-    a.by_segments = divisor((uint32_t)cut.segments);
+    const LogitsPlan plan = logits_plan(a.rows, a.vocab, TYPE, work_of(a.count), workspace != nullptr);
+    a.segments = plan.segments;
+    a.segment_vectors = plan.vectors;
+    a.by_segments = divisor((uint32_t)plan.segments);
     a.parts = static_cast<LogitsPart *>(workspace);
-    a.best = reinterpret_cast<uint64_t *>(a.parts + (cut.segments > 1 ? a.rows * cut.segments : 0));
+    a.best = reinterpret_cast<uint64_t *>(a.parts + (plan.segments > 1 ? a.rows * plan.segments : 0));
     const bool past = logits_past_caches(a.rows, a.vocab, TYPE);
     for (a.first_row = 0; a.first_row < a.rows; a.first_row += kRowsOfALaunch) {
-        const int64_t rows = std::min(a.rows - a.first_row, kRowsOfALaunch);
-        past ? launch_rows<TYPE, true>(a, rows, stream) : launch_rows<TYPE, false>(a, rows, stream);
+        launch_rows<TYPE>(a, plan.threads, std::min(a.rows - a.first_row, kRowsOfALaunch), past, stream);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -239,14 +270,14 @@ hipError_t launch(LogprobArgs a, void *workspace, hipStream_t stream)
 template <int TYPE, bool PAST>
 hipError_t launch_gradient(LogprobGradientArgs a, hipStream_t stream)
 {
-    const LogitsCut cut = gradient_cut(a.vocab, TYPE, kThreads * kGradientVectors);
-    a.segments = cut.segments;
-    a.segment_vectors = cut.vectors;
-    a.by_segments = divisor((uint32_t)cut.segments);
+    const LogitsPlan plan = gradient_plan(a.vocab, TYPE, kThreads * kGradientVectors);
+    a.segments = plan.segments;
+    a.segment_vectors = plan.vectors;
+    a.by_segments = divisor((uint32_t)plan.segments);
     const auto kernel = a.grad_entropies ? token_logprobs_backward_kernel<TYPE, true, PAST> : token_logprobs_backward_kernel<TYPE, false, PAST>;
-    const int64_t most = kRowsOfALaunch / cut.segments;
+    const int64_t most = kRowsOfALaunch / plan.segments;
     for (a.first_row = 0; a.first_row < a.rows; a.first_row += most) {
-        kernel<<<(int)(std::min(a.rows - a.first_row, most) * cut.segments), kThreads, 0, stream>>>(a);
+        kernel<<<(int)(std::min(a.rows - a.first_row, most) * plan.segments), kThreads, 0, stream>>>(a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -265,7 +296,7 @@ size_t token_logprobs_workspace_bytes(int64_t rows, int32_t vocab, int32_t count
 {
     size_t most = 0;  // over the types
     for (const int type : {QUAMBA_F32, QUAMBA_BF16}) {
-        const int segments = logits_cut(rows, vocab, type).segments;
+        const int segments = logits_plan(rows, vocab, type, work_of(count), true).segments;
         if (segments > 1) most = std::max(most, (size_t)rows * segments * (sizeof(LogitsPart) + sizeof(uint64_t) * count));
     }
     return most;
