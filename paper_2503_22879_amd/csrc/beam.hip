@@ -200,13 +200,6 @@ __global__ __launch_bounds__(kThreads) void beam_pieces_kernel(SelectArgs a, int
     }
 }
 
-template <int CTRL>
-__device__ __forceinline__ float row_step_max(float v) { return fmaxf(v, dpp_move<CTRL>(v)); }
-__device__ __forceinline__ float row_max(float v)  // of 16 lanes
-{
-    return row_step_max<0x140>(row_step_max<0x141>(row_step_max<0x4E>(row_step_max<0xB1>(v))));
-}
-
 // A workgroup to a sequence: 16 lanes join a beam's pieces, then all take the best of the pieces' best.  These are gone through place by
 // place, the first ones of all pieces, then the second ones: each piece's fall, so there are no better ones left once a place of every
 // piece brought none, mostly after the first round (1 sequence of 16 beams, 200000 logits each, 32 choices: 112 us in the order of the

@@ -7,6 +7,7 @@
 // difference would not be); the gradient is written as if no token were the teacher's, but for those, which come from their logits and
 // places.  Bound: HBM.
 #include <algorithm>
+#include <type_traits>
 
 #include "logits.h"
 
@@ -83,22 +84,45 @@ struct Places {
         const int at = token[h] + skip;
         return token[h] >= 0 && at >= first * Logits<TYPE>::kCount && at < last * Logits<TYPE>::kCount;
     }
-    // The sum of q over all places with the token of place h of the lane: a token may have several.  By the whole wave.
-    __device__ __forceinline__ void of_tokens(int places, float (&all)[2]) const
+    // The sum of q over all places with the token of place h of the lane, which may have several, and whether that place is its first.  By the
+    // whole wave.  Places are compared with one another only where two tokens have the same low bits: for each place that is some 10 operations of a
+    // wave, which took longer than all else in short rows (4096 rows of 2000, 64 places: 15.4 us, 12.4 without).
+    struct Seen {
+        static constexpr int kBits = 1 << 15;
+        uint32_t words[kBits / 32];
+    };
+    __device__ __forceinline__ void of_tokens(Seen &seen, int places, float (&all)[2], bool (&first)[2]) const
     {
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int i = 0; i < Seen::kBits / 32; i += 64) seen.words[i + lane] = 0;
+        bool twice = false;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            if (token[h] >= 0) {
+                const uint32_t at = (uint32_t)token[h] % Seen::kBits;
+                twice = twice || (atomicOr(&seen.words[at / 32], 1u << at % 32) >> at % 32 & 1);
+            }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            all[h] = q[h];
+            first[h] = true;
+        }
+        if (__builtin_amdgcn_ballot_w64(twice) == 0) return;
         all[0] = all[1] = 0.0f;
-        for (int i = 0; i < min(places, 64); ++i) {
-            const int t = __builtin_amdgcn_readlane(token[0], i);
-            const float p = from_bits(__builtin_amdgcn_readlane(__builtin_bit_cast(int, q[0]), i));
-            all[0] += token[0] == t ? p : 0.0f;
-            if (places > 64) all[1] += token[1] == t ? p : 0.0f;
-        }
-        for (int i = 64; i < places; ++i) {
-            const int t = __builtin_amdgcn_readlane(token[1], i - 64);
-            const float p = from_bits(__builtin_amdgcn_readlane(__builtin_bit_cast(int, q[1]), i - 64));
-            all[0] += token[0] == t ? p : 0.0f;
-            all[1] += token[1] == t ? p : 0.0f;
-        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            for (int i = 0; i < 64 && 64 * h + i < places; i += 8) {  // eight at a time: a lane's value is a while on its way to all
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int t = __builtin_amdgcn_readlane(token[h], i + j);
+                    const float p = from_bits(__builtin_amdgcn_readlane(__builtin_bit_cast(int, q[h]), i + j));
+                    all[0] += token[0] == t ? p : 0.0f;
+                    all[1] += token[1] == t ? p : 0.0f;
+                    first[0] = first[0] && (token[0] != t || 64 * h + i + j >= lane);
+                    first[1] = first[1] && (token[1] != t || 64 * h + i + j >= lane + 64);
+                }
+            }
     }
 };
 
@@ -142,14 +166,25 @@ __device__ __forceinline__ Slope slope_of(const DistillArgs &a, float weight, fl
     return s;
 }
 
-// Whether the rest counts: there is a token outside the teacher's that may come (or no number).
-__device__ __forceinline__ bool has_rest(const DistillArgs &a, const ExpSum &s) { return a.rest && s.second != 0.0f; }
+// A row's sums of exponentials, over all tokens and over those without a place, each against a reference logit of its own.
+struct RowSums {
+    float reference, sum;  // NaN for a row that has no distribution
+    float rest_reference, rest;
+    RowSums() = default;
+    __device__ __forceinline__ RowSums(float reference_, float sum_, float rest_reference_, float rest_)
+        : reference(reference_), sum(sum_ > 0.0f ? sum_ : __builtin_nanf("")), rest_reference(rest_reference_), rest(rest_)
+    {
+    }
+    __device__ __forceinline__ explicit RowSums(const ExpSum &s) : RowSums(s.reference, s.sum, s.reference, s.second) {}
+    // Whether the rest counts: there is a token outside the teacher's that may come (or no number).
+    __device__ __forceinline__ bool has_rest(const DistillArgs &a) const { return a.rest && rest != 0.0f; }
+};
 
 // From a row's sums, ...
-__device__ __forceinline__ Slope slope_of(const DistillArgs &a, float weight, const ExpSum &s, float sum_q)
+__device__ __forceinline__ Slope slope_of(const DistillArgs &a, float weight, const RowSums &s, float sum_q)
 {
-    const float sum = s.sum > 0.0f ? s.sum : __builtin_nanf("");
-    return slope_of(a, weight, s.reference, log2f(sum), s.reference, log2f(s.second), s.second / sum, has_rest(a, s), sum_q);
+    return slope_of(a, weight, s.reference, log2f(s.sum), s.rest_reference, log2f(s.rest), s.rest * exp2_of((s.rest_reference - s.reference) * a.c) / s.sum,
+                    s.has_rest(a), sum_q);
 }
 // ... and from the log sums that a call before has left.
 __device__ __forceinline__ Slope slope_of(const DistillArgs &a, float weight, int64_t row, float sum_q)
@@ -165,12 +200,19 @@ __device__ __forceinline__ float weight_of(const DistillArgs &a, int64_t row) { 
 // The logits at the teacher's tokens: asked for early, values late.
 template <int TYPE>
 struct TokenLogits {
-    uint32_t bits[2];
+    std::conditional_t<TYPE == QUAMBA_F32, uint32_t, uint16_t> bits[2];  // wider, and they would be waited for where they are made so
     template <bool PAST>
     __device__ __forceinline__ void load(const Places &p, const Row<TYPE, PAST> &x)
     {
 #pragma unroll
         for (int h = 0; h < 2; ++h) bits[h] = x.bits(0, max(p.token[h], 0) + x.skip);
+    }
+    // ... in vectors first .. last - 1; where a token is elsewhere, the first logit there.
+    template <bool PAST>
+    __device__ __forceinline__ void load(const Places &p, const Row<TYPE, PAST> &x, int first, int last)
+    {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) bits[h] = x.bits(0, p.template is_in<TYPE>(h, x.skip, first, last) ? p.token[h] + x.skip : max(first * Logits<TYPE>::kCount, x.skip));
     }
     __device__ __forceinline__ float operator[](int h) const { return Row<TYPE>::value(bits[h]); }
     // ... that are here, behind this.
@@ -179,20 +221,20 @@ struct TokenLogits {
 
 // The loss of a row and its log sums, by one wave.
 template <int TYPE>
-__device__ __forceinline__ void write_loss(const DistillArgs &a, int64_t row, const Places &p, const TokenLogits<TYPE> &logit, const ExpSum &s)
+__device__ __forceinline__ void write_loss(const DistillArgs &a, int64_t row, const Places &p, const TokenLogits<TYPE> &logit, const RowSums &s)
 {
-    const float log_sum = s.sum > 0.0f ? logf(s.sum) : __builtin_nanf("");
+    const float log_sum = logf(s.sum), log_rest = logf(s.rest);
     float loss = 0.0f;
 #pragma unroll
     for (int h = 0; h < 2; ++h)
         if (p.token[h] >= 0 && p.q[h] != 0.0f) loss += p.q[h] * (p.log_q[h] - ((logit[h] - s.reference) * a.per_temperature - log_sum));
     loss = group_sum<64>(loss);
     if ((threadIdx.x & 63) != 0) return;
-    const float left = fmaxf(1.0f - p.sum, 0.0f), log_rest = logf(s.second);
-    if (has_rest(a, s) && left > 0.0f) loss += left * (logf(left) - (log_rest - log_sum));
+    const float left = fmaxf(1.0f - p.sum, 0.0f);
+    if (s.has_rest(a) && left > 0.0f) loss += left * (logf(left) - ((s.rest_reference - s.reference) * a.per_temperature + (log_rest - log_sum)));
     a.losses[row] = log_sum == log_sum ? loss : log_sum;  // a row without a distribution may have no place that shows it
     if (a.log_sums) a.log_sums[row] = fmaf(s.reference, a.per_temperature, log_sum);
-    if (a.log_rests) a.log_rests[row] = a.rest ? fmaf(s.reference, a.per_temperature, log_rest) : 0.0f;
+    if (a.log_rests) a.log_rests[row] = a.rest ? fmaf(s.rest_reference, a.per_temperature, log_rest) : 0.0f;
 }
 __device__ __forceinline__ void write_no_loss(const DistillArgs &a, int64_t row)
 {
@@ -243,6 +285,7 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(DistillArgs a)
 {
     constexpr int N = Logits<TYPE>::kCount, kRange = (1 << 17) / N;  // vectors that are marked at once
     __shared__ uint32_t bits[REST ? (1 << 17) / 32 : 1];
+    __shared__ Places::Seen seen;
     const int t = threadIdx.x;
     const int local = quotient((int)blockIdx.x, a.by_segments), segment = (int)blockIdx.x - local * a.segments;
     const int64_t row = a.first_row + local;
@@ -283,10 +326,10 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(DistillArgs a)
     }
     logit.wait();  // before the barriers in join: the gradient may take the logits' place
     const ExpSum s = join<false, THREADS>(adder.result(), a.c);
-    if (alone && t < 64) write_loss(a, row, places, logit, s);
+    if (alone && t < 64) write_loss(a, row, places, logit, RowSums(s));
     if (a.parts && t == 0) a.parts[blockIdx.x] = {s.reference, s.sum, s.second, 0.0f};
     if (GRADIENT) {
-        const Slope slope = slope_of(a, weight, s, places.sum);
+        const Slope slope = slope_of(a, weight, RowSums(s), places.sum);
         const Span span(x, 0, x.vectors);
         walk<THREADS, 4>(
             x, 0, x.vectors,
@@ -303,7 +346,8 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(DistillArgs a)
         __syncthreads();
         if (t < 64) {
             float q[2];
-            places.of_tokens(a.places, q);
+            bool is_first[2];
+            places.of_tokens(seen, a.places, q, is_first);
             put_tokens(a, places, q, logit, slope, to, 0, x.vectors);
         }
     }
@@ -328,7 +372,7 @@ __global__ __launch_bounds__(64) void distill_join_kernel(DistillArgs a)
     }
     TokenLogits<TYPE> logit;
     logit.load(places, Row<TYPE>(a.logits, row * a.stride, a.vocab));
-    write_loss(a, row, places, logit, s);
+    write_loss(a, row, places, logit, RowSums(s));
     if (threadIdx.x == 0) parts[0] = {s.reference, s.sum, s.second, 0.0f};
 }
 
@@ -340,6 +384,7 @@ __global__ __launch_bounds__(kThreads) void distill_gradient_kernel(DistillArgs 
     constexpr int N = Logits<TYPE>::kCount;
     __shared__ int shared_tokens;  // whether the segment holds some of the teacher's; -1: the teacher has none
     __shared__ Slope shared_slope;
+    __shared__ Places::Seen seen;
     const int t = threadIdx.x;
     const int local = quotient((int)blockIdx.x, a.by_segments), segment = (int)blockIdx.x - local * a.segments;
     const int64_t row = a.first_row + local;
@@ -362,16 +407,12 @@ __global__ __launch_bounds__(kThreads) void distill_gradient_kernel(DistillArgs 
             slope = slope_of(a, weight, row, places.sum);
         } else {
             const LogitsPart part = a.parts[(int64_t)local * a.row_parts];
-            ExpSum s;
-            s.reference = part.reference;
-            s.sum = part.sum;
-            s.second = part.second;
-            slope = slope_of(a, weight, s, places.sum);
+            slope = slope_of(a, weight, RowSums(part.reference, part.sum, part.reference, part.second), places.sum);
         }
         const bool here = places.template is_in<TYPE>(0, x.skip, first, last) || places.template is_in<TYPE>(1, x.skip, first, last);
         const bool tokens = __builtin_amdgcn_ballot_w64(here) != 0;
         if (tokens) {
-            logit.load(places, x);  // also of other segments, of which nothing is used: the gradient may have taken their place
+            logit.load(places, x, first, last);
             logit.wait();
         }
         if (t == 0) {
@@ -391,17 +432,52 @@ __global__ __launch_bounds__(kThreads) void distill_gradient_kernel(DistillArgs 
     segment_of.write([&](const Logits<TYPE> &v, int, float(&g)[N]) { slope.of_others(v, a.c, g); });
     if (!tokens) return;
     float q[2];
-    if (t < 64) places.of_tokens(a.places, q);
+    bool is_first[2];
+    if (t < 64) places.of_tokens(seen, a.places, q, is_first);
     __syncthreads();
     if (t < 64) put_tokens(a, places, q, logit, slope, to, first, last);
 }
 
-// A row to a workgroup that holds it in its registers, so that it is read once for the loss and the gradient.  The row has a vector that lies inside it.
+// A bit for each logit of a row that is held in registers: whether it is the teacher's; the vectors of a thread in neighbouring bytes, the row's ends last.
+template <int N, int THREADS, int VECTORS>
+struct HeldMarks {
+    static constexpr int kOfThread = VECTORS / 4, kEnds = THREADS * kOfThread;
+    static_assert(VECTORS % 4 == 0, "whole words");
+    struct alignas(4 * kOfThread) Word {
+        uint32_t w[kOfThread];
+        __device__ __forceinline__ uint32_t of(int u) const { return w[u / 4] >> 8 * (u % 4) & 0xffu; }
+    };
+    Word words[THREADS];
+    uint32_t ends[2];
+
+    __device__ __forceinline__ void set(const Places &p, int skip, const Span &span)  // by one wave
+    {
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int i = 0; i < THREADS; i += 64) words[i + lane] = {};
+        if (lane < 2) ends[lane] = 0;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            if (p.token[h] >= 0) {
+                const int at = p.token[h] + skip, j = at / N, i = j - span.begin, u = i / THREADS;
+                if (i >= 0 && j < span.end)
+                    atomicOr(&words[i % THREADS].w[u / 4], 1u << (8 * (u % 4) + at % N));
+                else
+                    atomicOr(&ends[i < 0 ? 0 : 1], 1u << at % N);
+            }
+    }
+};
+
+// A row to a workgroup that holds it in its registers, so that it is read once for the loss and the gradient.  The row has a vector that lies inside
+// it.  For a rest the teacher's tokens are taken out of the registers, so that the row's sum is the rest's, to which theirs is added.
 template <int TYPE, int THREADS, int VECTORS, bool REST>
-__global__ __launch_bounds__(THREADS) void distill_resident_kernel(DistillArgs a)
+__global__ __launch_bounds__(THREADS, VECTORS <= 4 ? 8 : 4) void distill_resident_kernel(DistillArgs a)
 {
+    using TheirMarks = HeldMarks<Logits<TYPE>::kCount, THREADS, VECTORS>;
+    __shared__ std::conditional_t<REST, TheirMarks, int> marks;
+    __shared__ Places::Seen seen;
+    __shared__ float of_teacher[2];
     constexpr int N = Logits<TYPE>::kCount;
-    __shared__ uint32_t bits[REST ? THREADS * VECTORS * N / 32 : 1];
     const int t = threadIdx.x;
     const int64_t row = a.first_row + blockIdx.x;
     const Row<TYPE, true> x(a.logits, row * a.stride, a.vocab);
@@ -416,8 +492,6 @@ __global__ __launch_bounds__(THREADS) void distill_resident_kernel(DistillArgs a
     const Places::Raw raw(a, row);
     Held<THREADS, VECTORS, TYPE> held;
     held.load(x, span);
-    const Marks<N> marks{bits, 0};
-    if (REST) marks.clear(x.vectors, THREADS);
     const Places places(a, raw);
     if (!places.any) {
         write_no_loss(a, row);
@@ -426,17 +500,22 @@ __global__ __launch_bounds__(THREADS) void distill_resident_kernel(DistillArgs a
     }
     TokenLogits<TYPE> logit = {};
     float q[2] = {};
-    if (t < 64) logit.load(places, x);
-    if (REST) {
-        __syncthreads();
-        if (t < 64) marks.set(places, x.skip, x.vectors);
-        __syncthreads();
+    bool first[2] = {};
+    if (t < 64) {
+        logit.load(places, x);
+        if constexpr (REST) marks.set(places, x.skip, span);
     }
-    if (t < 64) places.of_tokens(a.places, q);  // while the logits are on the way
-    Adder<REST ? 2 : 0> adder(a.c);
-    held.go_through(span, [&](Logits<TYPE> &v, int j) {
+    typename TheirMarks::Word mine = {};
+    if constexpr (REST) {
+        __syncthreads();
+        mine = marks.words[t];
+    }
+    if (t < 64) places.of_tokens(seen, a.places, q, first);  // while the logits are on the way
+    Adder<0> adder(a.c);
+    held.go_through(span, [&](Logits<TYPE> &v, int j, int u) {
         if (j >= span.end) v.fill();
-        adder.add(v, REST ? marks.of(min(j, span.end - 1)) : 0u);
+        if (REST && mine.of(u)) v.fill(mine.of(u));
+        adder.add(v);
     });
     Logits<TYPE> ends = {};
     int end = 0;
@@ -445,13 +524,40 @@ __global__ __launch_bounds__(THREADS) void distill_resident_kernel(DistillArgs a
         loads.load(x, span);
         ends = loads.vector();
         end = loads.j;
-        adder.add(ends, REST ? marks.of(end) : 0u);
+        if constexpr (REST) ends.fill(marks.ends[end == 0 ? 0 : 1]);
+        adder.add(ends);
     }
     logit.wait();  // before the barriers in join: the gradient may take the logits' place
-    const ExpSum s = join<false, THREADS>(adder.result(), a.c);
-    if (t < 64) write_loss(a, row, places, logit, s);
-    const Slope slope = slope_of(a, weight, s, places.sum);
-    held.go_through(span, [&](const Logits<TYPE> &v, int j) {
+    ExpSum s = adder.result(), teachers;
+    if (REST && t < 64) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            if (places.token[h] >= 0 && first[h]) {
+                rebase<false>(teachers, fmaxf(teachers.reference, logit[h]), a.c);
+                teachers.sum += exp2_of((logit[h] - teachers.reference) * a.c);
+            }
+        teachers = join_lanes<false, 64>(teachers, a.c);
+        if (t == 0) {
+            of_teacher[0] = teachers.reference;
+            of_teacher[1] = teachers.sum;
+        }
+    }
+    s = join<false, THREADS>(s, a.c);
+    RowSums sums(s.reference, s.sum, 0.0f, 0.0f);
+    if (REST) {
+        if (THREADS > 64) {
+            teachers.reference = of_teacher[0];
+            teachers.sum = of_teacher[1];
+        }
+        const ExpSum rest = s;
+        const float top = fmaxf(s.reference, teachers.reference);
+        rebase<false>(s, top, a.c);
+        rebase<false>(teachers, top, a.c);
+        sums = RowSums(top, s.sum + teachers.sum, rest.reference, rest.sum);
+    }
+    if (t < 64) write_loss(a, row, places, logit, sums);
+    const Slope slope = slope_of(a, weight, sums, places.sum);
+    held.go_through(span, [&](const Logits<TYPE> &v, int j, int) {
         float g[N];
         slope.of_others(v, a.c, g);
         if (j < span.end) to.store(g, j);
@@ -465,6 +571,9 @@ __global__ __launch_bounds__(THREADS) void distill_resident_kernel(DistillArgs a
     if (t < 64) put_tokens(a, places, q, logit, slope, to, 0, x.vectors);
 }
 
+// Few vectors to a thread while the row's work is mostly waiting (bf16, 32 places and a rest: 256 rows of 8000 by 512 threads with 4 vectors 7.7 us, by 256
+// with 8 10.1; of 16000 8.5 and 10.2), more where several workgroups have to share a compute unit so that one's loads go while another computes (4096 rows of
+// 20000 by 1024 threads with 4 vectors 88 us, by 512 with 8 65; of 64000 by 1024 with 8 235 and by 512 with 16 186).
 template <int TYPE, bool REST>
 void launch_resident(const DistillArgs &a, int64_t rows, hipStream_t stream)
 {
@@ -475,10 +584,10 @@ void launch_resident(const DistillArgs &a, int64_t rows, hipStream_t stream)
         distill_resident_kernel<TYPE, 256, 4, REST><<<grid, 256, 0, stream>>>(a);
     else if (vectors <= 4 * 512)
         distill_resident_kernel<TYPE, 512, 4, REST><<<grid, 512, 0, stream>>>(a);
-    else if (vectors <= 4 * 1024)
-        distill_resident_kernel<TYPE, 1024, 4, REST><<<grid, 1024, 0, stream>>>(a);
-    else if (vectors <= 8 * 1024)
-        distill_resident_kernel<TYPE, 1024, 8, REST><<<grid, 1024, 0, stream>>>(a);
+    else if (vectors <= 8 * 512)
+        distill_resident_kernel<TYPE, 512, 8, REST><<<grid, 512, 0, stream>>>(a);
+    else if (vectors <= 16 * 512)
+        distill_resident_kernel<TYPE, 512, 16, REST><<<grid, 512, 0, stream>>>(a);
     else
         distill_resident_kernel<TYPE, 1024, 16, REST><<<grid, 1024, 0, stream>>>(a);
 }
@@ -511,13 +620,13 @@ void cut_into(DistillArgs &a, const LogitsPlan &plan)
     a.by_segments = divisor((uint32_t)plan.segments);
 }
 
-// Whether a row is held in registers for its loss and its gradient.  Few long rows are cut into segments instead (1 row of 64000 bf16 logits 10.8 us
-// held and 11.6 in segments, of 128000 16.6 and 11.5; 32 rows of them 18.1 and 16.1, 64 18.5 and 19.7).
+// Whether a row is held in registers for its loss and its gradient.  Few rows that take more than 16 vectors of 512 threads are cut into segments instead (bf16, 32
+// places, no rest: 1 row of 64000 logits 10.5 us held and 11.2 in segments, of 96000 13.3 and 11.2; 32 rows of 128000 17.5 and 15.8, 64 17.8 and 19.7).
 bool is_resident(int64_t rows, int32_t vocab, int32_t type, bool workspace)
 {
     const int vectors = logit_vectors(vocab, type);
     if (vocab < (type == QUAMBA_F32 ? 8 : 16) || vectors > 16 * 1024) return false;  // it has no vector of its own, or too many
-    return !workspace || rows * 8 > compute_units() || vectors <= 10000;
+    return !workspace || rows * 8 > compute_units() || vectors <= 16 * 512;
 }
 
 template <int TYPE, bool PAST>

@@ -24,13 +24,17 @@ __device__ __forceinline__ float wave_max(float v)
     return v;
 }
 
-// The same, mostly by moves between lanes that are part of an operation.
-__device__ __forceinline__ float group_max(float v)
+// The largest of 16 lanes, and of a wave, mostly by moves between lanes that are part of an operation.
+__device__ __forceinline__ float row_max(float v)
 {
-    v = fmaxf(v, dpp_move<0xB1>(v));   // the steps of group_sum
+    v = fmaxf(v, dpp_move<0xB1>(v));  // the steps of group_sum
     v = fmaxf(v, dpp_move<0x4E>(v));
     v = fmaxf(v, dpp_move<0x141>(v));
-    v = fmaxf(v, dpp_move<0x140>(v));
+    return fmaxf(v, dpp_move<0x140>(v));
+}
+__device__ __forceinline__ float group_max(float v)
+{
+    v = row_max(v);
     v = fmaxf(v, __builtin_bit_cast(float, __builtin_amdgcn_ds_swizzle(__builtin_bit_cast(int, v), 0x401F)));
     return fmaxf(v, __shfl_xor(v, 32, 64));
 }
@@ -62,6 +66,17 @@ struct Logits {
     {
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[i] = TYPE == QUAMBA_F32 ? 0xff800000u : TYPE == QUAMBA_BF16 ? 0xff80ff80u : 0xfc00fc00u;
+    }
+    __device__ __forceinline__ void fill(uint32_t which)  // those whose bit is set
+    {
+        Logits none;
+        none.fill();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const auto all = [&](int k) { return 0u - (which >> k & 1u); };
+            const uint32_t mask = kBytes == 4 ? all(i) : (all(2 * i) & 0xffffu) | all(2 * i + 1) << 16;
+            w[i] = (none.w[i] & mask) | (w[i] & ~mask);
+        }
     }
     __device__ __forceinline__ void load(const char *p, int left)  // the first `left`, -infinity behind them
     {
@@ -311,40 +326,48 @@ struct Adder {
     }
 };
 
-// The sums of a workgroup's threads as one, in every thread.
+__device__ __forceinline__ float first_lane(float v)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, v)));
+}
+
+// The sums of a wave's lanes as one, in every lane; LANES: of each 16 lanes, which all hold the same, or of 64.  Lane 0's: a product of rebase and
+// the sum behind it may be one operation, and then the lanes' sums differ in their last bit, so that what a thread makes of them would hang
+// on which thread makes it.
+template <bool ENTROPY, int LANES>
+__device__ __forceinline__ ExpSum join_lanes(ExpSum s, float c)
+{
+    rebase<ENTROPY>(s, LANES == 64 ? group_max(s.reference) : row_max(s.reference), c);
+    s.reference = first_lane(s.reference);
+    s.sum = first_lane(group_sum<LANES>(s.sum));
+    s.second = first_lane(group_sum<LANES>(s.second));
+    return s;
+}
+
+// The sums of a workgroup's threads as one, in every thread: of the waves', a wave's in a lane of 16.
 template <bool ENTROPY, int THREADS>
 __device__ __forceinline__ ExpSum join(ExpSum s, float c)
 {
     constexpr int kWaves = THREADS / 64;
-    __shared__ float wave[3][kWaves];
-    const int w = threadIdx.x / 64;
-    rebase<ENTROPY>(s, group_max(s.reference), c);
-    s.sum = group_sum<64>(s.sum);
-    s.second = group_sum<64>(s.second);
+    static_assert(kWaves <= 16, "a wave to a lane");
+    __shared__ float wave[3][16];
+    s = join_lanes<ENTROPY, 64>(s, c);
     if (kWaves == 1) return s;
     __syncthreads();  // an earlier call's
     if (threadIdx.x % 64 == 0) {
-        wave[0][w] = s.reference;
-        wave[1][w] = s.sum;
-        wave[2][w] = s.second;
+        wave[0][threadIdx.x / 64] = s.reference;
+        wave[1][threadIdx.x / 64] = s.sum;
+        wave[2][threadIdx.x / 64] = s.second;
     }
     __syncthreads();
-    float top = wave[0][0];
-#pragma unroll
-    for (int i = 1; i < kWaves; ++i) top = fmaxf(top, wave[0][i]);
-    ExpSum all;
-    all.reference = top;
-#pragma unroll
-    for (int i = 0; i < kWaves; ++i) {
-        ExpSum part;
-        part.reference = wave[0][i];
-        part.sum = wave[1][i];
-        part.second = wave[2][i];
-        rebase<ENTROPY>(part, top, c);
-        all.sum += part.sum;
-        all.second += part.second;
+    const int lane = threadIdx.x & 15;
+    ExpSum of_wave;
+    if (lane < kWaves) {
+        of_wave.reference = wave[0][lane];
+        of_wave.sum = wave[1][lane];
+        of_wave.second = wave[2][lane];
     }
-    return all;
+    return join_lanes<ENTROPY, 16>(of_wave, c);
 }
 
 // ... of the segments of a row, which are in memory.
@@ -696,13 +719,13 @@ struct Held {
 #pragma unroll
         for (int u = 0; u < VECTORS; ++u) x.load(v[u], min(span.begin + u * THREADS + (int)threadIdx.x, span.end - 1));
     }
-    // each(v, j) in turn; j may be span.end and above in some lanes
+    // each(v, j, u) in turn; j may be span.end and above in some lanes
     template <typename Each>
     __device__ __forceinline__ void go_through(const Span &span, const Each &each)
     {
 #pragma unroll
         for (int u = 0; u < VECTORS; ++u)
-            if (span.begin + u * THREADS < span.end) each(v[u], span.begin + u * THREADS + (int)threadIdx.x);
+            if (span.begin + u * THREADS < span.end) each(v[u], span.begin + u * THREADS + (int)threadIdx.x, u);
     }
 };
 
@@ -727,7 +750,7 @@ struct GradientSegment {
     template <typename Make>
     __device__ __forceinline__ void write(const Make &make)
     {
-        held.go_through(span, [&](const Logits<TYPE> &v, int j) {
+        held.go_through(span, [&](const Logits<TYPE> &v, int j, int) {
             float g[Logits<TYPE>::kCount];
             make(v, j, g);
             if (j < span.end) to.store(g, j);

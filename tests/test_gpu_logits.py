@@ -258,7 +258,7 @@ def test_what_is_not_asked_for(gpu_lib):
 
 def test_the_same_call_gives_the_same_bits(gpu_lib):
     import torch
-    for rows, vocab in ((1, 128000), (40, 50021), (600, 20011)):
+    for rows, vocab in ((1, 128000), (40, 50021), (600, 20011), (9000, 1031), (700, 40009)):
         x = _logits(rows, vocab, "bf16", 13)
         a, b = (_run(gpu_lib, x, np.zeros(rows, int), 64) for _ in range(2))
         assert all(torch.equal(a[k], b[k]) for k in a)
