@@ -460,7 +460,7 @@ struct LogitsPlan {
     int threads, segments, vectors;
 };
 enum class LogitsWork : int { sums, alternatives, distance };
-LogitsPlan logits_plan(int64_t rows, int32_t vocab, int32_t type, LogitsWork work, bool workspace);  // of a pass that sums
+LogitsPlan logits_plan(int64_t rows, int32_t vocab, int32_t type, LogitsWork work, bool entropy, bool workspace);  // of a pass that sums
 LogitsPlan gradient_plan(int32_t vocab, int32_t type, int vectors);                                 // into segments of at most so many
 int logit_vectors(int32_t vocab, int32_t type);
 int wave_vectors(int64_t rows, int most);  // of rows that a wave takes

@@ -193,15 +193,18 @@ int wave_vectors(int64_t rows, int most) { return (int)std::min<int64_t>(most, s
 
 // A workgroup of 256 threads takes a row, but where rows are few and long.  1024 threads then take one on a compute unit of its own (256 rows of
 // 200000 fp32 logits 44 -> 35 us, 128 of 128000 bf16 ones with 8 alternatives 17.8 -> 14.2; up to the borders below both take about as long).
-// Where a row still takes longer than a second launch that joins segments, it is cut into these (1 row of 128000 bf16 logits 15 us by 256
-// threads, 11 by 1024, 7.5 in segments; with alternatives 13.8, 12.7 and 10.4; 128 rows with alternatives 17.8, 14.2 and 16.0; 64 rows of 128000
-// fp32 ones with 20 of them and the entropy 21.6 and 17.5).
-LogitsPlan logits_plan(int64_t rows, int32_t vocab, int32_t type, LogitsWork work, bool workspace)
+// Where a row still takes longer than a second launch that joins segments, it is cut into these, by its logits and not its bytes (by 1024 threads and in
+// segments: 1 row of 70000 bf16 logits 5.8 and 7.3 us, of 70564 fp32 ones 5.9 and 7.3; 13 rows of 100000 both 7.4, with 5 alternatives 11.6 and 10.8; of
+// 166139 10.0 and 7.4, 15.2 and 11.8; 64 rows of 128000 with 20 alternatives 14.4 and 15.2).  Entropies and distances take half as much time again for a
+// logit and are cut earlier (64 rows of 128000 fp32 logits with 20 alternatives and the entropy 21.3 and 17.4; the distance of 1 row of 70000 bf16 ones, 32 places
+// and a rest, 8.1 and 6.4).
+LogitsPlan logits_plan(int64_t rows, int32_t vocab, int32_t type, LogitsWork work, bool entropy, bool workspace)
 {
     const int units = compute_units(), vectors = logit_vectors(vocab, type);
     const bool best = work == LogitsWork::alternatives;
     if (vectors <= wave_vectors(rows, 512)) return {64, 1, 0};
-    if (workspace && (best ? rows * 4 <= units && vocab > 100000 : rows * 8 <= units && vocab > 60000)) {
+    const bool more = entropy || work == LogitsWork::distance;
+    if (workspace && rows * (best && more ? 4 : 8) <= units && vocab > (more && !best ? 60000 : 100000)) {
         const int segments = (int)std::min<int64_t>({(4 * units + rows - 1) / rows, (vectors + 511) / 512, 256}), each = (vectors + segments - 1) / segments;
         return {256, (vectors + each - 1) / each, each};
     }
@@ -252,7 +255,7 @@ LogitsWork work_of(int count) { return count ? LogitsWork::alternatives : Logits
 template <int TYPE>
 hipError_t launch(LogprobArgs a, void *workspace, hipStream_t stream)
 {
-    const LogitsPlan plan = logits_plan(a.rows, a.vocab, TYPE, work_of(a.count), workspace != nullptr);
+    const LogitsPlan plan = logits_plan(a.rows, a.vocab, TYPE, work_of(a.count), a.entropies != nullptr, workspace != nullptr);
     a.segments = plan.segments;
     a.segment_vectors = plan.vectors;
     a.by_segments = divisor((uint32_t)plan.segments);
@@ -294,11 +297,12 @@ hipError_t launch_gradient(const LogprobGradientArgs &a, hipStream_t stream)
 
 size_t token_logprobs_workspace_bytes(int64_t rows, int32_t vocab, int32_t count)
 {
-    size_t most = 0;  // over the types
-    for (const int type : {QUAMBA_F32, QUAMBA_BF16}) {
-        const int segments = logits_plan(rows, vocab, type, work_of(count), true).segments;
-        if (segments > 1) most = std::max(most, (size_t)rows * segments * (sizeof(LogitsPart) + sizeof(uint64_t) * count));
-    }
+    size_t most = 0;  // over the types, with entropies and without
+    for (const int type : {QUAMBA_F32, QUAMBA_BF16})
+        for (const bool entropy : {false, true}) {
+            const int segments = logits_plan(rows, vocab, type, work_of(count), entropy, true).segments;
+            if (segments > 1) most = std::max(most, (size_t)rows * segments * (sizeof(LogitsPart) + sizeof(uint64_t) * count));
+        }
     return most;
 }
 
