@@ -571,25 +571,16 @@ __global__ __launch_bounds__(THREADS, VECTORS <= 4 ? 8 : 4) void distill_residen
     if (t < 64) put_tokens(a, places, q, logit, slope, to, 0, x.vectors);
 }
 
-// Few vectors to a thread while the row's work is mostly waiting (bf16, 32 places and a rest: 256 rows of 8000 by 512 threads with 4 vectors 7.7 us, by 256
-// with 8 10.1; of 16000 8.5 and 10.2), more where several workgroups have to share a compute unit so that one's loads go while another computes (4096 rows of
-// 20000 by 1024 threads with 4 vectors 88 us, by 512 with 8 65; of 64000 by 1024 with 8 235 and by 512 with 16 186).
 template <int TYPE, bool REST>
-void launch_resident(const DistillArgs &a, int64_t rows, hipStream_t stream)
+void launch_resident(const DistillArgs &a, const LogitsPlan &form, int64_t rows, hipStream_t stream)
 {
-    const int grid = (int)rows, vectors = logit_vectors(a.vocab, TYPE);
-    if (vectors <= wave_vectors(a.rows, 256))
-        distill_resident_kernel<TYPE, 64, 4, REST><<<grid, 64, 0, stream>>>(a);
-    else if (vectors <= 4 * 256)
-        distill_resident_kernel<TYPE, 256, 4, REST><<<grid, 256, 0, stream>>>(a);
-    else if (vectors <= 4 * 512)
-        distill_resident_kernel<TYPE, 512, 4, REST><<<grid, 512, 0, stream>>>(a);
-    else if (vectors <= 8 * 512)
-        distill_resident_kernel<TYPE, 512, 8, REST><<<grid, 512, 0, stream>>>(a);
-    else if (vectors <= 16 * 512)
-        distill_resident_kernel<TYPE, 512, 16, REST><<<grid, 512, 0, stream>>>(a);
-    else
-        distill_resident_kernel<TYPE, 1024, 16, REST><<<grid, 1024, 0, stream>>>(a);
+    const auto kernel = form.threads == 64      ? distill_resident_kernel<TYPE, 64, 4, REST>
+                        : form.threads == 256   ? distill_resident_kernel<TYPE, 256, 4, REST>
+                        : form.threads == 1024  ? distill_resident_kernel<TYPE, 1024, 16, REST>
+                        : form.vectors == 4     ? distill_resident_kernel<TYPE, 512, 4, REST>
+                        : form.vectors == 8     ? distill_resident_kernel<TYPE, 512, 8, REST>
+                                                : distill_resident_kernel<TYPE, 512, 16, REST>;
+    kernel<<<(int)rows, form.threads, 0, stream>>>(a);
 }
 
 template <int TYPE, int THREADS, bool PAST, bool GRADIENT>
@@ -620,19 +611,33 @@ void cut_into(DistillArgs &a, const LogitsPlan &plan)
     a.by_segments = divisor((uint32_t)plan.segments);
 }
 
-// Whether a row is held in registers for its loss and its gradient.  Few rows that take more than 16 vectors of 512 threads are cut into segments instead (bf16, 32
-// places, no rest: 1 row of 64000 logits 10.5 us held and 11.2 in segments, of 96000 13.3 and 11.2; 32 rows of 128000 17.5 and 15.8, 64 17.8 and 19.7).
-bool is_resident(int64_t rows, int32_t vocab, int32_t type, bool workspace)
+}  // namespace
+
+// Few vectors to a thread while the row's work is mostly waiting (bf16, 32 places and a rest: 256 rows of 8000 by 512 threads with 4 vectors 7.7 us, by 256
+// with 8 10.1; of 16000 8.5 and 10.2), more where several workgroups have to share a compute unit so that one's loads go while another computes (4096 rows of
+// 20000 by 1024 threads with 4 vectors 88 us, by 512 with 8 65; of 64000 by 1024 with 8 235 and by 512 with 16 186).  Few rows that take more than 16 vectors of
+// 512 threads are cut into segments instead (no rest: 1 row of 64000 logits 10.5 us held and 11.2 in segments, of 96000 13.3 and 11.2; 32 rows of
+// 128000 17.5 and 15.8, 64 17.8 and 19.7).
+LogitsPlan distill_form(int64_t rows, int32_t vocab, int32_t type, bool workspace)
 {
     const int vectors = logit_vectors(vocab, type);
-    if (vocab < (type == QUAMBA_F32 ? 8 : 16) || vectors > 16 * 1024) return false;  // it has no vector of its own, or too many
-    return !workspace || rows * 8 > compute_units() || vectors <= 16 * 512;
+    if (vocab < (type == QUAMBA_F32 ? 8 : 16)) return {};  // it may have no vector of its own
+    if (vectors <= wave_vectors(rows, 4 * 64)) return {64, 1, 4};
+    if (vectors <= 4 * 256) return {256, 1, 4};
+    for (const int each : {4, 8, 16})
+        if (vectors <= each * 512) return {512, 1, each};
+    if (vectors <= 16 * 1024 && (!workspace || rows * 8 > compute_units())) return {1024, 1, 16};
+    return {};
 }
+
+namespace {
 
 template <int TYPE, bool PAST>
 hipError_t launch(DistillArgs a, void *workspace, hipStream_t stream)
 {
-    const bool sums = !a.saved_sums, resident = sums && a.gradient && is_resident(a.rows, a.vocab, TYPE, workspace != nullptr);
+    const bool sums = !a.saved_sums;
+    const LogitsPlan form = sums && a.gradient ? distill_form(a.rows, a.vocab, TYPE, workspace != nullptr) : LogitsPlan{};
+    const bool resident = form.threads != 0;
     const LogitsPlan plan = logits_plan(a.rows, a.vocab, TYPE, LogitsWork::distance, false, workspace != nullptr);
     const LogitsPlan gradient = gradient_plan(a.vocab, TYPE, kThreads * kGradientVectors);
     a.parts = static_cast<LogitsPart *>(workspace);
@@ -641,7 +646,7 @@ hipError_t launch(DistillArgs a, void *workspace, hipStream_t stream)
     for (a.first_row = 0; a.first_row < a.rows; a.first_row += most) {
         const int64_t rows = std::min(a.rows - a.first_row, most);
         if (resident) {
-            a.rest ? launch_resident<TYPE, true>(a, rows, stream) : launch_resident<TYPE, false>(a, rows, stream);
+            a.rest ? launch_resident<TYPE, true>(a, form, rows, stream) : launch_resident<TYPE, false>(a, form, rows, stream);
         } else {
             cut_into(a, plan);
             if (sums) launch_sums<TYPE, PAST>(a, plan.threads, rows, stream);

@@ -83,11 +83,13 @@ def _run(q, logits, targets, count, T=1.0, workspace=True, everything=True):
     return o
 
 
-def _check(q, logits, targets, count=0, T=1.0):
-    x = _host(logits)
+def _check(q, logits, targets, count=0, T=1.0, rows=slice(None)):
+    """Of all rows, or of some of a call with more."""
+    x, of_all = _host(logits[rows]), targets
+    targets = None if targets is None else np.asarray(targets)[rows]
     want = oracle.ref_token_logprobs(x, targets, count, T)
     for workspace in (True, False):
-        got = {k: v.cpu().numpy() for k, v in _run(q, logits, targets, count, T, workspace).items()}
+        got = {k: v[rows].cpu().numpy() for k, v in _run(q, logits, of_all, count, T, workspace).items()}
         assert np.array_equal(got["top_tokens"], want["top_tokens"])
         for r in range(x.shape[0]):
             if targets is not None and not 0 <= targets[r] < x.shape[1] or np.isnan(want["log_sums"][r]):
@@ -276,15 +278,18 @@ def _gradient_close(got, want, kind, arithmetic):
     assert (off[fin] <= bound[fin]).all(), (off[fin] - bound[fin]).max()
 
 
-def _check_backward(q, logits, targets, forward, g, h, T, out=None):
+def _check_backward(q, logits, targets, forward, g, h, T, out=None, some=slice(None)):
     import torch
-    x, kind = _host(logits), {v: k for k, v in ((k, _torch_type(k)) for k in TYPES)}[logits.dtype]
+    x, kind = _host(logits[some]), {v: k for k, v in ((k, _torch_type(k)) for k in TYPES)}[logits.dtype]
     sums, entropies = _as(np.float32, forward["log_sums"]), _as(np.float32, forward["entropies"])
+    of_all = dict(targets=_dev(targets, np.int32), sums=_dev(sums), g=_dev(g), entropies=None if h is None else _dev(entropies), h=_dev(h))
+    sums, entropies = sums[some], entropies[some]
+    targets, g, h = (None if v is None else np.asarray(v)[some] for v in (targets, g, h))
     want = oracle.ref_token_logprobs_backward(x, targets, sums, entropies, None if g is None else _as(np.float32, g), None if h is None else _as(np.float32, h), T)
     dx = torch.full_like(logits, 3.0) if out is None else out
-    q.quamba_token_logprobs_backward(logits, _dev(targets, np.int32), _dev(sums), _dev(g), dx, entropies=None if h is None else _dev(entropies),
-                                     grad_entropies=_dev(h), temperature=T)
-    got = _host(dx)
+    q.quamba_token_logprobs_backward(logits, of_all["targets"], of_all["sums"], of_all["g"], dx, entropies=of_all["entropies"],
+                                     grad_entropies=of_all["h"], temperature=T)
+    got = _host(dx[some])
     with np.errstate(invalid="ignore", over="ignore"):
         log_p = x / T - sums[:, None]
         p = np.exp(log_p)
@@ -394,17 +399,21 @@ def _teacher(rows, vocab, K, rest, seed, T=1.0, empty=True):
     return _as(np.float32, t), tokens
 
 
-def _check_distill(q, logits, teacher, tokens, rest, weights=None, T=1.0, out=None, losses_only=False):
+def _check_distill(q, logits, teacher, tokens, rest, weights=None, T=1.0, out=None, losses_only=False, some=slice(None)):
+    """Of all rows, or of some of a call with more."""
     import torch
     kind = {v: k for k, v in ((k, _torch_type(k)) for k in TYPES)}[logits.dtype]
-    x = _host(logits)
+    x = _host(logits[some])
     rows, vocab = x.shape
     K = teacher.shape[1]
     teacher, tokens = _as(np.float32, teacher), _as(np.int32, tokens)
     w = None if weights is None else _as(np.float32, weights)
+    of_all = dict(teacher=_dev(teacher), tokens=_dev(tokens, np.int32), w=_dev(w))
+    all_rows = len(teacher)
+    teacher, tokens, w = teacher[some], tokens[some], None if w is None else w[some]
     want = oracle.ref_distill(x, teacher, tokens, rest, w, T)
     keep = logits.clone()
-    size = q.quamba_distill_loss_workspace_size(rows, vocab, K)
+    size = q.quamba_distill_loss_workspace_size(all_rows, vocab, K)
     dead = np.array([(want["q"][r] == 0).all() and not np.isnan(want["losses"][r]) for r in range(rows)])
     with np.errstate(invalid="ignore", over="ignore", divide="ignore"):
         err = np.array([U * _sum_error(x[r] / T, vocab) if np.isfinite(want["log_sums"][r]) and not dead[r] else 0.0 for r in range(rows)])
@@ -439,35 +448,35 @@ def _check_distill(q, logits, teacher, tokens, rest, weights=None, T=1.0, out=No
     for workspace in (True, False):
         for gradient in ((False,) if losses_only else (False, True)):
             logits.copy_(keep)
-            o = {k: torch.full((rows,), 7.0, device="cuda") for k in ("losses", "log_sums", "log_rests")}
+            o = {k: torch.full((all_rows,), 7.0, device="cuda") for k in ("losses", "log_sums", "log_rests")}
             dx = None if not gradient else torch.full_like(logits, 3.0) if out is None else out
             space = torch.full((size,), 0xFF, dtype=torch.uint8, device="cuda") if workspace and size else None
-            q.quamba_distill_loss(logits, _dev(teacher), _dev(tokens, np.int32), o["losses"], log_sums=o["log_sums"], log_rests=o["log_rests"],
-                                  weights=_dev(w), grad_logits=dx, rest=rest, temperature=T, workspace=space)
-            got = _host(o["losses"])
+            q.quamba_distill_loss(logits, of_all["teacher"], of_all["tokens"], o["losses"], log_sums=o["log_sums"], log_rests=o["log_rests"],
+                                  weights=of_all["w"], grad_logits=dx, rest=rest, temperature=T, workspace=space)
+            got = _host(o["losses"][some])
             fin = np.isfinite(want["losses"])
             assert np.array_equal(got[~fin], want["losses"][~fin], equal_nan=True)
-            assert (np.abs(got - want["losses"])[fin] <= tol[fin]).all(), (np.abs(got - want["losses"])[fin] / tol[fin]).max()
+            assert (np.abs(got[fin] - want["losses"][fin]) <= tol[fin]).all(), (np.abs(got[fin] - want["losses"][fin]) / tol[fin]).max()
             ok = fin & ~dead
-            sums, rests = _host(o["log_sums"]), _host(o["log_rests"])
-            assert (np.abs(sums - want["log_sums"])[ok] <= (err + U * (8 * np.abs(top) + 8 + 4 * np.log(vocab)))[ok]).all()
+            sums, rests = _host(o["log_sums"][some]), _host(o["log_rests"][some])
+            assert (np.abs(sums[ok] - want["log_sums"][ok]) <= (err + U * (8 * np.abs(top) + 8 + 4 * np.log(vocab)))[ok]).all()
             if rest:
                 few = ok & np.isfinite(want["log_rests"])
-                assert (np.abs(rests - want["log_rests"])[few] <= (2 * err + U * (8 * np.abs(top) + 8 * np.abs(want["log_rests"]) + 64))[few]).all()
+                assert (np.abs(rests[few] - want["log_rests"][few]) <= (2 * err + U * (8 * np.abs(top) + 8 * np.abs(want["log_rests"]) + 64))[few]).all()
             assert (sums[dead] == 0).all() and (rests[dead] == 0).all()
             if gradient:
-                _gradient_close(_host(dx), want["gradient"], kind, np.nan_to_num(arithmetic))
+                _gradient_close(_host(dx[some]), want["gradient"], kind, np.nan_to_num(arithmetic))
     if losses_only:
         return want
     # the gradient alone, from what the call left; the log sums' rounding goes into p
     logits.copy_(keep)
     dx = torch.full_like(logits, 3.0) if out is None else out
-    q.quamba_distill_backward(logits, _dev(teacher), _dev(tokens, np.int32), o["log_sums"], _dev(np.ones(rows) if w is None else w), dx,
+    q.quamba_distill_backward(logits, of_all["teacher"], of_all["tokens"], o["log_sums"], _dev(np.ones(all_rows)) if w is None else of_all["w"], dx,
                               log_rests=o["log_rests"] if rest else None, rest=rest, temperature=T)
     with np.errstate(invalid="ignore"):
         size_of_sums = np.abs(sums) + np.where(np.isfinite(rests), np.abs(rests), 0)
         saved = (p * (1 + left)[:, None] + share) * (U * 4 * (size_of_sums + 8) + np.abs(top) * U * 8)[:, None] * (wp / T)[:, None]
-    _gradient_close(_host(dx), want["gradient"], kind, np.nan_to_num(arithmetic + saved))
+    _gradient_close(_host(dx[some]), want["gradient"], kind, np.nan_to_num(arithmetic + saved))
     logits.copy_(keep)
     return want
 
@@ -546,6 +555,47 @@ def test_distill_of_a_vocabulary_that_is_marked_in_parts(gpu_lib):
     tokens[1, :4] = [(1 << 17) - 1, 1 << 17, (1 << 18) - 5, (1 << 20) - 1]
     x = _logits(2, (1 << 20) + 3, "bf16", 14)
     _check_distill(gpu_lib, x[:, 3:], teacher, tokens, True)
+
+
+# Of 16-bit logits, half as many of fp32: a size of each form that holds a row in registers (test_logits_plans.py checks which), and one that does not.
+HELD = [(3, 901), (2200, 2003), (3, 7001), (3, 15001), (3, 30001), (3, 60001), (40, 130001), (35, 133001)]
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("rows,vocab", HELD)
+def test_loss_and_gradient_of_rows_in_registers(gpu_lib, rows, vocab, rest, kind):
+    """At odd addresses; the teacher's tokens at both ends of a row, behind one another, in several places, and with the same low bits."""
+    import torch
+    vocab = vocab // 2 if kind == "fp32" else vocab
+    some = np.unique(np.linspace(0, rows - 1, 12).astype(int))
+    teacher, tokens = _teacher(rows, vocab, 100, rest, vocab + rows)
+    tokens[:, :6] = [0, vocab - 1, 1, 2, 3, vocab // 2]
+    tokens[1::3, 7] = vocab - 1
+    if vocab > 1 << 15:
+        tokens[:, 8] = 1 + (1 << 15)
+    wide = torch.zeros(rows, vocab + 5, dtype=_torch_type(kind), device="cuda")
+    x = wide[:, 3:vocab + 3]
+    x.copy_(_logits(rows, vocab, kind, vocab))
+    _check_distill(gpu_lib, x, teacher, tokens, rest, np.linspace(-0.5, 2, rows), some=some)
+
+
+@pytest.mark.parametrize("kind,rows,vocab", [("bf16", 700, 52001), ("fp16", 300, 131501), ("fp32", 300, 70001)])
+def test_logits_that_no_cache_holds(gpu_lib, kind, rows, vocab):
+    """More than 64 MiB of them, in all operators, padded rows between the others."""
+    some = np.array([0, 1, 2, rows // 2, rows - 1])
+    x = _logits(rows, vocab, kind, 21)
+    targets = np.arange(rows) * 71 % vocab
+    targets[1::4] = -1
+    for count in (0, 9):
+        want = _check(gpu_lib, x, targets, count, 0.8, some)
+    forward = {k: np.zeros(rows) for k in ("log_sums", "entropies")}
+    for k in forward:
+        forward[k][some] = want[k]
+    _check_backward(gpu_lib, x, targets, forward, np.linspace(-1, 1, rows), np.linspace(1, 2, rows), 0.8, some=some)
+    for rest in (False, True):
+        teacher, tokens = _teacher(rows, vocab, 9, rest, 22, 0.8)
+        _check_distill(gpu_lib, x, teacher, tokens, rest, None, 0.8, some=some)
 
 
 def test_distill_against_differences(gpu_lib):
