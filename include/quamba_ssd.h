@@ -495,7 +495,7 @@ int quamba_beam_reorder(int32_t batch, int32_t beams, const int32_t *parents, in
 
 /* ---- what a model answers: log probabilities of tokens, distance from a teacher ----
  * Rows of logits x [rows, vocab] of `type` (quamba_dtype), logits_stride >= vocab values apart, at any address that is a multiple of the type's
- * size.  z = x / temperature, p = softmax(z), everything in fp32.  A logit of -infinity is a token that cannot come (p = 0).  A row has no
+ * size.  z = x / temperature, p = softmax(z), everything in fp32: values beyond its range are infinite.  A logit of -infinity is a token that cannot come (p = 0).  A row has no
  * distribution where a logit is NaN or +infinity or none is above -infinity: its outputs are NaN.  No rows: nothing is launched. */
 
 /*
@@ -512,8 +512,8 @@ int quamba_beam_reorder(int32_t batch, int32_t beams, const int32_t *parents, in
  * quamba_token_logprobs_workspace_size is the scratch memory with which a call of this size takes its fastest launch on the current device (may
  * be 0; 0 for invalid sizes).  With a workspace that is NULL, smaller or not aligned a row is one workgroup's: the same tokens, values to
  * rounding, slower for few rows.  Calls that share a workspace must not overlap.
- * Errors: ENULL, ESHAPE (negative rows, more than 2^31, vocab not positive or above 2^26, count, stride below vocab or above 2^40), EINVAL (type,
- * temperature outside 2^-100 .. 2^100, logits at an address between the type's), EHIP.
+ * Errors: ENULL, ESHAPE (negative rows, more than 2^31, vocab not positive or above 2^26, count, stride below vocab or above 2^40, rows x stride above
+ * 2^46), EINVAL (type, temperature outside 2^-100 .. 2^100, logits at an address between the type's), EHIP.
  */
 size_t quamba_token_logprobs_workspace_size(int64_t rows, int64_t vocab, int32_t count);
 int quamba_token_logprobs(int64_t rows, int64_t vocab, const void *logits, int32_t type, int64_t logits_stride,
@@ -547,7 +547,7 @@ int quamba_token_logprobs_backward(int64_t rows, int64_t vocab, const void *logi
  *   rest = 1:  teacher holds log probabilities at this temperature, as quamba_token_logprobs gives them: q = exp(teacher), and what they
  *              leave, q_R = max(0, 1 - sum_k q_k), is one more outcome,
  *                loss += q_R (ln q_R - ln p_R),  p_R = sum of p over the tokens without a place
- *              (left out, with q_R = 0, where p_R = 0).
+ *              (left out, with q_R = 0, where p_R = 0; a p_R below 2^-120 may count as 0).
  *   weights    device fp32 [rows] or NULL (1).  A row whose weight is 0, or whose places are all empty, is not read: its loss and its
  *              gradient are 0.
  *   losses     device fp32 [rows], without the weights
@@ -555,7 +555,7 @@ int quamba_token_logprobs_backward(int64_t rows, int64_t vocab, const void *logi
  *   grad_logits  NULL, or device `type` [rows, vocab], rows grad_stride >= vocab values apart: d / dx of sum over the rows of weights losses,
  *                grad_logits[v] = weight / temperature (p_v (sum q + q_R) - sum of the q_k with token_k = v - [no place] q_R p_v / p_R);
  *              it may take the logits' place (the same address and stride) and must not overlap them otherwise
- *   workspace  as for quamba_token_logprobs
+ *   workspace  as for quamba_token_logprobs (never 0 bytes for rows > 0)
  * A place of 1 is the cross-entropy of its token.  A teacher's NaN makes its row NaN.
  * Errors: as above, ESHAPE also for places outside 1 .. 128, EINVAL also for rest other than 0 and 1 and a gradient that overlaps the logits.
  */

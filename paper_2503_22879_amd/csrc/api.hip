@@ -454,7 +454,8 @@ bool logits_size(int64_t rows, int64_t vocab, int32_t count, int32_t most)
 {
     return rows >= 0 && rows <= quamba::kMaxLogitRows && vocab > 0 && vocab <= quamba::kMaxVocab && count >= 0 && count <= most;
 }
-bool rows_apart(int64_t vocab, int64_t stride) { return stride >= vocab && stride <= (int64_t)1 << 40; }
+// No row's place passes 2^46 values.
+bool rows_apart(int64_t rows, int64_t vocab, int64_t stride) { return stride >= vocab && stride <= (int64_t)1 << 40 && rows <= ((int64_t)1 << 46) / stride; }
 int type_bytes(int32_t type) { return type == QUAMBA_F32 ? 4 : 2; }
 bool at_its_type(const void *p, int32_t type) { return reinterpret_cast<uintptr_t>(p) % type_bytes(type) == 0; }
 bool is_temperature(float t) { return t >= 0x1p-100f && t <= 0x1p100f; }
@@ -483,7 +484,7 @@ extern "C" int quamba_token_logprobs(int64_t rows, int64_t vocab, const void *lo
                                      float *entropies, int32_t count, float *top_logprobs, int32_t *top_tokens,
                                      void *workspace, size_t workspace_bytes, void *hip_stream)
 {
-    if (!logits_size(rows, vocab, count, quamba::kMaxChoices) || !rows_apart(vocab, logits_stride)) return QUAMBA_ESHAPE;
+    if (!logits_size(rows, vocab, count, quamba::kMaxChoices) || !rows_apart(rows, vocab, logits_stride)) return QUAMBA_ESHAPE;
     if (!known_type(type) || !is_temperature(temperature) || !at_its_type(logits, type)) return QUAMBA_EINVAL;
     if (rows == 0) return QUAMBA_OK;
     if (!logits || !targets != !logprobs || (count > 0 && (!top_logprobs || !top_tokens))) return QUAMBA_ENULL;
@@ -504,7 +505,7 @@ extern "C" int quamba_token_logprobs_backward(int64_t rows, int64_t vocab, const
                                               const float *grad_entropies, void *grad_logits, int64_t grad_stride,
                                               void *hip_stream)
 {
-    if (!logits_size(rows, vocab, 0, 0) || !rows_apart(vocab, logits_stride) || !rows_apart(vocab, grad_stride)) return QUAMBA_ESHAPE;
+    if (!logits_size(rows, vocab, 0, 0) || !rows_apart(rows, vocab, logits_stride) || !rows_apart(rows, vocab, grad_stride)) return QUAMBA_ESHAPE;
     if (!known_type(type) || !is_temperature(temperature) || !at_its_type(logits, type) || !at_its_type(grad_logits, type)) return QUAMBA_EINVAL;
     if (rows == 0) return QUAMBA_OK;
     if (!logits || !grad_logits || !log_sums || !targets != !grad_logprobs || !entropies != !grad_entropies) return QUAMBA_ENULL;
@@ -525,8 +526,8 @@ int distill_args(quamba::DistillArgs &a, int64_t rows, int64_t vocab, const void
                  float temperature, int32_t places, const float *teacher, const int32_t *teacher_tokens, int32_t rest,
                  const float *weights, void *gradient, int64_t grad_stride)
 {
-    if (!logits_size(rows, vocab, places, quamba::kMaxPlaces) || places == 0 || !rows_apart(vocab, logits_stride) ||
-        (gradient && !rows_apart(vocab, grad_stride)))
+    if (!logits_size(rows, vocab, places, quamba::kMaxPlaces) || places == 0 || !rows_apart(rows, vocab, logits_stride) ||
+        (gradient && !rows_apart(rows, vocab, grad_stride)))
         return QUAMBA_ESHAPE;
     if (!known_type(type) || !is_temperature(temperature) || !at_its_type(logits, type) || !at_its_type(gradient, type) || rest < 0 || rest > 1)
         return QUAMBA_EINVAL;

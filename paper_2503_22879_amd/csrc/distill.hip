@@ -441,7 +441,7 @@ __global__ __launch_bounds__(kThreads) void distill_gradient_kernel(DistillArgs 
 // A bit for each logit of a row that is held in registers: whether it is the teacher's; the vectors of a thread in neighbouring bytes, the row's ends last.
 template <int N, int THREADS, int VECTORS>
 struct HeldMarks {
-    static constexpr int kOfThread = VECTORS / 4, kEnds = THREADS * kOfThread;
+    static constexpr int kOfThread = VECTORS / 4;
     static_assert(VECTORS % 4 == 0, "whole words");
     struct alignas(4 * kOfThread) Word {
         uint32_t w[kOfThread];

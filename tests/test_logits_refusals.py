@@ -19,7 +19,7 @@ def _call(f, good, **change):
 
 
 BAD_ROWS = (dict(rows=-1), dict(rows=2 ** 31 + 1), dict(vocab=0), dict(vocab=-4), dict(vocab=2 ** 26 + 1, stride=2 ** 27), dict(stride=9),
-            dict(stride=2 ** 40 + 1))
+            dict(stride=2 ** 40 + 1), dict(rows=2 ** 20, stride=2 ** 27), dict(rows=2 ** 31, stride=2 ** 40))
 BAD_VALUES = (dict(type=3), dict(type=-1), dict(temperature=0.0), dict(temperature=-1.0), dict(temperature=float("nan")),
               dict(temperature=float("inf")), dict(temperature=2.0 ** -101), dict(temperature=2.0 ** 101))
 
