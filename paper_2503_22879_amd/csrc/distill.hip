@@ -450,7 +450,8 @@ struct HeldMarks {
     Word words[THREADS];
     uint32_t ends[2];
 
-    __device__ __forceinline__ void set(const Places &p, int skip, const Span &span)  // by one wave
+    // By one wave.  Vectors held_end .. span.end - 1 are not held.
+    __device__ __forceinline__ void set(const Places &p, int skip, const Span &span, int held_end)
     {
         const int lane = threadIdx.x & 63;
 #pragma unroll
@@ -460,21 +461,24 @@ struct HeldMarks {
         for (int h = 0; h < 2; ++h)
             if (p.token[h] >= 0) {
                 const int at = p.token[h] + skip, j = at / N, i = j - span.begin, u = i / THREADS;
-                if (i >= 0 && j < span.end)
+                if (i >= 0 && j < held_end)
                     atomicOr(&words[i % THREADS].w[u / 4], 1u << (8 * (u % 4) + at % N));
-                else
+                else if (i < 0 || j >= span.end)
                     atomicOr(&ends[i < 0 ? 0 : 1], 1u << at % N);
             }
     }
 };
 
 // A row to a workgroup that holds it in its registers, so that it is read once for the loss and the gradient.  The row has a vector that lies inside
-// it.  For a rest the teacher's tokens are taken out of the registers, so that the row's sum is the rest's, to which theirs is added.
-template <int TYPE, int THREADS, int VECTORS, bool REST>
+// it.  For a rest the teacher's tokens are taken out of the registers, so that the row's sum is the rest's, to which theirs is added.  MORE: a row of up to
+// twice what the registers hold, of which the rest is read again (before the registers are filled and after they are written, when they are free).
+template <int TYPE, int THREADS, int VECTORS, bool REST, bool MORE>
 __global__ __launch_bounds__(THREADS, VECTORS <= 4 ? 8 : 4) void distill_resident_kernel(DistillArgs a)
 {
     using TheirMarks = HeldMarks<Logits<TYPE>::kCount, THREADS, VECTORS>;
+    constexpr int kHeld = THREADS * VECTORS;
     __shared__ std::conditional_t<REST, TheirMarks, int> marks;
+    __shared__ uint32_t bits[REST && MORE ? kHeld * Logits<TYPE>::kCount / 32 : 1];
     __shared__ Places::Seen seen;
     __shared__ float of_teacher[2];
     constexpr int N = Logits<TYPE>::kCount;
@@ -491,7 +495,7 @@ __global__ __launch_bounds__(THREADS, VECTORS <= 4 ? 8 : 4) void distill_residen
     }
     const Places::Raw raw(a, row);
     Held<THREADS, VECTORS, TYPE> held;
-    held.load(x, span);
+    if (!MORE) held.load(x, span);
     const Places places(a, raw);
     if (!places.any) {
         write_no_loss(a, row);
@@ -501,17 +505,36 @@ __global__ __launch_bounds__(THREADS, VECTORS <= 4 ? 8 : 4) void distill_residen
     TokenLogits<TYPE> logit = {};
     float q[2] = {};
     bool first[2] = {};
+    const int held_end = MORE ? min(span.begin + kHeld, span.end) : span.end;
+    const Row<TYPE, false> again(a.logits, row * a.stride, a.vocab);  // stays in the caches
+    const Marks<N> of_more{bits, held_end};
+    if (REST && MORE) {
+        of_more.clear(span.end - held_end, THREADS);
+        __syncthreads();
+    }
     if (t < 64) {
         logit.load(places, x);
-        if constexpr (REST) marks.set(places, x.skip, span);
+        if constexpr (REST) marks.set(places, x.skip, span, held_end);
+        if (REST && MORE) of_more.set(places, x.skip, span.end - held_end);
     }
     typename TheirMarks::Word mine = {};
     if constexpr (REST) {
         __syncthreads();
         mine = marks.words[t];
     }
-    if (t < 64) places.of_tokens(seen, a.places, q, first);  // while the logits are on the way
     Adder<0> adder(a.c);
+    if (MORE) {
+        walk<THREADS, 4>(
+            again, held_end, span.end,
+            [&](Logits<TYPE> &v, int j, int) {
+                const uint32_t which = REST && j < span.end ? of_more.of(j) : 0;
+                if (which) v.fill(which);
+                adder.add(v);
+            },
+            [](const Logits<TYPE> &, int) {});
+        held.load(x, span);
+    }
+    if (t < 64) places.of_tokens(seen, a.places, q, first);  // while the logits are on the way
     held.go_through(span, [&](Logits<TYPE> &v, int j, int u) {
         if (j >= span.end) v.fill();
         if (REST && mine.of(u)) v.fill(mine.of(u));
@@ -562,6 +585,15 @@ __global__ __launch_bounds__(THREADS, VECTORS <= 4 ? 8 : 4) void distill_residen
         slope.of_others(v, a.c, g);
         if (j < span.end) to.store(g, j);
     });
+    if (MORE)
+        walk<THREADS, 4>(
+            again, held_end, span.end,
+            [&](const Logits<TYPE> &v, int j, int) {
+                float g[N];
+                slope.of_others(v, a.c, g);
+                if (j < span.end) to.store(g, j);
+            },
+            [](const Logits<TYPE> &, int) {});
     if (span.takes_end()) {
         float g[N];
         slope.of_others(ends, a.c, g);
@@ -574,12 +606,15 @@ __global__ __launch_bounds__(THREADS, VECTORS <= 4 ? 8 : 4) void distill_residen
 template <int TYPE, bool REST>
 void launch_resident(const DistillArgs &a, const LogitsPlan &form, int64_t rows, hipStream_t stream)
 {
-    const auto kernel = form.threads == 64      ? distill_resident_kernel<TYPE, 64, 4, REST>
-                        : form.threads == 256   ? distill_resident_kernel<TYPE, 256, 4, REST>
-                        : form.threads == 1024  ? distill_resident_kernel<TYPE, 1024, 16, REST>
-                        : form.vectors == 4     ? distill_resident_kernel<TYPE, 512, 4, REST>
-                        : form.vectors == 8     ? distill_resident_kernel<TYPE, 512, 8, REST>
-                                                : distill_resident_kernel<TYPE, 512, 16, REST>;
+    auto kernel = form.threads == 64    ? distill_resident_kernel<TYPE, 64, 4, REST, false>
+                  : form.threads == 256 ? distill_resident_kernel<TYPE, 256, 4, REST, false>
+                  : form.vectors == 4   ? distill_resident_kernel<TYPE, 512, 4, REST, false>
+                  : form.vectors == 8   ? distill_resident_kernel<TYPE, 512, 8, REST, false>
+                  : form.threads == 512 ? distill_resident_kernel<TYPE, 512, 16, REST, false>
+                  : form.vectors == 16  ? distill_resident_kernel<TYPE, 1024, 16, REST, false>
+                                        : distill_resident_kernel<TYPE, 1024, 16, REST, true>;
+    if constexpr (REST && TYPE != QUAMBA_F32)
+        if (form.threads == 512 && form.vectors == 32) kernel = distill_resident_kernel<TYPE, 512, 16, true, true>;
     kernel<<<(int)rows, form.threads, 0, stream>>>(a);
 }
 
@@ -615,18 +650,25 @@ void cut_into(DistillArgs &a, const LogitsPlan &plan)
 
 // Few vectors to a thread while the row's work is mostly waiting (bf16, 32 places and a rest: 256 rows of 8000 by 512 threads with 4 vectors 7.7 us, by 256
 // with 8 10.1; of 16000 8.5 and 10.2), more where several workgroups have to share a compute unit so that one's loads go while another computes (4096 rows of
-// 20000 by 1024 threads with 4 vectors 88 us, by 512 with 8 65; of 64000 by 1024 with 8 235 and by 512 with 16 186).  Few rows that take more than 16 vectors of
-// 512 threads are cut into segments instead (no rest: 1 row of 64000 logits 10.5 us held and 11.2 in segments, of 96000 13.3 and 11.2; 32 rows of
-// 128000 17.5 and 15.8, 64 17.8 and 19.7).
-LogitsPlan distill_form(int64_t rows, int32_t vocab, int32_t type, bool workspace)
+// 20000 by 1024 threads with 4 vectors 88 us, by 512 with 8 65; of 64000 by 1024 with 8 235 and by 512 with 16 186).  So the most work, that of a rest in 16-bit
+// logits, is left to two workgroups of 512 threads even where each has to read some of its row again, from the caches (4096 rows of 70000 by 1024 with 16
+// vectors 278, by 512 that hold 16 of 32 222; of 128000 414 and 404; without a rest 241 and 218, 375 and 401; 2048 of 50000 in fp32 160 and 165).
+// Rows of up to twice what 1024 threads hold are cheaper in part than in two launches (2048 of 140000 bf16 logits 210 and 271 us, of 260000 439 and 524).  Few
+// long rows are cut into segments instead (no rest: 1 row of 64000 logits 10.5 us held and 11.2 in segments, of 96000 13.3 and 11.2; 32 rows of 128000 17.5
+// and 15.8, 64 17.8 and 19.7; 40 of 200000 24.0 and 21.3, 100 24.6 and 27.8).
+LogitsPlan distill_form(int64_t rows, int32_t vocab, int32_t type, bool rest, bool workspace)
 {
-    const int vectors = logit_vectors(vocab, type);
+    const int vectors = logit_vectors(vocab, type), units = compute_units();
     if (vocab < (type == QUAMBA_F32 ? 8 : 16)) return {};  // it may have no vector of its own
     if (vectors <= wave_vectors(rows, 4 * 64)) return {64, 1, 4};
     if (vectors <= 4 * 256) return {256, 1, 4};
     for (const int each : {4, 8, 16})
         if (vectors <= each * 512) return {512, 1, each};
-    if (vectors <= 16 * 1024 && (!workspace || rows * 8 > compute_units())) return {1024, 1, 16};
+    if (vectors <= 16 * 1024 && (!workspace || rows * 8 > units)) {
+        if (rest && type != QUAMBA_F32) return {512, 1, 32};
+        return {1024, 1, 16};
+    }
+    if (vectors <= 32 * 1024 && (!workspace || rows * 4 > units)) return {1024, 1, 32};
     return {};
 }
 
@@ -636,7 +678,7 @@ template <int TYPE, bool PAST>
 hipError_t launch(DistillArgs a, void *workspace, hipStream_t stream)
 {
     const bool sums = !a.saved_sums;
-    const LogitsPlan form = sums && a.gradient ? distill_form(a.rows, a.vocab, TYPE, workspace != nullptr) : LogitsPlan{};
+    const LogitsPlan form = sums && a.gradient ? distill_form(a.rows, a.vocab, TYPE, a.rest, workspace != nullptr) : LogitsPlan{};
     const bool resident = form.threads != 0;
     const LogitsPlan plan = logits_plan(a.rows, a.vocab, TYPE, LogitsWork::distance, false, workspace != nullptr);
     const LogitsPlan gradient = gradient_plan(a.vocab, TYPE, kThreads * kGradientVectors);

@@ -462,8 +462,8 @@ struct LogitsPlan {
 enum class LogitsWork : int { sums, alternatives, distance };
 LogitsPlan logits_plan(int64_t rows, int32_t vocab, int32_t type, LogitsWork work, bool entropy, bool workspace);  // of a pass that sums
 LogitsPlan gradient_plan(int32_t vocab, int32_t type, int vectors);                                 // into segments of at most so many
-// Of loss and gradient at once: the threads that hold a row in registers and the vectors of each; none: it is not held.
-LogitsPlan distill_form(int64_t rows, int32_t vocab, int32_t type, bool workspace);
+// Of loss and gradient at once: the threads that take a row and the vectors of each, of which they hold up to 16 in registers; none: two passes.
+LogitsPlan distill_form(int64_t rows, int32_t vocab, int32_t type, bool rest, bool workspace);
 int logit_vectors(int32_t vocab, int32_t type);
 int wave_vectors(int64_t rows, int most);  // of rows that a wave takes
 bool logits_past_caches(int64_t rows, int32_t vocab, int32_t type);  // whether the logits are not to stay in the caches

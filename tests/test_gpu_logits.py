@@ -557,8 +557,9 @@ def test_distill_of_a_vocabulary_that_is_marked_in_parts(gpu_lib):
     _check_distill(gpu_lib, x[:, 3:], teacher, tokens, True)
 
 
-# Of 16-bit logits, half as many of fp32: a size of each form that holds a row in registers (test_logits_plans.py checks which), and one that does not.
-HELD = [(3, 901), (2200, 2003), (3, 7001), (3, 15001), (3, 30001), (3, 60001), (40, 130001), (35, 133001)]
+# Of 16-bit logits, half as many of fp32: a size of each form that holds a row, or most of it, in registers (test_logits_plans.py checks which), and one
+# that does not.
+HELD = [(3, 901), (2200, 2003), (3, 7001), (3, 15001), (3, 30001), (3, 60001), (40, 130001), (70, 133001), (66, 261001), (70, 270001)]
 
 
 @pytest.mark.parametrize("kind", TYPES)
@@ -574,6 +575,7 @@ def test_loss_and_gradient_of_rows_in_registers(gpu_lib, rows, vocab, rest, kind
     tokens[1::3, 7] = vocab - 1
     if vocab > 1 << 15:
         tokens[:, 8] = 1 + (1 << 15)
+        tokens[:, 9:13] = vocab // 2 + np.arange(4)
     wide = torch.zeros(rows, vocab + 5, dtype=_torch_type(kind), device="cuda")
     x = wide[:, 3:vocab + 3]
     x.copy_(_logits(rows, vocab, kind, vocab))

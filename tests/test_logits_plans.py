@@ -24,9 +24,9 @@ def _plan(rows, vocab, kind, work, entropy=False, workspace=True):
     return f(rows, vocab, kind, work, entropy, workspace)
 
 
-def _form(rows, vocab, kind, workspace=True):
-    f = _internal("_ZN6quamba12distill_formEliib", Plan, C.c_int64, C.c_int32, C.c_int32, C.c_bool)
-    return f(rows, vocab, kind, workspace)
+def _form(rows, vocab, kind, rest=False, workspace=True):
+    f = _internal("_ZN6quamba12distill_formEliibb", Plan, C.c_int64, C.c_int32, C.c_int32, C.c_bool, C.c_bool)
+    return f(rows, vocab, kind, rest, workspace)
 
 
 def _vectors(vocab, kind):
@@ -74,25 +74,29 @@ def test_a_gradients_segments_hold_the_whole_row(kind, vectors):
 
 @pytest.mark.parametrize("kind", [F32, F16, BF16])
 def test_a_row_in_registers_is_all_there(kind):
-    """A thread has room for its vectors, and the row a vector that lies inside it wherever it begins."""
+    """A thread has room for its vectors (16 in registers, as many again are read twice), and the row a vector that lies inside it wherever
+    it begins."""
     for rows in ROWS:
         for vocab in VOCABS:
             for workspace in (False, True):
-                form = _form(rows, vocab, kind, workspace)
-                if form.threads:
-                    assert _vectors(vocab, kind) <= form.threads * form.vectors and vocab >= (8 if kind == F32 else 16)
-                    assert form.segments == 1
+                for rest in (False, True):
+                    form = _form(rows, vocab, kind, rest, workspace)
+                    if form.threads:
+                        assert _vectors(vocab, kind) <= form.threads * form.vectors and vocab >= (8 if kind == F32 else 16)
+                        assert form.segments == 1 and form.vectors in (4, 8, 16, 32)
 
 
 def test_each_form_has_a_size_that_is_tested():
     from test_gpu_logits import HELD
-    forms = {F32: [], BF16: []}
-    for kind in forms:
-        for rows, vocab in HELD:
-            form = _form(rows, vocab // 2 if kind == F32 else vocab, kind)
-            forms[kind].append((form.threads, form.vectors))
-    want = [(64, 4), (64, 4), (256, 4), (512, 4), (512, 8), (512, 16), (1024, 16), (0, 0)]
-    assert forms[F32] == want and forms[BF16] == want
+    forms = {}
+    for kind in (F32, BF16):
+        for rest in (False, True):
+            of = [_form(rows, vocab // 2 if kind == F32 else vocab, kind, rest) for rows, vocab in HELD]
+            forms[kind, rest] = [(form.threads, form.vectors) for form in of]
+    want = [(64, 4), (64, 4), (256, 4), (512, 4), (512, 8), (512, 16), (1024, 16), (1024, 32), (1024, 32), (0, 0)]
+    assert forms[F32, False] == forms[F32, True] == forms[BF16, False] == want
+    want[6] = (512, 32)
+    assert forms[BF16, True] == want
     # sums, alternatives and distances by 64, 256 and 1024 threads and in segments: of test_logprobs and test_distill
     assert {_plan(r, v, BF16, SUMS).threads for r, v in ((3, 7), (3, 40000), (700, 52001))} == {64, 256, 1024}
     assert {_plan(r, v, BF16, ALTERNATIVES).threads for r, v in ((5, 33), (33, 4099), (4, 90001))} == {64, 256, 1024}
