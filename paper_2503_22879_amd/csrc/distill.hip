@@ -5,7 +5,8 @@
 //
 // One pass over a row makes its sum of exponentials and the other tokens' (whose own sum is exact where it is a small part of the row's: a
 // difference would not be); the gradient is written as if no token were the teacher's, but for those, which come from their logits and
-// places.  Bound: HBM.
+// places.  Bound: HBM (bf16: 2048 rows of 128000 logits, 64 places and a rest, 80 us, 6.1 TB/s; with the gradient, 4096 rows, 403 us, 5.1 TB/s of what has to
+// be read and written once; the gradient alone of 1000 of 50021, 20 places, 36 us, 5.4 TB/s).
 #include <algorithm>
 #include <type_traits>
 

@@ -4,8 +4,9 @@
 //   logprob = (x_t - m) / T - ln S,   S = sum_v exp((x_v - m) / T)       entropy = ln S - sum_v exp(e_v) e_v / S,   e_v = (x_v - m) / T
 //   dx_v = (g ([v = t] - p_v) - h p_v (ln p_v + entropy)) / T
 //
-// One pass over a row makes the sum, the entropy's sum and the list of the best tokens (logits.h).  Bound: HBM, the logits read once, and read
-// and written once for the gradient.
+// One pass over a row makes the sum, the entropy's sum and what bounds the best tokens (logits.h).  Bound: HBM, the logits read once, and read
+// and written once for the gradient (8192 rows of 128000 bf16 logits with 5 alternatives and the entropy 318 us, 6.2 TB/s; 2048 of 50021 alone 34 us, 5.6 TB/s;
+// the gradient of 4096 of 128000 311 us, 6.5 TB/s); single rows are two to three times a launch (1 of 50021 with 8 alternatives 9.5 us, without 5.5).
 #include <algorithm>
 
 #include "logits.h"
