@@ -8,7 +8,6 @@
 // places.  Bound: HBM (bf16: 2048 rows of 128000 logits, 64 places and a rest, 80 us, 6.1 TB/s; with the gradient, 4096 rows, 403 us, 5.1 TB/s of what has to
 // be read and written once; the gradient alone of 1000 of 50021, 20 places, 36 us, 5.4 TB/s).
 #include <algorithm>
-#include <type_traits>
 
 #include "logits.h"
 
@@ -201,7 +200,7 @@ __device__ __forceinline__ float weight_of(const DistillArgs &a, int64_t row) { 
 // The logits at the teacher's tokens: asked for early, values late.
 template <int TYPE>
 struct TokenLogits {
-    std::conditional_t<TYPE == QUAMBA_F32, uint32_t, uint16_t> bits[2];  // wider, and they would be waited for where they are made so
+    LogitBits<TYPE> bits[2];
     template <bool PAST>
     __device__ __forceinline__ void load(const Places &p, const Row<TYPE, PAST> &x)
     {
@@ -277,6 +276,11 @@ struct Marks {
         const uint32_t at = (uint32_t)(j - first) * N;
         return bits[at / 32] >> at % 32 & ((1u << N) - 1);
     }
+    __device__ __forceinline__ uint32_t is(int place) const  // from vector 0 on
+    {
+        const uint32_t at = place - first * N;
+        return bits[at / 32] >> at % 32 & 1u;
+    }
 };
 
 // A segment of a row to a workgroup; where a row has one only, that is all.  GRADIENT: with the gradient in a second pass, where there is no
@@ -317,8 +321,9 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(DistillArgs a)
             __syncthreads();
             if (t < 64) marks.set(places, x.skip, to - from);
             __syncthreads();
-            const auto add = [&](const Logits<TYPE> &v, int j) { adder.add(v, marks.of(min(j, to - 1))); };
-            walk<THREADS, 4>(x, from, to, [&](const Logits<TYPE> &v, int j, int) { add(v, j); }, add);
+            walk<THREADS, 4>(
+                x, from, to, [&](const Logits<TYPE> &v, int j, int) { adder.add(v, marks.of(min(j, to - 1))); },
+                [&](const Logits<TYPE> &v, int token) { adder.add(v, token >= 0 ? marks.is(token + x.skip) : 0u); });
             __syncthreads();
         }
     } else {
@@ -339,10 +344,10 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(DistillArgs a)
                 slope.of_others(v, a.c, g);
                 if (j < span.end) to.store(g, j);
             },
-            [&](const Logits<TYPE> &v, int j) {
+            [&](const Logits<TYPE> &v, int token) {
                 float g[N];
                 slope.of_others(v, a.c, g);
-                if (span.takes_end()) to.store_within(g, j);
+                if (token >= 0) to.store_one(g[0], token);
             });
         __syncthreads();
         if (t < 64) {
@@ -449,7 +454,7 @@ struct HeldMarks {
         __device__ __forceinline__ uint32_t of(int u) const { return w[u / 4] >> 8 * (u % 4) & 0xffu; }
     };
     Word words[THREADS];
-    uint32_t ends[2];
+    uint32_t ends;  // as in Ends, a bit for a lane
 
     // By one wave.  Vectors held_end .. span.end - 1 are not held.
     __device__ __forceinline__ void set(const Places &p, int skip, const Span &span, int held_end)
@@ -457,7 +462,7 @@ struct HeldMarks {
         const int lane = threadIdx.x & 63;
 #pragma unroll
         for (int i = 0; i < THREADS; i += 64) words[i + lane] = {};
-        if (lane < 2) ends[lane] = 0;
+        if (lane == 0) ends = 0;
 #pragma unroll
         for (int h = 0; h < 2; ++h)
             if (p.token[h] >= 0) {
@@ -465,7 +470,7 @@ struct HeldMarks {
                 if (i >= 0 && j < held_end)
                     atomicOr(&words[i % THREADS].w[u / 4], 1u << (8 * (u % 4) + at % N));
                 else if (i < 0 || j >= span.end)
-                    atomicOr(&ends[i < 0 ? 0 : 1], 1u << at % N);
+                    atomicOr(&ends, 1u << (i < 0 ? 0 : N) + at % N);
             }
     }
 };
@@ -497,6 +502,8 @@ __global__ __launch_bounds__(THREADS, VECTORS <= 4 ? 8 : 4) void distill_residen
     const Places::Raw raw(a, row);
     Held<THREADS, VECTORS, TYPE> held;
     if (!MORE) held.load(x, span);
+    Ends<TYPE> ends = {};
+    if (t < 64 && span.has_ends()) ends.load(x, span);
     const Places places(a, raw);
     if (!places.any) {
         write_no_loss(a, row);
@@ -541,15 +548,10 @@ __global__ __launch_bounds__(THREADS, VECTORS <= 4 ? 8 : 4) void distill_residen
         if (REST && mine.of(u)) v.fill(mine.of(u));
         adder.add(v);
     });
-    Logits<TYPE> ends = {};
-    int end = 0;
     if (t < 64 && span.has_ends()) {
-        Ends<TYPE> loads;
-        loads.load(x, span);
-        ends = loads.vector();
-        end = loads.j;
-        if constexpr (REST) ends.fill(marks.ends[end == 0 ? 0 : 1]);
-        adder.add(ends);
+        Logits<TYPE> v = ends.vector();
+        if constexpr (REST) v.fill(t < 32 ? marks.ends >> t & 1u : 0u);
+        adder.add(v);
     }
     logit.wait();  // before the barriers in join: the gradient may take the logits' place
     ExpSum s = adder.result(), teachers;
@@ -595,10 +597,10 @@ __global__ __launch_bounds__(THREADS, VECTORS <= 4 ? 8 : 4) void distill_residen
                 if (j < span.end) to.store(g, j);
             },
             [](const Logits<TYPE> &, int) {});
-    if (span.takes_end()) {
+    if (t < 64 && span.has_ends()) {
         float g[N];
-        slope.of_others(ends, a.c, g);
-        to.store_within(g, end);
+        slope.of_others(ends.vector(), a.c, g);
+        if (ends.token >= 0) to.store_one(g[0], ends.token);
     }
     __syncthreads();
     if (t < 64) put_tokens(a, places, q, logit, slope, to, 0, x.vectors);

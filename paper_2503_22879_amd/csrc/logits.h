@@ -1,6 +1,8 @@
 // What the kernels over rows of logits share: floats as whole numbers of the same order, 16 bytes of logits at a time, a row's running sum of
 // exponentials, and a wave's best tokens.
 #pragma once
+#include <type_traits>
+
 #include "quamba_internal.h"
 
 namespace quamba {
@@ -99,6 +101,10 @@ struct Logits {
     }
 };
 
+// A logit as it lies in memory.  Held wider, a 16-bit one would be waited for where it is widened.
+template <int TYPE>
+using LogitBits = std::conditional_t<TYPE == QUAMBA_F32, uint32_t, uint16_t>;
+
 // A row of logits as vectors of 16 bytes that lie at multiples of 16 bytes, whatever the row's address: vector j holds the logits from
 // j * kCount - skip on; what the first and the last hold around the row reads as -infinity.  PAST: the row is not to stay in the
 // caches.
@@ -151,46 +157,40 @@ struct Span {
         tail = first < last && last > whole && (whole > 0 || !head);
     }
     __device__ __forceinline__ bool has_ends() const { return head || tail; }
-    __device__ __forceinline__ bool takes_end() const { return (head && threadIdx.x == 0) || (tail && threadIdx.x == 1); }
 };
 
-// The ends of a span, in a wave: the head in lane 0, the tail in lane 1, -infinity in the others.  All loads go together.
+// What of a span lies in vectors across the row's ends, in a wave: the head's logits in the first kCount lanes, the tail's in the next, one to a lane, so that
+// all are one load.
 template <int TYPE>
 struct Ends {
-    uint32_t bits[Logits<TYPE>::kCount];
-    int j, lo, hi;  // the vector, and which of its logits are the row's
+    LogitBits<TYPE> bits;
+    int token;  // -1: the lane has none
     template <bool PAST>
     __device__ __forceinline__ void load(const Row<TYPE, PAST> &row, const Span &span)
     {
-        constexpr int N = Logits<TYPE>::kCount;
-        const int t = threadIdx.x;
-        const bool at_tail = span.tail && (t == 1 || !span.head);
-        j = at_tail ? span.whole : 0;
-        lo = j == 0 ? row.skip : 0;
-        hi = min(N, row.vocab + row.skip - j * N);
-#pragma unroll
-        for (int i = 0; i < N; ++i) bits[i] = row.bits(j, min(max(i, lo), hi - 1));
-        if (t != (at_tail ? 1 : 0)) hi = lo;  // not this lane's
+        token = token_of(row, span);
+        bits = row.bits(0, row.skip + max(token, 0));
     }
+    template <typename Row>
+    static __device__ __forceinline__ int token_of(const Row &row, const Span &span)
+    {
+        constexpr int N = Logits<TYPE>::kCount;
+        const int t = threadIdx.x, token = (t < N ? t : span.whole * N + t - N) - row.skip;
+        return (t < N ? span.head : t < 2 * N && span.tail) && token >= 0 && token < row.vocab ? token : -1;
+    }
+    // The lane's logit, and -infinity behind it.
     __device__ __forceinline__ Logits<TYPE> vector() const
     {
         Logits<TYPE> v;
         v.fill();
-#pragma unroll
-        for (int i = 0; i < Logits<TYPE>::kCount; ++i)
-            if (i >= lo && i < hi) {
-                if (Logits<TYPE>::kBytes == 4)
-                    v.w[i] = bits[i];
-                else
-                    v.w[i / 2] = i & 1 ? (v.w[i / 2] & 0xffffu) | bits[i] << 16 : (v.w[i / 2] & 0xffff0000u) | bits[i];
-            }
+        if (token >= 0) v.w[0] = Logits<TYPE>::kBytes == 4 ? bits : (v.w[0] & 0xffff0000u) | bits;
         return v;
     }
 };
 
 // Vectors first .. last - 1 of a row by a workgroup of THREADS: each(v, j, u) for those that lie inside the row, the vectors of a thread in
-// rising order, u = 0 .. U - 1 in turn; in every thread of a wave as often, with -infinity where there is none.  At last end(v, j) for the row's first and last vector, where
-// they lie across its ends, in the first wave (Span::takes_end).
+// rising order, u = 0 .. U - 1 in turn; in every thread of a wave as often, with -infinity where there is none.  At last end(v, token) for the first and last logits that
+// no such vector has, in the first wave, if there are some (Ends; token -1 in lanes that have none).
 //
 // U loads of a thread are on their way together, and what follows them waits for one after the other; there is no branch between a load
 // and its use, since behind one the compiler waits for all loads.  The next U are not asked for ahead: with 8 waves to a SIMD the other
@@ -201,6 +201,8 @@ __device__ __forceinline__ void walk(const Row<TYPE, PAST> &row, int first, int 
     constexpr int kStep = THREADS * U;
     const int t = threadIdx.x;
     const Span span(row, first, last);
+    Ends<TYPE> ends;
+    if (t < 64 && span.has_ends()) ends.load(row, span);
     int from = span.begin;
     for (; from + kStep <= span.end; from += kStep) {
         Logits<TYPE> v[U];
@@ -220,11 +222,7 @@ __device__ __forceinline__ void walk(const Row<TYPE, PAST> &row, int first, int 
                 each(v[u], from + u * THREADS + t, u);
             }
     }
-    if (t < 64 && span.has_ends()) {
-        Ends<TYPE> ends;
-        ends.load(row, span);
-        end(ends.vector(), ends.j);
-    }
+    if (t < 64 && span.has_ends()) end(ends.vector(), ends.token);
 }
 
 // A sum of exponentials 2^e, e = (x - reference) c with c = log2(e) / temperature.  The reference is a logit that was among the largest when
@@ -566,6 +564,8 @@ __device__ __forceinline__ void best_tokens(TopKeys<THREADS / 64> &shared, const
     constexpr int WAVES = THREADS / 64, N = Logits<TYPE>::kCount, kStep = THREADS * U, kRoom = WAVES * kListed, kShare = THREADS > 256 ? THREADS / 256 : 1;
     const int t = threadIdx.x, lane = t & 63;
     const Span span(row, first, last);
+    Ends<TYPE> ends;
+    if (t < 64 && span.has_ends()) ends.load(row, span);
     float top = tops[0];
 #pragma unroll
     for (int u = 1; u < U; ++u) top = fmaxf(top, tops[u]);
@@ -596,12 +596,12 @@ __device__ __forceinline__ void best_tokens(TopKeys<THREADS / 64> &shared, const
         bound = n >= count ? higher : bound;
     }
     const float least = fmaxf(of_ordered(max(bound, 1u)), -__FLT_MAX__);
-    auto take = [&](const Logits<TYPE> &v, int j) {
+    auto take = [&](const Logits<TYPE> &v, int token) {
 #pragma unroll
         for (int e = 0; e < N; ++e)
             if (v[e] >= least) {
                 const int at = atomicAdd(&shared.n, 1);
-                if (at < kRoom) shared.keys[at / kListed][at % kListed] = key_of(v[e], row.token(j) + e);
+                if (at < kRoom) shared.keys[at / kListed][at % kListed] = key_of(v[e], token + e);
             }
     };
 #pragma unroll
@@ -614,14 +614,10 @@ __device__ __forceinline__ void best_tokens(TopKeys<THREADS / 64> &shared, const
         if (j < span.end) {
             Logits<TYPE> v;
             row.load(v, j);
-            take(v, j);
+            take(v, row.token(j));
         }
     }
-    if (t < 64 && span.has_ends()) {
-        Ends<TYPE> ends;
-        ends.load(row, span);
-        if (span.takes_end()) take(ends.vector(), ends.j);
-    }
+    if (t < 64 && span.has_ends()) take(ends.vector(), ends.token);
     __syncthreads();
     const int n = shared.n;
     __syncthreads();  // all know it
@@ -633,8 +629,8 @@ __device__ __forceinline__ void best_tokens(TopKeys<THREADS / 64> &shared, const
             [&](const Logits<TYPE> &v, int j, int) {
                 list.template offer<N, true>(largest(v), [&](int e) { return v.at(e); }, [&](int e) { return key_of(v.at(e), row.token(j) + e); });
             },
-            [&](const Logits<TYPE> &v, int j) {
-                list.template offer<N, false>(largest(v), [&](int e) { return v.at(e); }, [&](int e) { return key_of(v.at(e), row.token(j) + e); });
+            [&](const Logits<TYPE> &v, int token) {
+                list.template offer<1, false>(v[0], [&](int) { return v[0]; }, [&](int) { return key_of(v[0], token); });
             });
         list.ranked(out);
         return;
@@ -699,13 +695,6 @@ struct GradientRow {
         else
             *reinterpret_cast<uint16_t *>(p) = (uint16_t)b;
     }
-    __device__ __forceinline__ void store_within(const float (&v)[kCount], int j) const  // what of it is the row's
-    {
-        const int token = j * kCount - skip;
-#pragma unroll
-        for (int i = 0; i < kCount; ++i)
-            if (token + i >= 0 && token + i < vocab) store_one(v[i], token + i);
-    }
 };
 
 // Up to THREADS * VECTORS vectors of a row in a workgroup's registers.  All are asked for together and without a branch between them (behind one
@@ -729,7 +718,7 @@ struct Held {
     }
 };
 
-// A segment of a row's gradient: make(v, j, g) is that of vector j.  It may take the logits' place: a vector's values are read before they are
+// A segment of a row's gradient: make(v, token, g) is that of the logits v from `token` on.  It may take the logits' place: a vector's values are read before they are
 // written, by the same thread, and by no other.
 template <int THREADS, int VECTORS, int TYPE, bool PAST>
 struct GradientSegment {
@@ -752,13 +741,13 @@ struct GradientSegment {
     {
         held.go_through(span, [&](const Logits<TYPE> &v, int j, int) {
             float g[Logits<TYPE>::kCount];
-            make(v, j, g);
+            make(v, x.token(j), g);
             if (j < span.end) to.store(g, j);
         });
-        if (span.takes_end()) {
+        if (threadIdx.x < 64 && span.has_ends()) {
             float g[Logits<TYPE>::kCount];
-            make(ends.vector(), ends.j, g);
-            to.store_within(g, ends.j);
+            make(ends.vector(), ends.token, g);
+            if (ends.token >= 0) to.store_one(g[0], ends.token);
         }
     }
 };
@@ -780,7 +769,8 @@ __device__ __forceinline__ void write_zeros(const Row<TYPE, PAST> &x, const Grad
     const float zero[Logits<TYPE>::kCount] = {};
     const Span span(x, first, last);
     for (int j = span.begin + threadIdx.x; j < span.end; j += THREADS) to.store(zero, j);
-    if (span.takes_end()) to.store_within(zero, span.tail && (threadIdx.x == 1 || !span.head) ? span.whole : 0);
+    const int token = Ends<TYPE>::token_of(x, span);
+    if (token >= 0) to.store_one(0.0f, token);
 }
 
 }  // namespace

@@ -164,13 +164,13 @@ __global__ __launch_bounds__(kThreads) void token_logprobs_backward_kernel(Logpr
     const Saved saved(a.log_sums[row], a.temperature, a.c);
     // -g p - h p (ln p + entropy), over T: p (flat + tilted log2 p)
     const float flat = -(ENTROPY ? fmaf(h, entropy, g) : g) * a.per_temperature, tilted = -h * 0.693147180559945309f * a.per_temperature;
-    segment_of.write([&](const Logits<TYPE> &v, int j, float(&d)[N]) {
+    segment_of.write([&](const Logits<TYPE> &v, int token, float(&d)[N]) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const float e = fmaf(v[i] - saved.reference, a.c, -saved.log), p = exp2_of(e);
             d[i] = p * (ENTROPY ? fmaf(tilted, fmaxf(e, kFarBelow), flat) : flat);
         }
-        const int at = target - x.token(j);
+        const int at = target - token;
         if (at >= 0 && at < N) {
 #pragma unroll
             for (int i = 0; i < N; ++i) d[i] = i == at ? fmaf(g, a.per_temperature, d[i]) : d[i];
