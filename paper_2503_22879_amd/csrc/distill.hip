@@ -683,7 +683,7 @@ hipError_t launch(DistillArgs a, void *workspace, hipStream_t stream)
     const bool sums = !a.saved_sums;
     const LogitsPlan form = sums && a.gradient ? distill_form(a.rows, a.vocab, TYPE, a.rest, workspace != nullptr) : LogitsPlan{};
     const bool resident = form.threads != 0;
-    const LogitsPlan plan = logits_plan(a.rows, a.vocab, TYPE, LogitsWork::distance, false, workspace != nullptr);
+    const LogitsPlan plan = logits_plan(a.rows, a.vocab, TYPE, true, 0, false, workspace != nullptr);
     const LogitsPlan gradient = gradient_plan(a.vocab, TYPE, kThreads * kGradientVectors);
     a.parts = static_cast<LogitsPart *>(workspace);
     a.row_parts = plan.segments;
@@ -716,7 +716,7 @@ size_t distill_workspace_bytes(int64_t rows, int32_t vocab)
 {
     size_t most = 0;  // over the types
     for (const int type : {QUAMBA_F32, QUAMBA_BF16}) {
-        most = std::max(most, (size_t)rows * logits_plan(rows, vocab, type, LogitsWork::distance, false, true).segments * sizeof(LogitsPart));
+        most = std::max(most, (size_t)rows * logits_plan(rows, vocab, type, true, 0, false, true).segments * sizeof(LogitsPart));
     }
     return most;
 }

@@ -459,8 +459,8 @@ constexpr int kMaxPlaces = 128;  // of a teacher
 struct LogitsPlan {
     int threads, segments, vectors;
 };
-enum class LogitsWork : int { sums, alternatives, distance };
-LogitsPlan logits_plan(int64_t rows, int32_t vocab, int32_t type, LogitsWork work, bool entropy, bool workspace);  // of a pass that sums
+// Of a pass that sums: a distance's, or with `count` alternatives and the entropy or without.
+LogitsPlan logits_plan(int64_t rows, int32_t vocab, int32_t type, bool distance, int32_t count, bool entropy, bool workspace);
 LogitsPlan gradient_plan(int32_t vocab, int32_t type, int vectors);                                 // into segments of at most so many
 // Of loss and gradient at once: the threads that take a row and the vectors of each, of which they hold up to 16 in registers; none: two passes.
 LogitsPlan distill_form(int64_t rows, int32_t vocab, int32_t type, bool rest, bool workspace);

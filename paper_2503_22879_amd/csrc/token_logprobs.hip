@@ -198,15 +198,17 @@ int wave_vectors(int64_t rows, int most) { return (int)std::min<int64_t>(most, s
 // segments: 1 row of 70000 bf16 logits 5.8 and 7.3 us, of 70564 fp32 ones 5.9 and 7.3; 13 rows of 100000 both 7.4, with 5 alternatives 11.6 and 10.8; of
 // 166139 10.0 and 7.4, 15.2 and 11.8; 64 rows of 128000 with 20 alternatives 14.4 and 15.2).  Entropies and distances take half as much time again for a
 // logit and are cut earlier (64 rows of 128000 fp32 logits with 20 alternatives and the entropy 21.3 and 17.4; the distance of 1 row of 70000 bf16 ones, 32 places
-// and a rest, 8.1 and 6.4).
-LogitsPlan logits_plan(int64_t rows, int32_t vocab, int32_t type, LogitsWork work, bool entropy, bool workspace)
+// and a rest, 8.1 and 6.4).  Segments are as many as fill the card, but with alternatives half of that and no shorter than 40 vectors for each of them, for the
+// launch that joins them goes through all (4 rows of 150000 with 64 alternatives 21.6 and 16.5 us, 64 of 128000 in bf16 with 20 and the entropy 15.8 and 14.8).
+LogitsPlan logits_plan(int64_t rows, int32_t vocab, int32_t type, bool distance, int32_t count, bool entropy, bool workspace)
 {
     const int units = compute_units(), vectors = logit_vectors(vocab, type);
-    const bool best = work == LogitsWork::alternatives;
+    const bool best = count > 0, more = entropy || distance;
     if (vectors <= wave_vectors(rows, 512)) return {64, 1, 0};
-    const bool more = entropy || work == LogitsWork::distance;
     if (workspace && rows * (best && more ? 4 : 8) <= units && vocab > (more && !best ? 60000 : 100000)) {
-        const int segments = (int)std::min<int64_t>({(4 * units + rows - 1) / rows, (vectors + 511) / 512, 256}), each = (vectors + segments - 1) / segments;
+        const int least = std::max(512, 40 * count);
+        const int segments = (int)std::min<int64_t>({((best ? 2 : 4) * units + rows - 1) / rows, (vectors + least - 1) / least, 256});
+        const int each = (vectors + segments - 1) / segments;
         return {256, (vectors + each - 1) / each, each};
     }
     return {rows <= units && vectors > (best ? 8000 : 4000) ? 1024 : 256, 1, 0};
@@ -251,12 +253,10 @@ void launch_rows(const LogprobArgs &a, int threads, int64_t rows, bool past, hip
     join_kernel<<<(int)rows, kThreads, 0, stream>>>(a);
 }
 
-LogitsWork work_of(int count) { return count ? LogitsWork::alternatives : LogitsWork::sums; }
-
 template <int TYPE>
 hipError_t launch(LogprobArgs a, void *workspace, hipStream_t stream)
 {
-    const LogitsPlan plan = logits_plan(a.rows, a.vocab, TYPE, work_of(a.count), a.entropies != nullptr, workspace != nullptr);
+    const LogitsPlan plan = logits_plan(a.rows, a.vocab, TYPE, false, a.count, a.entropies != nullptr, workspace != nullptr);
     a.segments = plan.segments;
     a.segment_vectors = plan.vectors;
     a.by_segments = divisor((uint32_t)plan.segments);
@@ -301,7 +301,7 @@ size_t token_logprobs_workspace_bytes(int64_t rows, int32_t vocab, int32_t count
     size_t most = 0;  // over the types, with entropies and without
     for (const int type : {QUAMBA_F32, QUAMBA_BF16})
         for (const bool entropy : {false, true}) {
-            const int segments = logits_plan(rows, vocab, type, work_of(count), entropy, true).segments;
+            const int segments = logits_plan(rows, vocab, type, false, count, entropy, true).segments;
             if (segments > 1) most = std::max(most, (size_t)rows * segments * (sizeof(LogitsPart) + sizeof(uint64_t) * count));
         }
     return most;

@@ -6,7 +6,7 @@ import pytest
 import paper_2503_22879_amd as q
 
 F32, F16, BF16 = range(3)
-SUMS, ALTERNATIVES, DISTANCE = range(3)
+SUMS, ALTERNATIVES, MANY, DISTANCE = 0, 8, 128, -1      # so many alternatives, or a distance
 
 
 class Plan(C.Structure):
@@ -20,8 +20,8 @@ def _internal(name, restype, *argtypes):
 
 
 def _plan(rows, vocab, kind, work, entropy=False, workspace=True):
-    f = _internal("_ZN6quamba11logits_planEliiNS_10LogitsWorkEbb", Plan, C.c_int64, C.c_int32, C.c_int32, C.c_int, C.c_bool, C.c_bool)
-    return f(rows, vocab, kind, work, entropy, workspace)
+    f = _internal("_ZN6quamba11logits_planEliibibb", Plan, C.c_int64, C.c_int32, C.c_int32, C.c_bool, C.c_int32, C.c_bool, C.c_bool)
+    return f(rows, vocab, kind, work == DISTANCE, max(work, 0), entropy, workspace)
 
 
 def _form(rows, vocab, kind, rest=False, workspace=True):
@@ -39,12 +39,12 @@ VOCABS = [1, 7, 8, 9, 500, 1025, 2048, 4100, 16000, 32768, 50021, 60001, 65536, 
 
 
 @pytest.mark.parametrize("kind", [F32, F16, BF16])
-@pytest.mark.parametrize("work", [SUMS, ALTERNATIVES, DISTANCE])
+@pytest.mark.parametrize("work", [SUMS, ALTERNATIVES, MANY, DISTANCE])
 def test_segments_hold_the_whole_row(work, kind):
     for rows in ROWS:
         for vocab in VOCABS:
             size = (q.quamba_distill_loss_workspace_size(rows, vocab, 8) if work == DISTANCE
-                    else q.quamba_token_logprobs_workspace_size(rows, vocab, 8 if work == ALTERNATIVES else 0))
+                    else q.quamba_token_logprobs_workspace_size(rows, vocab, work))
             for entropy in (False, True):
                 assert _plan(rows, vocab, kind, work, entropy, False).segments == 1     # they need a place to meet
                 plan = _plan(rows, vocab, kind, work, entropy)
@@ -54,7 +54,7 @@ def test_segments_hold_the_whole_row(work, kind):
                 else:
                     assert plan.segments <= 256 and plan.threads == 256
                     assert plan.segments * plan.vectors >= _vectors(vocab, kind) > (plan.segments - 1) * plan.vectors
-                    assert size >= rows * plan.segments * (16 + (8 * 8 if work == ALTERNATIVES else 0))
+                    assert size >= rows * plan.segments * (16 + 8 * max(work, 0))
                 if work == DISTANCE:
                     assert size >= 16 * rows * plan.segments
                 if plan.threads == 64:
