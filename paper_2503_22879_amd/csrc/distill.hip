@@ -383,7 +383,9 @@ __global__ __launch_bounds__(64) void distill_join_kernel(DistillArgs a)
 }
 
 // A segment of a row's gradient to a workgroup: from the sums that the launches in front left, or from those of an earlier call.  One wave makes
-// what the others need, while their logits are on the way.
+// what the others need, while their logits are on the way.  Joining: each workgroup joins the sums of the row's parts for itself and the first one of a
+// row writes its loss, which saves a launch (1 row of 144086 bf16 logits, 95 places, 10.6 -> 8.5 us, 21 of 90480 11.8 -> 9.3); it reads the teacher's logits while others write, so not
+// where the gradient takes their place.
 template <int TYPE, bool PAST>
 __global__ __launch_bounds__(kThreads) void distill_gradient_kernel(DistillArgs a)
 {
@@ -398,7 +400,9 @@ __global__ __launch_bounds__(kThreads) void distill_gradient_kernel(DistillArgs 
     const GradientRow<TYPE, PAST> to(a.gradient, row * a.gradient_stride, x);
     const int first = segment * a.segment_vectors, last = min(first + a.segment_vectors, x.vectors);
     const float weight = weight_of(a, row);
+    const bool loss = a.joining && segment == 0;
     if (weight == 0.0f) {
+        if (loss) write_no_loss(a, row);
         write_zeros<kThreads>(x, to, first, last);
         return;
     }
@@ -407,14 +411,12 @@ __global__ __launch_bounds__(kThreads) void distill_gradient_kernel(DistillArgs 
     TokenLogits<TYPE> logit;
     if (t < 64) {
         places = Places(a, row);
+        RowSums sums;
+        TokenLogits<TYPE> of_row;
+        if (!a.saved_sums) sums = RowSums(join<false, 64>(a.parts + (int64_t)local * a.row_parts, a.joining ? a.row_parts : 1, a.c));
+        if (loss) of_row.load(places, x);
         segment_of.load();
-        Slope slope;
-        if (a.saved_sums) {
-            slope = slope_of(a, weight, row, places.sum);
-        } else {
-            const LogitsPart part = a.parts[(int64_t)local * a.row_parts];
-            slope = slope_of(a, weight, RowSums(part.reference, part.sum, part.reference, part.second), places.sum);
-        }
+        const Slope slope = a.saved_sums ? slope_of(a, weight, row, places.sum) : slope_of(a, weight, sums, places.sum);
         const bool here = places.template is_in<TYPE>(0, x.skip, first, last) || places.template is_in<TYPE>(1, x.skip, first, last);
         const bool tokens = __builtin_amdgcn_ballot_w64(here) != 0;
         if (tokens) {
@@ -425,6 +427,10 @@ __global__ __launch_bounds__(kThreads) void distill_gradient_kernel(DistillArgs 
             shared_tokens = places.any ? (tokens ? 1 : 0) : -1;
             shared_slope = slope;
         }
+        if (loss && places.any)
+            write_loss(a, row, places, of_row, sums);
+        else if (loss)
+            write_no_loss(a, row);
     } else {
         segment_of.load();
     }
@@ -639,7 +645,7 @@ void launch_sums(const DistillArgs &a, int threads, int64_t rows, hipStream_t st
         launch_first<TYPE, 64, false, false>(a, grid, stream);
     else
         launch_first<TYPE, 256, PAST, false>(a, grid, stream);
-    if (a.segments > 1) distill_join_kernel<TYPE><<<(int)rows, 64, 0, stream>>>(a);
+    if (a.segments > 1 && !a.joining) distill_join_kernel<TYPE><<<(int)rows, 64, 0, stream>>>(a);
 }
 
 void cut_into(DistillArgs &a, const LogitsPlan &plan)
@@ -687,6 +693,7 @@ hipError_t launch(DistillArgs a, void *workspace, hipStream_t stream)
     const LogitsPlan gradient = gradient_plan(a.vocab, TYPE, kThreads * kGradientVectors);
     a.parts = static_cast<LogitsPart *>(workspace);
     a.row_parts = plan.segments;
+    a.joining = plan.segments > 1 && a.gradient && a.gradient != a.logits;
     const int64_t most = a.gradient && !resident ? kRowsOfALaunch / gradient.segments : kRowsOfALaunch;
     for (a.first_row = 0; a.first_row < a.rows; a.first_row += most) {
         const int64_t rows = std::min(a.rows - a.first_row, most);

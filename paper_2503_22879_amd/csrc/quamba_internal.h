@@ -519,6 +519,7 @@ struct DistillArgs {
     Divisor by_segments;
     int32_t segments, segment_vectors;
     int32_t row_parts;                           // parts of a row
+    bool joining;                                // the gradient's launch joins them
 };
 size_t distill_workspace_bytes(int64_t rows, int32_t vocab);
 hipError_t launch_distill(const DistillArgs &a, void *workspace, hipStream_t stream);
