@@ -655,6 +655,9 @@ void cut_into(DistillArgs &a, const LogitsPlan &plan)
     a.by_segments = divisor((uint32_t)plan.segments);
 }
 
+// The gradient's launch joins segments where it does not take the logits' place.
+LogitsWork work_of(bool in_place) { return in_place ? LogitsWork::distance : LogitsWork::step; }
+
 }  // namespace
 
 // Few vectors to a thread while the row's work is mostly waiting (bf16, 32 places and a rest: 256 rows of 8000 by 512 threads with 4 vectors 7.7 us, by 256
@@ -662,22 +665,19 @@ void cut_into(DistillArgs &a, const LogitsPlan &plan)
 // 20000 by 1024 threads with 4 vectors 88 us, by 512 with 8 65; of 64000 by 1024 with 8 235 and by 512 with 16 186).  So the most work, that of a rest in 16-bit
 // logits, is left to two workgroups of 512 threads even where each has to read some of its row again, from the caches (4096 rows of 70000 by 1024 with 16
 // vectors 278, by 512 that hold 16 of 32 222; of 128000 414 and 404; without a rest 241 and 218, 375 and 401; 2048 of 50000 in fp32 160 and 165).
-// Rows of up to twice what 1024 threads hold are cheaper in part than in two launches (2048 of 140000 bf16 logits 210 and 271 us, of 260000 439 and 524).  Few
-// long rows are cut into segments instead (no rest: 1 row of 64000 logits 10.5 us held and 11.2 in segments, of 96000 13.3 and 11.2; 32 rows of 128000 17.5
-// and 15.8, 64 17.8 and 19.7; 40 of 200000 24.0 and 21.3, 100 24.6 and 27.8).
-LogitsPlan distill_form(int64_t rows, int32_t vocab, int32_t type, bool rest, bool workspace)
+// Rows of up to twice what 1024 threads hold are cheaper in part than in two launches (2048 of 140000 bf16 logits 210 and 271 us, of 260000 439 and 524; 100 of
+// 200000 24.6 and 27.8).  Few long rows are cut into segments instead.
+LogitsPlan distill_form(int64_t rows, int32_t vocab, int32_t type, bool rest, bool in_place, bool workspace)
 {
-    const int vectors = logit_vectors(vocab, type), units = compute_units();
+    const int vectors = logit_vectors(vocab, type);
     if (vocab < (type == QUAMBA_F32 ? 8 : 16)) return {};  // it may have no vector of its own
+    if (logits_plan(rows, vocab, type, work_of(in_place), 0, false, workspace).segments > 1) return {};
     if (vectors <= wave_vectors(rows, 4 * 64)) return {64, 1, 4};
     if (vectors <= 4 * 256) return {256, 1, 4};
     for (const int each : {4, 8, 16})
         if (vectors <= each * 512) return {512, 1, each};
-    if (vectors <= 16 * 1024 && (!workspace || rows * 8 > units)) {
-        if (rest && type != QUAMBA_F32) return {512, 1, 32};
-        return {1024, 1, 16};
-    }
-    if (vectors <= 32 * 1024 && (!workspace || rows * 4 > units)) return {1024, 1, 32};
+    if (vectors <= 16 * 1024) return rest && type != QUAMBA_F32 ? LogitsPlan{512, 1, 32} : LogitsPlan{1024, 1, 16};
+    if (vectors <= 32 * 1024) return {1024, 1, 32};
     return {};
 }
 
@@ -687,13 +687,14 @@ template <int TYPE, bool PAST>
 hipError_t launch(DistillArgs a, void *workspace, hipStream_t stream)
 {
     const bool sums = !a.saved_sums;
-    const LogitsPlan form = sums && a.gradient ? distill_form(a.rows, a.vocab, TYPE, a.rest, workspace != nullptr) : LogitsPlan{};
+    const bool in_place = a.gradient == a.logits, step = sums && a.gradient;
+    const LogitsPlan form = step ? distill_form(a.rows, a.vocab, TYPE, a.rest, in_place, workspace != nullptr) : LogitsPlan{};
     const bool resident = form.threads != 0;
-    const LogitsPlan plan = logits_plan(a.rows, a.vocab, TYPE, true, 0, false, workspace != nullptr);
+    const LogitsPlan plan = logits_plan(a.rows, a.vocab, TYPE, step ? work_of(in_place) : LogitsWork::distance, 0, false, workspace != nullptr);
     const LogitsPlan gradient = gradient_plan(a.vocab, TYPE, kThreads * kGradientVectors);
     a.parts = static_cast<LogitsPart *>(workspace);
     a.row_parts = plan.segments;
-    a.joining = plan.segments > 1 && a.gradient && a.gradient != a.logits;
+    a.joining = plan.segments > 1 && step && !in_place;
     const int64_t most = a.gradient && !resident ? kRowsOfALaunch / gradient.segments : kRowsOfALaunch;
     for (a.first_row = 0; a.first_row < a.rows; a.first_row += most) {
         const int64_t rows = std::min(a.rows - a.first_row, most);
@@ -721,10 +722,10 @@ hipError_t launch(const DistillArgs &a, void *workspace, hipStream_t stream)
 
 size_t distill_workspace_bytes(int64_t rows, int32_t vocab)
 {
-    size_t most = 0;  // over the types
-    for (const int type : {QUAMBA_F32, QUAMBA_BF16}) {
-        most = std::max(most, (size_t)rows * logits_plan(rows, vocab, type, true, 0, false, true).segments * sizeof(LogitsPart));
-    }
+    size_t most = 0;  // over the types, with the gradient and without
+    for (const int type : {QUAMBA_F32, QUAMBA_BF16})
+        for (const LogitsWork work : {LogitsWork::distance, LogitsWork::step})
+            most = std::max(most, (size_t)rows * logits_plan(rows, vocab, type, work, 0, false, true).segments * sizeof(LogitsPart));
     return most;
 }
 

@@ -459,11 +459,12 @@ constexpr int kMaxPlaces = 128;  // of a teacher
 struct LogitsPlan {
     int threads, segments, vectors;
 };
-// Of a pass that sums: a distance's, or with `count` alternatives and the entropy or without.
-LogitsPlan logits_plan(int64_t rows, int32_t vocab, int32_t type, bool distance, int32_t count, bool entropy, bool workspace);
+// Of a pass that sums: with `count` alternatives and the entropy or without, a distance's, or a distance's in front of its gradient's launch, which joins segments.
+enum class LogitsWork : int { answers, distance, step };
+LogitsPlan logits_plan(int64_t rows, int32_t vocab, int32_t type, LogitsWork work, int32_t count, bool entropy, bool workspace);
 LogitsPlan gradient_plan(int32_t vocab, int32_t type, int vectors);                                 // into segments of at most so many
 // Of loss and gradient at once: the threads that take a row and the vectors of each, of which they hold up to 16 in registers; none: two passes.
-LogitsPlan distill_form(int64_t rows, int32_t vocab, int32_t type, bool rest, bool workspace);
+LogitsPlan distill_form(int64_t rows, int32_t vocab, int32_t type, bool rest, bool in_place, bool workspace);
 int logit_vectors(int32_t vocab, int32_t type);
 int wave_vectors(int64_t rows, int most);  // of rows that a wave takes
 bool logits_past_caches(int64_t rows, int32_t vocab, int32_t type);  // whether the logits are not to stay in the caches

@@ -200,12 +200,16 @@ int wave_vectors(int64_t rows, int most) { return (int)std::min<int64_t>(most, s
 // logit and are cut earlier (64 rows of 128000 fp32 logits with 20 alternatives and the entropy 21.3 and 17.4; the distance of 1 row of 70000 bf16 ones, 32 places
 // and a rest, 8.1 and 6.4).  Segments are as many as fill the card, but with alternatives half of that and no shorter than 40 vectors for each of them, for the
 // launch that joins them goes through all (4 rows of 150000 with 64 alternatives 21.6 and 16.5 us, 64 of 128000 in bf16 with 20 and the entropy 15.8 and 14.8).
-LogitsPlan logits_plan(int64_t rows, int32_t vocab, int32_t type, bool distance, int32_t count, bool entropy, bool workspace)
+// In front of a gradient's launch that joins them they cost no launch (held in registers and in segments, 32 places, a rest: 32 rows of 42000 bf16 logits 9.6 and 9.4,
+// of 64000 12.0 and 10.2; 16 of 50000 fp32 ones 12.1, by 1024 threads, and 8.8; 64 rows of 64000 12.3 and 12.6, of 90000 16.2 and 14.1).
+LogitsPlan logits_plan(int64_t rows, int32_t vocab, int32_t type, LogitsWork work, int32_t count, bool entropy, bool workspace)
 {
     const int units = compute_units(), vectors = logit_vectors(vocab, type);
-    const bool best = count > 0, more = entropy || distance;
+    const bool best = count > 0, more = entropy || work == LogitsWork::distance;
+    const auto few_long = [&](int least_units, int least_vocab) { return rows * least_units <= units && vocab > least_vocab; };
     if (vectors <= wave_vectors(rows, 512)) return {64, 1, 0};
-    if (workspace && rows * (best && more ? 4 : 8) <= units && vocab > (more && !best ? 60000 : 100000)) {
+    if (workspace && (work == LogitsWork::step ? few_long(8, 40000) || few_long(4, 80000)
+                                               : few_long(best && more ? 4 : 8, more && !best ? 60000 : 100000))) {
         const int least = std::max(512, 40 * count);
         const int segments = (int)std::min<int64_t>({((best ? 2 : 4) * units + rows - 1) / rows, (vectors + least - 1) / least, 256});
         const int each = (vectors + segments - 1) / segments;
@@ -256,7 +260,7 @@ void launch_rows(const LogprobArgs &a, int threads, int64_t rows, bool past, hip
 template <int TYPE>
 hipError_t launch(LogprobArgs a, void *workspace, hipStream_t stream)
 {
-    const LogitsPlan plan = logits_plan(a.rows, a.vocab, TYPE, false, a.count, a.entropies != nullptr, workspace != nullptr);
+    const LogitsPlan plan = logits_plan(a.rows, a.vocab, TYPE, LogitsWork::answers, a.count, a.entropies != nullptr, workspace != nullptr);
     a.segments = plan.segments;
     a.segment_vectors = plan.vectors;
     a.by_segments = divisor((uint32_t)plan.segments);
@@ -301,7 +305,7 @@ size_t token_logprobs_workspace_bytes(int64_t rows, int32_t vocab, int32_t count
     size_t most = 0;  // over the types, with entropies and without
     for (const int type : {QUAMBA_F32, QUAMBA_BF16})
         for (const bool entropy : {false, true}) {
-            const int segments = logits_plan(rows, vocab, type, false, count, entropy, true).segments;
+            const int segments = logits_plan(rows, vocab, type, LogitsWork::answers, count, entropy, true).segments;
             if (segments > 1) most = std::max(most, (size_t)rows * segments * (sizeof(LogitsPart) + sizeof(uint64_t) * count));
         }
     return most;

@@ -557,9 +557,10 @@ def test_distill_of_a_vocabulary_that_is_marked_in_parts(gpu_lib):
     _check_distill(gpu_lib, x[:, 3:], teacher, tokens, True)
 
 
-# Of 16-bit logits, half as many of fp32: a size of each form that holds a row, or most of it, in registers (test_logits_plans.py checks which), and one
-# that does not.
-HELD = [(3, 901), (2200, 2003), (3, 7001), (3, 15001), (3, 30001), (3, 60001), (40, 130001), (70, 133001), (66, 261001), (70, 270001)]
+# Of 16-bit logits, half as many of fp32: a size of each form that holds a row, or most of it, in registers (test_logits_plans.py checks which), one that
+# does not, and two that are cut into segments.
+HELD = [(3, 901), (2200, 2003), (3, 7001), (3, 15001), (3, 30001), (40, 60001), (70, 130001), (70, 133001), (66, 261001), (70, 270001),
+        (3, 60001), (40, 130001)]
 
 
 @pytest.mark.parametrize("kind", TYPES)
@@ -579,7 +580,23 @@ def test_loss_and_gradient_of_rows_in_registers(gpu_lib, rows, vocab, rest, kind
     wide = torch.zeros(rows, vocab + 5, dtype=_torch_type(kind), device="cuda")
     x = wide[:, 3:vocab + 3]
     x.copy_(_logits(rows, vocab, kind, vocab))
-    _check_distill(gpu_lib, x, teacher, tokens, rest, np.linspace(-0.5, 2, rows), some=some)
+    w = np.linspace(-0.5, 2, rows)
+    w[some[1]] = 0                    # a row that is left out, and one without a teacher
+    teacher[some[2]] = -np.inf
+    _check_distill(gpu_lib, x, teacher, tokens, rest, w, some=some)
+
+
+@pytest.mark.parametrize("kind", ["fp32", "bf16"])
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("rows,vocab", [(3, 130001), (40, 60001), (70, 133001), (66, 261001), (33, 270001)])
+def test_loss_and_gradient_of_long_rows_in_the_logits_place(gpu_lib, rows, vocab, rest, kind):
+    """Held, held in part, in segments and in two passes."""
+    vocab = vocab // 2 if kind == "fp32" else vocab
+    some = np.array([0, 1, rows - 1])
+    teacher, tokens = _teacher(rows, vocab, 33, rest, vocab)
+    teacher[1] = -np.inf
+    x = _logits(rows, vocab, kind, rows)
+    _check_distill(gpu_lib, x, teacher, tokens, rest, None, 1.3 if not rest else 1.0, out=x, some=some)
 
 
 @pytest.mark.parametrize("kind,rows,vocab", [("bf16", 700, 52001), ("fp16", 300, 131501), ("fp32", 300, 70001)])
