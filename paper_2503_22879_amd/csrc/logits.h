@@ -238,6 +238,10 @@ struct ExpSum {
 };
 constexpr float kFarBelow = -200.0f;  // 2^-200 is 0, and 0 times this as well
 
+// Products x c below this round to within half a unit, so that 2^ of what the rounding leaves is a factor of at most 2^0.5.  From 2^31 on (a finite mask
+// of -10^10, a temperature of 10^-8) it passes 2^127, and a sum of 0 times that is no number.
+constexpr float kLargestOffset = 0x1p24f;
+
 __device__ __forceinline__ float exp2_of(float e) { return __builtin_amdgcn_exp2f(e); }
 
 // The sum against another, larger reference.
@@ -262,7 +266,7 @@ __device__ __forceinline__ float largest(const Logits<TYPE> &v)
 // A thread's sum while it grows.  SECOND: 0 none, 1 times e, 2 without the logits that are marked.  Mostly e is made by one operation, x c -
 // offset with offset = reference c: the product is not rounded, and what the offset's rounding leaves is the same for all terms, so it
 // is taken out at the end.  A vector for which the reference is too low (its sum shows it, so no largest logit is sought) and all where
-// reference c leaves fp32's range are made from the difference.
+// reference c is no longer a small step of fp32 from its product are made from the difference.
 template <int SECOND>
 struct Adder {
     ExpSum s;
@@ -300,7 +304,7 @@ struct Adder {
             if ((top - s.reference) * c > 8.0f) {
                 result();
                 rebase<SECOND == 1>(s, top, c);
-                if (__builtin_fabsf(top * c) < 0x1p100f) offset = top * c;
+                if (__builtin_fabsf(top * c) < kLargestOffset) offset = top * c;
                 shift(residue());
             }
             const float r = residue();
