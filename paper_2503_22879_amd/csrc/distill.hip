@@ -129,7 +129,7 @@ struct Places {
 // What the gradient of a row is made from: that of other tokens is flat 2^((x - reference) c - log), that of the teacher's comes from p and q.
 struct Slope {
     float reference, log, flat;
-    float offset, times;  // 16-bit logits: the same as times 2^(x c - offset), whose rounding is far below the result's; offset +infinity: it is not
+    float offset, times;  // 16-bit logits: the same as times 2^(x c - offset), whose rounding is far below the result's; offset +infinity: times may leave fp32's range
     float own_reference, own_log, whole, scale;
     template <int TYPE>
     __device__ __forceinline__ void of_others(const Logits<TYPE> &x, float c, float (&g)[Logits<TYPE>::kCount]) const
@@ -162,7 +162,7 @@ __device__ __forceinline__ Slope slope_of(const DistillArgs &a, float weight, fl
     s.flat = (rest ? fmaf(s.whole, share, -left) : s.whole) * s.scale;
     const float offset = fmaf(s.reference, a.c, s.log);
     s.times = s.flat * exp2_of(-(fmaf(s.reference, a.c, -offset) + s.log));
-    s.offset = __builtin_fabsf(offset) < 0x1p100f || offset != offset ? offset : __builtin_inff();
+    s.offset = __builtin_fabsf(offset) < kLargestOffset || offset != offset ? offset : __builtin_inff();
     return s;
 }
 

@@ -199,7 +199,7 @@ def test_gradient_of_logprobs_at_temperatures_near_0(gpu_lib, T, kind):
     _check_backward(gpu_lib, x, targets, forward, g, h, T)
 
 
-@pytest.mark.parametrize("kind", ["fp32"])
+@pytest.mark.parametrize("kind", ["fp32", "bf16"])
 @pytest.mark.parametrize("rest", [False, True])
 @pytest.mark.parametrize("rows,vocab", STEPS)
 def test_distill_beside_finite_masks(gpu_lib, rows, vocab, rest, kind):
@@ -209,7 +209,7 @@ def test_distill_beside_finite_masks(gpu_lib, rows, vocab, rest, kind):
         _check_steps(gpu_lib, _rows(rows, vocab, kind, mask), teacher, tokens, rest, in_place=mask == MASKS[3])
 
 
-@pytest.mark.parametrize("kind", ["fp32"])
+@pytest.mark.parametrize("kind", TYPES)
 @pytest.mark.parametrize("rest", [False, True])
 @pytest.mark.parametrize("rows,vocab", [(8, 403), (8, 9001), (8, 130001)])
 def test_distill_at_temperatures_near_0(gpu_lib, rows, vocab, rest, kind):
@@ -218,3 +218,22 @@ def test_distill_at_temperatures_near_0(gpu_lib, rows, vocab, rest, kind):
     for T in (2.0 ** -20, 2.0 ** -27, 2.0 ** -60):
         teacher, tokens = _teacher(rows, vocab, rest, T)
         _check_steps(gpu_lib, x, teacher, tokens, rest, T, w=np.linspace(-1, 1, rows) * T)
+
+
+@pytest.mark.parametrize("kind", ["fp32", "bf16"])
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("size", [1e10, -1e10, 1e20, -1e20, 2.0 ** 25, -2.0 ** 31])
+def test_gradient_alone_from_log_sums_of_that_size(gpu_lib, size, rest, kind):
+    """No sum is made here: the log sums are float64's, in fp32."""
+    import torch
+    x = _rows(8, 5003, kind, size)
+    teacher, tokens = _teacher(8, 5003, rest)
+    h = _host(x)
+    want = oracle.ref_distill(h, teacher, tokens, rest)
+    S, R = (_as(np.float32, want[k]) for k in ("log_sums", "log_rests"))
+    dx = torch.full_like(x, 3.0)
+    gpu_lib.quamba_distill_backward(x, _dev(teacher), _dev(tokens, np.int32), _dev(S), _dev(np.ones(8)), dx, log_rests=_dev(R) if rest else None, rest=rest)
+    given = _from_sums(h, want["q"], want["left"], tokens, np.ones(tokens.shape, bool), _as(np.float64, S), _as(np.float64, R), np.ones(8), 1.0)
+    # terms: p, q and p / p_R, each with the roundings of an argument of at most 88 (below that they are 0) and the factor's; the teacher's sum is exact to 6 places' additions
+    most = np.exp(np.minimum(h - S[:, None], 80)) + np.where(rest, np.exp(np.minimum(h - (R if rest else S)[:, None], 80)), 0) + 1
+    _gradient_close(_host(dx), given, kind, U * (4 * 88 + 60) * most)
