@@ -234,7 +234,8 @@ __device__ __forceinline__ void write_loss(const DistillArgs &a, int64_t row, co
     if (s.has_rest(a) && left > 0.0f) loss += left * (logf(left) - ((s.rest_reference - s.reference) * a.per_temperature + (log_rest - log_sum)));
     a.losses[row] = log_sum == log_sum ? loss : log_sum;  // a row without a distribution may have no place that shows it
     if (a.log_sums) a.log_sums[row] = fmaf(s.reference, a.per_temperature, log_sum);
-    if (a.log_rests) a.log_rests[row] = a.rest ? fmaf(s.rest_reference, a.per_temperature, log_rest) : 0.0f;
+    // A rest may have a sum where the row has none: what spoils the row may be a token of the teacher's.
+    if (a.log_rests) a.log_rests[row] = !a.rest ? 0.0f : log_sum == log_sum ? fmaf(s.rest_reference, a.per_temperature, log_rest) : log_sum;
 }
 __device__ __forceinline__ void write_no_loss(const DistillArgs &a, int64_t row)
 {
