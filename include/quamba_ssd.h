@@ -529,7 +529,7 @@ int quamba_token_logprobs(int64_t rows, int64_t vocab, const void *logits, int32
  *   grad_logits  device `type` [rows, vocab], rows grad_stride >= vocab values apart; it may take the logits' place (the same address and
  *                stride) and must not overlap them otherwise
  * Rows of padding, and rows whose gradients are 0, are not read: their gradient is 0.  p is made from log_sums, so its relative error is theirs
- * (2^-24 of |log_sum|).
+ * (2^-24 of |log_sum|; where that passes 1, p is off by a factor of up to its exponential).
  * Errors: as above, and EINVAL for a gradient that overlaps the logits.
  */
 int quamba_token_logprobs_backward(int64_t rows, int64_t vocab, const void *logits, int32_t type, int64_t logits_stride,

@@ -4,6 +4,7 @@ Beside the scan and the steps around it: projections in 8-bit floating point (qu
 (quamba_beam_select, quamba_beam_reorder); examples/beam_search.py runs them together.  On what a model answers: log probabilities of
 given tokens with the entropy and the most likely alternatives (quamba_token_logprobs), the distance from a teacher that such alternatives
 describe (quamba_distill_loss), and the gradients of both by the logits (quamba_token_logprobs_backward, quamba_distill_backward).
+All calls stand outside autograd: a tensor that requires a gradient is read like any other, and what a call writes has no history.
 
 A thin binding over libquamba_ssd.so (C ABI in include/quamba_ssd.h).  Every step of the path runs in the
 library's HIP kernels; this package only marshals arguments.  There is no CPU fallback: calls raise if the

@@ -665,7 +665,8 @@ LogitsWork work_of(bool in_place) { return in_place ? LogitsWork::distance : Log
 // with 8 10.1; of 16000 8.5 and 10.2), more where several workgroups have to share a compute unit so that one's loads go while another computes (4096 rows of
 // 20000 by 1024 threads with 4 vectors 88 us, by 512 with 8 65; of 64000 by 1024 with 8 235 and by 512 with 16 186).  So the most work, that of a rest in 16-bit
 // logits, is left to two workgroups of 512 threads even where each has to read some of its row again, from the caches (4096 rows of 70000 by 1024 with 16
-// vectors 278, by 512 that hold 16 of 32 222; of 128000 414 and 404; without a rest 241 and 218, 375 and 401; 2048 of 50000 in fp32 160 and 165).
+// vectors 278, by 512 that hold 16 of 32 222; of 128000 414 and 404; without a rest 241 and 218, 375 and 401; 2048 of 50000 in fp32 160 and 165; and where each has
+// a unit for itself both take about as long: 96 rows of 128000 21.4 and 21.8, 250 30.1 and 29.5, 257 46.8 and 39.0, 96 of 70000 15.8 and 14.9).
 // Rows of up to twice what 1024 threads hold are cheaper in part than in two launches (2048 of 140000 bf16 logits 210 and 271 us, of 260000 439 and 524; 100 of
 // 200000 24.6 and 27.8).  Few long rows are cut into segments instead.
 LogitsPlan distill_form(int64_t rows, int32_t vocab, int32_t type, bool rest, bool in_place, bool workspace)

@@ -197,11 +197,14 @@ int wave_vectors(int64_t rows, int most) { return (int)std::min<int64_t>(most, s
 // Where a row still takes longer than a second launch that joins segments, it is cut into these, by its logits and not its bytes (by 1024 threads and in
 // segments: 1 row of 70000 bf16 logits 5.8 and 7.3 us, of 70564 fp32 ones 5.9 and 7.3; 13 rows of 100000 both 7.4, with 5 alternatives 11.6 and 10.8; of
 // 166139 10.0 and 7.4, 15.2 and 11.8; 64 rows of 128000 with 20 alternatives 14.4 and 15.2).  Entropies and distances take half as much time again for a
-// logit and are cut earlier (64 rows of 128000 fp32 logits with 20 alternatives and the entropy 21.3 and 17.4; the distance of 1 row of 70000 bf16 ones, 32 places
-// and a rest, 8.1 and 6.4).  Segments are as many as fill the card, but with alternatives half of that and no shorter than 40 vectors for each of them, for the
+// logit.  Without alternatives they are cut from 60000 logits on (1 row of 70000 bf16 ones with the entropy 7.0 and 5.5, the distance with 32 places and a rest 7.9
+// and 6.2), with alternatives up to 64 rows instead of 32 (128000 logits, 20 alternatives, the entropy, in fp32 and bf16: 64 rows 17.3 and 16.5, 16.9 and
+// 15.0; 65 rows 17.3 and 17.1, 16.9 and 16.2; 96 in fp32 17.6 and 19.4; 128 18.1 and 21.0, 17.3 and 18.6: more segments are more to join) and not earlier (35 rows of 48400
+// bf16 logits with 5 and the entropy 10.1 and 10.9, 13 of 45848 9.9 and 10.3; but 6 of 70564 in fp32 with 1 11.1 and 9.4).  Segments are as many as fill the card, but with alternatives half of that and no shorter than 40 vectors for each of them, for the
 // launch that joins them goes through all (4 rows of 150000 with 64 alternatives 21.6 and 16.5 us, 64 of 128000 in bf16 with 20 and the entropy 15.8 and 14.8).
 // In front of a gradient's launch that joins them they cost no launch (held in registers and in segments, 32 places, a rest: 32 rows of 42000 bf16 logits 9.6 and 9.4,
-// of 64000 12.0 and 10.2; 16 of 50000 fp32 ones 12.1, by 1024 threads, and 8.8; 64 rows of 64000 12.3 and 12.6, of 90000 16.2 and 14.1).
+// of 64000 12.0 and 10.2; 16 of 50000 fp32 ones 12.1, by 1024 threads, and 8.8; 64 rows of 64000 12.3 and 12.6, of 90000 16.2 and 14.1; fp32 ones of 61578 in 32 rows 14.0 and 11.7, in 33 14.1 and
+// 11.7, in 64 14.5 and 15.0, in 128 17.9 and 20.9).
 LogitsPlan logits_plan(int64_t rows, int32_t vocab, int32_t type, LogitsWork work, int32_t count, bool entropy, bool workspace)
 {
     const int units = compute_units(), vectors = logit_vectors(vocab, type);
