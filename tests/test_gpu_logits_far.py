@@ -220,6 +220,16 @@ def test_distill_at_temperatures_near_0(gpu_lib, rows, vocab, rest, kind):
         _check_steps(gpu_lib, x, teacher, tokens, rest, T, w=np.linspace(-1, 1, rows) * T)
 
 
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("T", [2.0 ** 20, 2.0 ** 100])
+def test_distill_at_high_temperatures(gpu_lib, T, rest, kind):
+    """Every token is as likely as any other; the weights bring the gradient back into fp32's and fp16's range."""
+    for rows, vocab in ((8, 403), (8, 9001), (8, 130001)):
+        teacher, tokens = _teacher(rows, vocab, rest)
+        _check_steps(gpu_lib, _logits(rows, vocab, kind, vocab), teacher, tokens, rest, T, w=np.linspace(-1, 1, rows) * T)
+
+
 @pytest.mark.parametrize("kind", ["fp32", "bf16"])
 @pytest.mark.parametrize("rest", [False, True])
 @pytest.mark.parametrize("size", [1e10, -1e10, 1e20, -1e20, 2.0 ** 25, -2.0 ** 31])
